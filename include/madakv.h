@@ -8,6 +8,9 @@
  *   stage 4  madakv_select       per-head, per-modality eviction: keep the budgeted top-psi tokens     (Section 3.3, text after Eq. 8)
  *            madakv_compact      gather the kept K/V rows into a ragged per-head cache
  *   stage 5  madakv_decode_attn  cache append and decode attention over the ragged cache                (Eq. 4, Eq. 5)
+ * and two things that a long generation needs beside it and the paper does not have:
+ *   a ragged cache in 4 bits      madakv_compact_quant, madakv_decode_attn_quant, madakv_expand_quant
+ *   a cache that stays bounded    madakv_decode_attn_track, madakv_evict, madakv_evict_quant
  *
  * General rules for every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller (the only host pointers are `cfg` and the
@@ -234,6 +237,83 @@ int madakv_decode_attn_static(const madakv_config* cfg, int32_t layer, const voi
                               const int64_t* seg_off, const int32_t* kept_len, int64_t capacity, void* out,
                               float* lse_out, void* stream);
 
+/* ---- The ragged cache in 4 bits. (No counterpart in the paper.) ---------------------------------------------------
+ * In the place of k_c and v_c [capacity, d] a cache row of K (and one of V) has d / 2 bytes of codes and, for each of
+ * its d / 32 groups of 32 elements, a pair of bf16 parameters (step, mid): 80 bytes for d = 128, 40 for d = 64.
+ *   k_code, v_code [capacity, d / 2] uint8;  k_par, v_par [capacity, d / 32, 2] bf16, step first
+ *   With lo, hi the extremes of a group:
+ *     mid = bf16((lo + hi) / 2)    step = bf16((hi - lo) / 15)      (rounded to fp32, then to bf16)
+ *     code(x) = floor((x - mid) / step) + 8, brought into [0, 15]; 8 if step = 0
+ *     value   = mid + (code - 7.5) * step
+ *   so a value is at most half a step from x, plus what the roundings of mid and step move the outermost levels by. A group with
+ *   a NaN or an infinity (or a mid beyond bf16's range) gets mid = step = NaN: all its values are NaN.
+ *   The code of element 32 G + 4 i + e (G < d / 32, i < 8, e < 4) is nibble e (the lowest first) of the little-endian 16-bit word
+ *   i * (d / 32) + G of its row.
+ * Segments, seg_off, kept_len, kept_idx and capacity are those of the ragged cache above; all four arrays start on a
+ * 16-byte boundary and are contiguous.                                                                        */
+
+/* Stage 4b into the cache in 4 bits: madakv_compact's rows, quantised. Same arguments otherwise. */
+int madakv_compact_quant(const madakv_config* cfg, const void* k, const void* v, madakv_strides skv, const int32_t* kept_idx,
+                         const int64_t* seg_off, const int32_t* kept_len, uint8_t* k_code, void* k_par, uint8_t* v_code,
+                         void* v_par, int64_t capacity, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows of the cache in 4 bits back in cfg->dtype (the value above, computed in fp32 and rounded once): k_out[j, :] and
+ * v_out[j, :] are the values of cache row rows[j] for j < n_rows, of row j where `rows` is null (n_rows <= capacity then). A row
+ * outside [0, capacity) gives zeros. rows [n_rows] int64 or null; k_out, v_out [n_rows, d] dtype, contiguous. No workspace. */
+int madakv_expand_quant(const madakv_config* cfg, const int64_t* rows, int64_t n_rows, const uint8_t* k_code,
+                        const void* k_par, const uint8_t* v_code, const void* v_par, int64_t capacity, void* k_out,
+                        void* v_out, void* stream);
+
+/* Stage 5 on the cache in 4 bits: madakv_decode_attn with the values of the codes in the place of k_c and v_c. An appended row
+ * (k_new, v_new in dtype) is quantised first, and attention sees its quantised values. Accumulation is fp32, out is
+ * rounded to dtype once. A NaN among the values or queries gives NaN in out and lse. g <= 8 for fp32, g <= 16 for bf16.
+ * acc, scratch, kept_idx, position, decay: as for madakv_decode_attn_track; acc null (with the other three) for a call without
+ * tracking.                                                                                                   */
+int madakv_decode_attn_quant(const madakv_config* cfg, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                             uint8_t* k_code, void* k_par, uint8_t* v_code, void* v_par, const int64_t* seg_off,
+                             int32_t* kept_len, int64_t capacity, void* out, float* lse_out, float* acc, float* scratch,
+                             int32_t* kept_idx, const int32_t* position, float decay, void* ws, size_t ws_bytes,
+                             void* stream);
+
+/* ---- A cache that stays bounded. (No counterpart in the paper, whose eviction ends with prefill: Eq. 4 adds a row per head
+ * and step. Here the decode steps sum up every row's attention weight, the quantity that Eq. 7 sums over the proxy tokens, and a
+ * segment that has outgrown its limit loses the rows with the smallest sums.) ------------------------------------------------ */
+
+/* Stage 5 with tracking: madakv_decode_attn (same out, lse_out and cache, to the bit), and for every row of the segments that
+ * the call attends over
+ *   acc[seg_off[u] + j] = decay * acc[seg_off[u] + j] + sum over the g query heads of the softmax weight of row j
+ * A row that this call appends starts from 0, and its kept_idx becomes position[b]. A head that has no softmax (no row, or
+ * logits that are not numbers) adds nothing; where a bounded wait ran out (MADAKV_ETIMEOUT) the segment's acc stays as it was.
+ *   acc      [capacity] fp32, in and out. Zeros to begin with, or psi at the kept positions
+ *   scratch  [capacity, g] fp32, 16-byte aligned, overwritten (the step's logits); calls in flight at once need one each
+ *   kept_idx [capacity] int32, position [B] int32: both null if positions are not kept up (eviction then may protect
+ *            no recent rows); otherwise position[b] is the new token's position in sequence b
+ *   decay    in [0, 1]; 1 sums all steps alike                                                                */
+int madakv_decode_attn_track(const madakv_config* cfg, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                             void* k_c, void* v_c, const int64_t* seg_off, int32_t* kept_len, int64_t capacity, void* out,
+                             float* lse_out, float* acc, float* scratch, int32_t* kept_idx, const int32_t* position,
+                             float decay, void* ws, size_t ws_bytes, void* stream);
+
+/* Eviction by accumulated weight, in place. Of every unit u of layer `layer` (all layers when layer = -1) with
+ * kept_len[u] > limit[u] the call keeps c = max(limit[u], protected rows) rows (nothing happens if that is all of them):
+ *   the protected rows, whose position kept_idx is above newest - recent, newest the largest position of the segment;
+ *   then the rows with the largest acc (one that is not > 0, NaN included, counts as 0; equal ones: the lower row first).
+ * Rows at and behind c that stay move into the rows below c that go, the first into the first and so on, with their acc
+ * and kept_idx; kept_len[u] = c. No other row is written, those at and behind c keep their contents. (So the rows of
+ * a segment are no longer in the order of their positions; attention does not depend on that order, and kept_idx says it.)
+ *   limit    [B, L, H_kv] int32 (a negative one counts as 0); recent >= 0
+ *   acc, kept_idx [capacity], as madakv_decode_attn_track keeps them
+ * A segment that does not fit its slot or the capacity, or is longer than max_seq_len + max_new_tokens, is left as it is.
+ * MADAKV_EUNSUPPORTED if max_seq_len + max_new_tokens exceeds 1572864.                                        */
+int madakv_evict(const madakv_config* cfg, int32_t layer, const int32_t* limit, int32_t recent, float* acc, int32_t* kept_idx,
+                 const int64_t* seg_off, int32_t* kept_len, int64_t capacity, void* k_c, void* v_c, void* ws,
+                 size_t ws_bytes, void* stream);
+
+/* The same on the cache in 4 bits. */
+int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* limit, int32_t recent, float* acc,
+                       int32_t* kept_idx, const int64_t* seg_off, int32_t* kept_len, int64_t capacity, uint8_t* k_code,
+                       void* k_par, uint8_t* v_code, void* v_par, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronises `stream`, copies the device status word (a madakv_status) to *status_out and clears it. */
 int madakv_poll_status(void* ws, void* stream, int32_t* status_out);
 
@@ -242,7 +322,9 @@ const char* madakv_status_string(int status);
 /* Library version, bumped when the ABI changes. 2: madakv_score_lse, madakv_allocate_layer and MADAKV_HCC_DEMAND added
  * (nothing that version 1 had was changed). 3: madakv_config grew by keep_window and pool_kernel (struct_size is
  * checked: a caller built against version 2 gets MADAKV_EINVAL, not a misread struct). 4: madakv_demand_layer
- * added, madakv_allocate_layer accepts psi = NULL (nothing that version 3 had was changed). */
+ * added, madakv_allocate_layer accepts psi = NULL (nothing that version 3 had was changed). Calls that were added since (the
+ * cache in 4 bits, tracking and eviction) changed nothing that version 4 had and left the number as it is: a program that
+ * may meet an older library of version 4 looks their symbols up. */
 int madakv_abi_version(void);
 
 #ifdef __cplusplus

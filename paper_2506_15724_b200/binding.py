@@ -24,6 +24,8 @@ EXPORTS = [
     "madakv_abi_version", "madakv_status_string", "madakv_workspace_bytes", "madakv_score", "madakv_score_lse",
     "madakv_allocate", "madakv_allocate_layer", "madakv_demand_layer",
     "madakv_select", "madakv_compact", "madakv_decode_attn", "madakv_decode_attn_static", "madakv_poll_status",
+    "madakv_compact_quant", "madakv_expand_quant", "madakv_decode_attn_quant", "madakv_decode_attn_track", "madakv_evict",
+    "madakv_evict_quant",
 ]
 
 
@@ -75,6 +77,13 @@ def lib():
         L.madakv_compact.argtypes = [cfgp, vp, vp, MadakvStrides, vp, vp, vp, vp, vp, i64, vp, sz, vp]
         L.madakv_decode_attn.argtypes = [cfgp, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
         L.madakv_decode_attn_static.argtypes = [cfgp, i32, vp, vp, vp, vp, vp, i64, vp, vp, vp]
+        f32 = ctypes.c_float
+        L.madakv_compact_quant.argtypes = [cfgp, vp, vp, MadakvStrides, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+        L.madakv_expand_quant.argtypes = [cfgp, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp]
+        L.madakv_decode_attn_quant.argtypes = [cfgp, i32] + [vp] * 9 + [i64] + [vp] * 6 + [f32, vp, sz, vp]
+        L.madakv_decode_attn_track.argtypes = [cfgp, i32] + [vp] * 7 + [i64] + [vp] * 6 + [f32, vp, sz, vp]
+        L.madakv_evict.argtypes = [cfgp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.madakv_evict_quant.argtypes = [cfgp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
         L.madakv_poll_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         for f in EXPORTS:
             if f not in ("madakv_status_string",):
@@ -192,6 +201,50 @@ def madakv_decode_attn_static(cfg, layer, q, k_c, v_c, seg_off, kept_len, out, l
                                                                         _stream()))
 
 
+# The calls from here on check their tensors against the config: a wrong dtype, size or device, or a tensor that is not contiguous
+# (k and v of compaction may be strided), raises ValueError before anything is launched.
+def madakv_compact_quant(cfg, k, v, kept_idx, seg_off, kept_len, k_code, k_par, v_code, v_par, ws):
+    rc = _native.compact_quant(cfg, k, v, kept_idx, seg_off, kept_len, k_code, k_par, v_code, v_par, ws)
+    if rc:
+        raise MadakvError("madakv_compact_quant", rc)
+
+
+def madakv_expand_quant(cfg, rows, k_code, k_par, v_code, v_par, k_out, v_out):
+    """rows (int64) may be None: all rows of the cache."""
+    rc = _native.expand_quant(cfg, rows, k_code, k_par, v_code, v_par, k_out, v_out)
+    if rc:
+        raise MadakvError("madakv_expand_quant", rc)
+
+
+def madakv_decode_attn_quant(cfg, layer, q, k_new, v_new, k_code, k_par, v_code, v_par, seg_off, kept_len, out, lse_out, ws,
+                             acc=None, scratch=None, kept_idx=None, position=None, decay=1.0):
+    """With acc and scratch the call also accumulates every row's attention weight (see madakv_decode_attn_track)."""
+    rc = _native.decode_attn_quant(cfg, layer, q, k_new, v_new, k_code, k_par, v_code, v_par, seg_off, kept_len, out, lse_out, ws,
+                                   acc, scratch, kept_idx, position, decay)
+    if rc:
+        raise MadakvError("madakv_decode_attn_quant", rc)
+
+
+def madakv_decode_attn_track(cfg, layer, q, k_new, v_new, k_c, v_c, seg_off, kept_len, out, lse_out, ws, acc, scratch,
+                             kept_idx=None, position=None, decay=1.0):
+    rc = _native.decode_attn_track(cfg, layer, q, k_new, v_new, k_c, v_c, seg_off, kept_len, out, lse_out, ws, acc, scratch,
+                                   kept_idx, position, decay)
+    if rc:
+        raise MadakvError("madakv_decode_attn_track", rc)
+
+
+def madakv_evict(cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_len, k_c, v_c, ws):
+    rc = _native.evict(cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_len, k_c, v_c, ws)
+    if rc:
+        raise MadakvError("madakv_evict", rc)
+
+
+def madakv_evict_quant(cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_len, k_code, k_par, v_code, v_par, ws):
+    rc = _native.evict_quant(cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_len, k_code, k_par, v_code, v_par, ws)
+    if rc:
+        raise MadakvError("madakv_evict_quant", rc)
+
+
 def madakv_poll_status(ws):
     out = ctypes.c_int32(0)
     _check("madakv_poll_status", lib().madakv_poll_status(_ptr(ws), _stream(), ctypes.byref(out)))
@@ -203,15 +256,18 @@ def madakv_status_string(code):
 
 
 class EvictionBuffers:
-    """Device tensors the five calls write (allocated once through torch; no arithmetic here)."""
+    """Device tensors the calls write (allocated once through torch; no arithmetic here).
 
-    def __init__(self, cfg, capacity_rows, device="cuda", want_lse=False):
+    quant: the ragged cache is held in 4 bits (k_code, k_par, v_code, v_par in the place of k_c and v_c).
+    track: decode steps accumulate every row's attention weight in `acc`, so that run_trim can cut segments back."""
+
+    def __init__(self, cfg, capacity_rows, device="cuda", want_lse=False, quant=False, track=False):
         B, L, Hq, Hkv = cfg.batch, cfg.n_layers, cfg.n_q_heads, cfg.n_kv_heads
         d, n = cfg.head_dim, cfg.max_seq_len
         units = B * L * Hkv
         dt = torch.float32 if cfg.dtype == MADAKV_F32 else torch.bfloat16
         z = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
-        self.cfg = cfg
+        self.cfg, self.quant, self.track = cfg, quant, track
         self.ws = new_workspace(cfg, device)
         self.psi = z((B, L, Hkv, n), torch.float32)
         self.lse = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
@@ -223,8 +279,17 @@ class EvictionBuffers:
         self.kept_len = z((units,), torch.int32)
         self.seg_off = z((units + 1,), torch.int64)
         self.kept_idx = torch.full((capacity_rows,), -1, dtype=torch.int32, device=device)
-        self.k_c = z((capacity_rows, d), dt)
-        self.v_c = z((capacity_rows, d), dt)
+        if quant:
+            self.k_code, self.v_code = (z((capacity_rows, d // 2), torch.uint8) for _ in range(2))
+            self.k_par, self.v_par = (z((capacity_rows, d // 32, 2), torch.bfloat16) for _ in range(2))
+            self.cache = (self.k_code, self.k_par, self.v_code, self.v_par)
+        else:
+            self.k_c = z((capacity_rows, d), dt)
+            self.v_c = z((capacity_rows, d), dt)
+            self.cache = (self.k_c, self.v_c)
+        if track:
+            self.acc = z((capacity_rows,), torch.float32)
+            self.scratch = z((capacity_rows, Hq // Hkv), torch.float32)
         self.out = z((B, L, Hq, d), dt)
         self.lse_dec = z((B, L, Hq), torch.float32)
 
@@ -235,8 +300,22 @@ class EvictionBuffers:
         madakv_allocate(c, self.psi, mask, seq_len, budget, self.mass, self.pref, self.demand, self.phi, self.budgets,
                         self.ws)
         madakv_select(c, self.psi, mask, seq_len, self.budgets, self.kept_len, self.seg_off, self.kept_idx, self.ws)
-        madakv_compact(c, k, v, self.kept_idx, self.seg_off, self.kept_len, self.k_c, self.v_c, self.ws)
+        compact = madakv_compact_quant if self.quant else madakv_compact
+        compact(c, k, v, self.kept_idx, self.seg_off, self.kept_len, *self.cache, self.ws)
+        if self.track:
+            self.acc.zero_()
 
-    def run_decode(self, q, k_new=None, v_new=None, layer=-1):
-        madakv_decode_attn(self.cfg, layer, q, k_new, v_new, self.k_c, self.v_c, self.seg_off, self.kept_len, self.out,
-                           self.lse_dec, self.ws)
+    def run_decode(self, q, k_new=None, v_new=None, layer=-1, position=None, decay=1.0):
+        """One decode step. With tracking, position [B] int32 says where the new tokens stand (None: kept_idx is not kept up)."""
+        head = (self.cfg, layer, q, k_new, v_new, *self.cache, self.seg_off, self.kept_len, self.out, self.lse_dec, self.ws)
+        if not (self.quant or self.track):
+            return madakv_decode_attn(*head)
+        tracked = ()
+        if self.track:
+            tracked = (self.acc, self.scratch, self.kept_idx if position is not None else None, position, decay)
+        (madakv_decode_attn_quant if self.quant else madakv_decode_attn_track)(*head, *tracked)
+
+    def run_trim(self, limit, recent=0, layer=-1):
+        """Segments longer than limit [B, L, H_kv] int32 lose their rows of the smallest accumulated weight; needs track."""
+        call = madakv_evict_quant if self.quant else madakv_evict
+        call(self.cfg, layer, limit, recent, self.acc, self.kept_idx, self.seg_off, self.kept_len, *self.cache, self.ws)

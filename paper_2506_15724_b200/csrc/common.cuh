@@ -255,6 +255,18 @@ __device__ __forceinline__ unsigned arrive_inc(unsigned* counter, unsigned last)
 __device__ __forceinline__ void set_status(void* ws, int code) { atomicCAS((int*)ws, 0, code); }
 #endif
 
+// What a decode call with tracking keeps beside its attention (see madakv_decode_attn_track).
+struct Tracking {
+  float* acc;
+  float* scores;
+  int32_t* kept_idx;
+  const int32_t* position;
+  float decay;
+};
+// The heads' log2-sum-exps [B * L * H_q] on their way from a decode kernel to accumulate_kernel: the place where scoring keeps its
+// rows' (at least as many; the two stages of one workspace never run at once).
+inline float* tracking_lse2(const madakv_config& c, void* ws) { return reinterpret_cast<float*>((char*)ws + ws_layout(c).score_lse_off); }
+
 // Stage launchers implemented in the .cu files (all return a madakv_status).
 int launch_score(const madakv_config& c, const void* q, madakv_strides sq, const void* k, madakv_strides sk,
                  const int32_t* seq_len, float* lse, float* psi, void* ws, cudaStream_t st);
@@ -288,6 +300,23 @@ int launch_compact(const madakv_config& c, const void* k, const void* v, madakv_
                    cudaStream_t st);
 int launch_decode(const madakv_config& c, int layer, const void* q, const void* k_new, const void* v_new, void* k_c,
                   void* v_c, const int64_t* seg_off, int32_t* kept_len, int64_t capacity, void* out, float* lse_out,
-                  void* ws, cudaStream_t st);
+                  const Tracking* track, void* ws, cudaStream_t st);
+int launch_decode_quant(const madakv_config& c, int layer, const void* q, const void* k_new, const void* v_new, uint8_t* k_code,
+                        void* k_par, uint8_t* v_code, void* v_par, const int64_t* seg_off, int32_t* kept_len, int64_t capacity,
+                        void* out, float* lse_out, const Tracking* track, void* ws, cudaStream_t st);
+int launch_accumulate(const madakv_config& c, int layer, const int64_t* seg_off, const int32_t* kept_len, int64_t capacity,
+                      const Tracking& track, void* ws, cudaStream_t st);
+int launch_compact_quant(const madakv_config& c, const void* k, const void* v, madakv_strides s, const int32_t* kept_idx,
+                         const int64_t* seg_off, const int32_t* kept_len, uint8_t* k_code, void* k_par, uint8_t* v_code,
+                         void* v_par, int64_t capacity, cudaStream_t st);
+int launch_expand_quant(const madakv_config& c, const int64_t* rows, int64_t n_rows, const uint8_t* k_code, const void* k_par,
+                        const uint8_t* v_code, const void* v_par, int64_t capacity, void* k_out, void* v_out, cudaStream_t st);
+// One array of rows that eviction moves: `bytes` per row, a multiple of 8.
+struct RowArray {
+  void* base;
+  int bytes;
+};
+int launch_evict(const madakv_config& c, int layer, const int32_t* limit, int recent, float* acc, int32_t* kept_idx,
+                 const int64_t* seg_off, int32_t* kept_len, int64_t capacity, const RowArray (&rows)[4], cudaStream_t st);
 
 }  // namespace madakv

@@ -2,9 +2,12 @@
 // status comes back as an int. What bounds a call on one layer is the host: with the arguments gathered in Python and handed
 // over by ctypes a decode call took 5.4 us, here 3.1, nearly all of it the launch.
 #define PY_SSIZE_T_CLEAN
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
 
 #include "madakv.h"
 
@@ -213,6 +216,211 @@ PyObject* decode_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the cache in 4 bits, tracking, eviction: tensors are checked against the config before their pointers are passed on
+struct Checked : Args {
+  const madakv_config* cfg;
+  int64_t units, heads;  // (sequence, layer, KV head)s; (sequence, layer, query head)s
+  int bad_config = MADAKV_OK;
+  c10::DeviceIndex device;
+
+  Checked(PyObject* const* args, Py_ssize_t n, Py_ssize_t want) : Args(args, n, want) {
+    cfg = config();
+    size_t bytes;
+    bad_config = madakv_workspace_bytes(cfg, &bytes);  // (before its numbers are used)
+    units = (int64_t)cfg->batch * cfg->n_layers * cfg->n_kv_heads;
+    heads = (int64_t)cfg->batch * cfg->n_layers * cfg->n_q_heads;
+    device = c10::cuda::current_device();
+  }
+  [[noreturn]] static void wrong(const char* name, const char* what) {
+    PyErr_Format(PyExc_ValueError, "%s: %s", name, what);
+    throw python_error();
+  }
+  at::ScalarType dtype() const { return cfg->dtype == MADAKV_F32 ? at::kFloat : at::kBFloat16; }
+  const at::Tensor& on_device(PyObject* o, const char* name, at::ScalarType type) {
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.device().index() != device) wrong(name, "expected a tensor on the current CUDA device");
+    if (t.scalar_type() != type) wrong(name, "wrong dtype");
+    return t;
+  }
+  // A contiguous tensor of at least `least` elements (exactly so many with `exact`).
+  template <typename P = void>
+  P* array(const char* name, at::ScalarType type, int64_t least, bool optional = false, bool exact = false) {
+    PyObject* o = next();
+    if (optional && o == Py_None) return nullptr;
+    const at::Tensor& t = on_device(o, name, type);
+    if (!t.is_contiguous()) wrong(name, "expected a contiguous tensor");
+    if (t.numel() < least || (exact && t.numel() != least)) wrong(name, "wrong size for this config and cache");
+    return static_cast<P*>(t.data_ptr());
+  }
+  // [capacity, row] of a cache; its first array says the capacity
+  template <typename P = void>
+  P* cache(const char* name, at::ScalarType type, int64_t row, int64_t& capacity) {
+    if (capacity < 0) {
+      const at::Tensor& t = tensor(*at);
+      if (t.dim() < 2) wrong(name, "expected [capacity, ...]");
+      capacity = t.size(0);
+    }
+    return array<P>(name, type, capacity * row, false, true);
+  }
+  void* strided(const char* name, madakv_strides& st) {  // [B, L, H_kv, at least n_max, d]
+    const at::Tensor& t = on_device(next(), name, dtype());
+    st = strides(t);
+    if (t.size(0) != cfg->batch || t.size(1) != cfg->n_layers || t.size(2) != cfg->n_kv_heads || t.size(3) < cfg->max_seq_len ||
+        t.size(4) != cfg->head_dim)
+      wrong(name, "wrong size for this config");
+    return t.data_ptr();
+  }
+  void* workspace(size_t& bytes) {
+    const at::Tensor& t = tensor();
+    if (!t.is_cuda() || t.device().index() != device || !t.is_contiguous()) wrong("ws", "expected a contiguous tensor on the current CUDA device");
+    bytes = t.nbytes();
+    return t.data_ptr();
+  }
+  float real() {
+    const double v = PyFloat_AsDouble(next());
+    if (v == -1.0 && PyErr_Occurred()) throw python_error();
+    return (float)v;
+  }
+};
+
+struct QuantCache {
+  uint8_t *k_code, *v_code;
+  void *k_par, *v_par;
+  int64_t capacity = -1;
+  explicit QuantCache(Checked& a) {
+    const int64_t d = a.cfg->head_dim;
+    k_code = a.cache<uint8_t>("k_code", at::kByte, d / 2, capacity);
+    k_par = a.cache("k_par", at::kBFloat16, d / 16, capacity);
+    v_code = a.cache<uint8_t>("v_code", at::kByte, d / 2, capacity);
+    v_par = a.cache("v_par", at::kBFloat16, d / 16, capacity);
+  }
+};
+
+PyObject* compact_quant(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Checked a(args, n, 11);
+  if (a.bad_config) return PyLong_FromLong(a.bad_config);
+  madakv_strides sk, sv;
+  void *k = a.strided("k", sk), *v = a.strided("v", sv);
+  if (sk.batch != sv.batch || sk.layer != sv.layer || sk.head != sv.head || sk.token != sv.token)
+    Args::fail(PyExc_AssertionError, "k and v must have the same strides");
+  const int32_t* kept_idx = a.array<int32_t>("kept_idx", at::kInt, 0);
+  const int64_t listed = a.tensor(args[3]).numel();
+  const int64_t* seg_off = a.array<int64_t>("seg_off", at::kLong, a.units + 1);
+  const int32_t* kept_len = a.array<int32_t>("kept_len", at::kInt, a.units);
+  const QuantCache c(a);
+  if (listed < c.capacity) Checked::wrong("kept_idx", "shorter than the cache");
+  size_t bytes;
+  void *ws = a.workspace(bytes), *st = stream();
+  return without_lock([&] {
+    return madakv_compact_quant(a.cfg, k, v, sk, kept_idx, seg_off, kept_len, c.k_code, c.k_par, c.v_code, c.v_par, c.capacity,
+                                ws, bytes, st);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* expand_quant(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Checked a(args, n, 8);
+  if (a.bad_config) return PyLong_FromLong(a.bad_config);
+  const int64_t* rows = a.array<int64_t>("rows", at::kLong, 0, true);
+  const int64_t given = rows || args[1] != Py_None ? a.tensor(args[1]).numel() : -1;
+  const QuantCache c(a);
+  const int64_t d = a.cfg->head_dim, n_rows = given >= 0 ? given : c.capacity;
+  void *k = a.array("k_out", a.dtype(), n_rows * d, false, true), *v = a.array("v_out", a.dtype(), n_rows * d, false, true), *st = stream();
+  if (n_rows == 0) return PyLong_FromLong(MADAKV_OK);  // (empty tensors have no pointers)
+  return without_lock(
+      [&] { return madakv_expand_quant(a.cfg, rows, n_rows, c.k_code, c.k_par, c.v_code, c.v_par, c.capacity, k, v, st); });
+  END_HANDLE_TH_ERRORS
+}
+
+struct Track {
+  float *acc, *scratch;
+  int32_t* kept_idx;
+  const int32_t* position;
+  float decay;
+  Track(Checked& a, int64_t capacity, bool optional) {
+    acc = a.array<float>("acc", at::kFloat, capacity, optional);
+    scratch = a.array<float>("scratch", at::kFloat, capacity * (a.cfg->n_q_heads / a.cfg->n_kv_heads), optional);
+    kept_idx = a.array<int32_t>("kept_idx", at::kInt, capacity, true);
+    position = a.array<int32_t>("position", at::kInt, a.cfg->batch, true);
+    decay = a.real();
+  }
+};
+
+template <bool kQuant>
+PyObject* decode_more(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Checked a(args, n, kQuant ? 19 : 17);
+  if (a.bad_config) return PyLong_FromLong(a.bad_config);
+  const int64_t d = a.cfg->head_dim;
+  const int32_t layer = a.integer();
+  void* q = a.array("q", a.dtype(), a.heads * d, false, true);
+  void *k_new = a.array("k_new", a.dtype(), a.units * d, true, true), *v_new = a.array("v_new", a.dtype(), a.units * d, true, true);
+  int64_t capacity = -1;
+  void *k_c, *v_c, *k_par = nullptr, *v_par = nullptr;
+  if constexpr (kQuant) {
+    const QuantCache c(a);
+    k_c = c.k_code, k_par = c.k_par, v_c = c.v_code, v_par = c.v_par, capacity = c.capacity;
+  } else {
+    k_c = a.cache("k_c", a.dtype(), d, capacity);
+    v_c = a.cache("v_c", a.dtype(), d, capacity);
+  }
+  const int64_t* seg_off = a.array<int64_t>("seg_off", at::kLong, a.units + 1);
+  int32_t* kept_len = a.array<int32_t>("kept_len", at::kInt, a.units);
+  void* out = a.array("out", a.dtype(), a.heads * d, false, true);
+  float* lse = a.array<float>("lse_out", at::kFloat, a.heads, true, true);
+  size_t bytes;
+  void* ws = a.workspace(bytes);
+  const Track t(a, capacity, kQuant);
+  void* st = stream();
+  return without_lock([&] {
+    if constexpr (kQuant)
+      return madakv_decode_attn_quant(a.cfg, layer, q, k_new, v_new, (uint8_t*)k_c, k_par, (uint8_t*)v_c, v_par, seg_off, kept_len,
+                                      capacity, out, lse, t.acc, t.scratch, t.kept_idx, t.position, t.decay, ws, bytes, st);
+    else
+      return madakv_decode_attn_track(a.cfg, layer, q, k_new, v_new, k_c, v_c, seg_off, kept_len, capacity, out, lse, t.acc,
+                                      t.scratch, t.kept_idx, t.position, t.decay, ws, bytes, st);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+template <bool kQuant>
+PyObject* evict(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Checked a(args, n, kQuant ? 13 : 11);
+  if (a.bad_config) return PyLong_FromLong(a.bad_config);
+  const int64_t d = a.cfg->head_dim;
+  const int32_t layer = a.integer();
+  const int32_t* limit = a.array<int32_t>("limit", at::kInt, a.units);
+  const int32_t recent = a.integer();
+  float* acc = a.array<float>("acc", at::kFloat, 0);
+  int32_t* kept_idx = a.array<int32_t>("kept_idx", at::kInt, 0);
+  const int64_t least = std::min(a.tensor(args[4]).numel(), a.tensor(args[5]).numel());
+  const int64_t* seg_off = a.array<int64_t>("seg_off", at::kLong, a.units + 1);
+  int32_t* kept_len = a.array<int32_t>("kept_len", at::kInt, a.units);
+  int64_t capacity = -1;
+  void *k_c, *v_c, *k_par = nullptr, *v_par = nullptr;
+  if constexpr (kQuant) {
+    const QuantCache c(a);
+    k_c = c.k_code, k_par = c.k_par, v_c = c.v_code, v_par = c.v_par, capacity = c.capacity;
+  } else {
+    k_c = a.cache("k_c", a.dtype(), d, capacity);
+    v_c = a.cache("v_c", a.dtype(), d, capacity);
+  }
+  if (least < capacity) Checked::wrong("acc, kept_idx", "shorter than the cache");
+  size_t bytes;
+  void *ws = a.workspace(bytes), *st = stream();
+  return without_lock([&] {
+    if constexpr (kQuant)
+      return madakv_evict_quant(a.cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_len, capacity, (uint8_t*)k_c, k_par,
+                                (uint8_t*)v_c, v_par, ws, bytes, st);
+    else
+      return madakv_evict(a.cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_len, capacity, k_c, v_c, ws, bytes, st);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 PyCFunction as_method(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -226,6 +434,12 @@ PyMethodDef methods[] = {
     {"select", as_method(select), METH_FASTCALL, nullptr},
     {"compact", as_method(compact), METH_FASTCALL, nullptr},
     {"decode_attn", as_method(decode_attn), METH_FASTCALL, nullptr},
+    {"compact_quant", as_method(compact_quant), METH_FASTCALL, nullptr},
+    {"expand_quant", as_method(expand_quant), METH_FASTCALL, nullptr},
+    {"decode_attn_quant", as_method(decode_more<true>), METH_FASTCALL, nullptr},
+    {"decode_attn_track", as_method(decode_more<false>), METH_FASTCALL, nullptr},
+    {"evict", as_method(evict<false>), METH_FASTCALL, nullptr},
+    {"evict_quant", as_method(evict<true>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
