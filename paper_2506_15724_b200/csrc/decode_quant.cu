@@ -1,7 +1,18 @@
 // Stage 5 on a cache in 4 bits: cache append (Eq. 4, the row quantised on the way) and decode attention (Eq. 5).
 //
-// The rows of a segment are shared out over blocks as in decode.cu. A row is shared by D / 4 lanes, four elements each, which turn
-// its codes into values; the g query heads of the KV group share every row read; online softmax in the log2 domain, fp32 accumulation.
+// Bound by HBM at 160 bytes a row (d = 128) only if little is done per code: an SM gets a row of K and V, 256 codes, in seven clocks.
+// So the codes go into the tensor cores as they are and the groups' (step, mid) are applied to sums:
+//   logits   q . k = sum over groups of step sum q (code - 7.5) + mid sum q, the inner sums by m16n8k16 products of 16 rows with 8 heads;
+//            a row's step and mid meet four numbers per thread and group
+//   values   sum of w v = sum of (w step) (code - 7.5) + w mid: the weights take the step of every group before they are rounded to
+//            bf16 for the product with the codes; mid is summed up in fp32
+// A code becomes an operand by a shift and one logical operation: its four bits are bits 3-6 of a bf16 mantissa under the exponent of
+// 16, which makes 16 + code. 23.5 times the sum of the other operand is taken off again: of the queries by where the product's
+// accumulator starts, of the weights by one more product, with ones, per group. The order of codes in a row is that of the operands: a
+// lane's words are one piece of 16 bytes (K) or 8 (V), pairs along d for K, and of two rows for V.
+// fp32 (queries and weights): three bf16 terms each, whose products are exact and whose sum is fp32 again; the operands are
+// code - 7.5 then, so that no sum loses bits to the 23.5.
+// A warp has tiles of 32 rows of its own, read ahead into a ring in shared memory by asynchronous copies.
 #include <type_traits>
 
 #include "decode_common.cuh"
@@ -10,16 +21,75 @@
 namespace madakv {
 namespace {
 
-constexpr int NT = 128;
+constexpr int kWarps = 4, NT = 32 * kWarps;
+constexpr int kTile = 32;    // rows of a warp at a time
+constexpr int kAhead = 3;    // stages of a warp's ring
 
-template <typename T, int D, int G, bool kTrack>
-__global__ void __launch_bounds__(NT) decode_quant_kernel(const __grid_constant__ DecodeParams p) {
+template <int D>
+struct QuantTile {
   using R = QuantRow<D>;
-  constexpr int LANES = R::LANES, GROUPS = NT / LANES, U = 4;
-  __shared__ __align__(16) float s_o[GROUPS * G * D];
-  __shared__ float s_m[GROUPS * G], s_l[GROUPS * G];
-  __shared__ __align__(16) float b_o[G * D];
-  __shared__ float b_m[G], b_l[G], fac[G * kDecodeSlots];
+  static constexpr int K_CODE = 0, K_PAR = kTile * R::CODE_BYTES, V_CODE = K_PAR + kTile * R::PAR_BYTES,
+                       V_PAR = V_CODE + kTile * R::CODE_BYTES, STAGE = V_PAR + kTile * R::PAR_BYTES;
+  static constexpr int WARP = kAhead * STAGE;
+  static constexpr int FRESH = kWarps * WARP;  // the appended row: codes and parameters of K, then of V
+  static constexpr int BYTES = FRESH + 2 * (R::CODE_BYTES + R::PAR_BYTES);
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {  // an 8 x 8 matrix of 16-bit elements, two of a row per lane
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+// Rows kTile apart from a tile's base for the 8 row slots of a product: slots 2 t and 2 t + 1 are neighbours, slots 0, 2, 4, 6 are rows
+// 0, 3, 4, 7, so that neither the loads of K (all slots) nor of V (every other slot) meet more than twice in a bank.
+__device__ __forceinline__ int slot_row(int s) { return s ^ ((s >> 1) & 1); }
+
+// The four operand registers of eight codes, the e-th of either half-word: 16 + code, or code - 7.5.
+template <bool kExact>
+__device__ __forceinline__ void operands(uint32_t x, uint32_t (&r)[4]) {
+  r[0] = ((x << 3) & 0x00780078u) | 0x41804180u;
+  r[1] = ((x >> 1) & 0x00780078u) | 0x41804180u;
+  r[2] = ((x >> 5) & 0x00780078u) | 0x41804180u;
+  r[3] = ((x >> 9) & 0x00780078u) | 0x41804180u;
+  if constexpr (kExact) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __nv_bfloat162 v = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&r[e]), __floats2bfloat162_rn(23.5f, 23.5f));
+      r[e] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+  }
+}
+// The n-th bf16 term of x and y (0: the nearest; what is left goes on to the next).
+__device__ __forceinline__ uint32_t next_term(float& x, float& y) {
+  const uint32_t w = pack_bf16x2(x, y);
+  x -= bf16_lo(w);
+  y -= bf16_hi(w);
+  return w;
+}
+
+// NH: groups of eight query heads.
+template <typename T, int D, int NH, bool kTrack>
+__global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const __grid_constant__ DecodeParams p) {
+  using R = QuantRow<D>;
+  using QT = QuantTile<D>;
+  constexpr int NG = R::NG;
+  constexpr bool kExact = sizeof(T) == 4;
+  constexpr int TERMS = kExact ? 3 : 1;
+  constexpr int KW = D / 32, VW = D / 64;  // words of a row that a lane takes of K and of V
+  constexpr int OPITCH = D + 4;            // floats from one head's merged row to the next
+  static_assert(8 * NH * (OPITCH + 2) * 4 <= QT::WARP && 16 * kDecodeSlots * 4 <= QT::WARP, "the merge reuses the rings");
+  extern __shared__ __align__(128) unsigned char dsmem[];
   pdl_wait();
   pdl_go();
   const int y = blockIdx.x / p.slots, slot = blockIdx.x % p.slots;
@@ -29,115 +99,322 @@ __global__ void __launch_bounds__(NT) decode_quant_kernel(const __grid_constant_
   int row_begin, row_end;
   block_rows(nb, len, slot, row_begin, row_end);  // (empty beyond the nb-th block)
   const int h = u % p.Hkv, bl = u / p.Hkv;
-  const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES, gi = lane % R::NG;
-  const int first = 32 * gi + 4 * (lane / R::NG);  // the lane's elements
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int gid = lane / 4, t = lane % 4;  // fragment coordinates: row slots gid and gid + 8, columns (heads) 2 t and 2 t + 1
+  float* so = reinterpret_cast<float*>(dsmem + warp * QT::WARP);  // the warp's result, once its ring is done with
+  float* bo = reinterpret_cast<float*>(dsmem + QT::WARP);         // the block's: [8 NH][D], [8 NH], [8 NH]
   if (slot < nb) {
     const int64_t off = p.seg_off[u];
-    uint16_t *kc = reinterpret_cast<uint16_t*>(p.k_c) + off * (D / 4) + lane, *vc = reinterpret_cast<uint16_t*>(p.v_c) + off * (D / 4) + lane;
-    uint32_t *kp = reinterpret_cast<uint32_t*>(p.k_par) + off * R::NG + gi, *vp = reinterpret_cast<uint32_t*>(p.v_par) + off * R::NG + gi;
+    const char* src[4] = {(const char*)p.k_c + off * R::CODE_BYTES, (const char*)p.k_par + off * R::PAR_BYTES,
+                          (const char*)p.v_c + off * R::CODE_BYTES, (const char*)p.v_par + off * R::PAR_BYTES};
+    unsigned char* ring = dsmem + warp * QT::WARP;
+    const uint32_t ring_a = smem_addr(ring);
+    auto load_tile = [&](int r, int stage) {
+      const uint32_t dst = ring_a + stage * QT::STAGE;
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const int bytes = a % 2 ? R::PAR_BYTES : R::CODE_BYTES;
+        const int piece = bytes < 16 ? 8 : 16, per_row = bytes / piece;
+        const uint32_t to = dst + (a == 0 ? QT::K_CODE : a == 1 ? QT::K_PAR : a == 2 ? QT::V_CODE : QT::V_PAR);
+#pragma unroll
+        for (int x = lane; x < kTile * per_row; x += 32) {
+          const int rr = x / per_row;
+          // (rows behind the share and the appended one, which another thread is writing, are zeros)
+          const bool valid = r + rr < row_end && r + rr != view.new_row;
+          const char* from = src[a] + (int64_t)(r + (valid ? rr : 0)) * bytes + x % per_row * piece;
+          if (piece == 16)
+            cp_async16(to + x * 16, from, valid);
+          else
+            cp_async8(to + x * 8, from, valid);
+        }
+      }
+    };
+    const int r_first = row_begin + kTile * warp;
+#pragma unroll
+    for (int s = 0; s < kAhead - 1; ++s) {
+      if (r_first + kTile * kWarps * s < row_end) load_tile(r_first + kTile * kWarps * s, s);
+      cp_async_commit();
+    }
+    // the appended row: quantised into the cache and, for the tile that holds it, into shared memory
     if (view.new_row >= row_begin && view.new_row < row_end) {
-      if (threadIdx.x < 32) {
+      if (warp < 2) {
+        const int l = lane % R::LANES, G = l % NG;
         float x[4];
         uint32_t codes, par;
-        load4(reinterpret_cast<const T*>(p.k_new) + (int64_t)u * D + first, x);
+        load4(reinterpret_cast<const T*>(warp ? p.v_new : p.k_new) + (int64_t)u * D + 32 * G + 4 * (l / NG), x);
         quantise4<D>(x, codes, par);
-        if (grp == 0) {
-          kc[(int64_t)view.new_row * (D / 4)] = (uint16_t)codes;
-          if (lane < R::NG) kp[(int64_t)view.new_row * R::NG] = par;
+        unsigned char* fresh = dsmem + QT::FRESH + warp * (R::CODE_BYTES + R::PAR_BYTES);
+        const int64_t row = off + view.new_row;
+        if (lane < R::LANES) {
+          reinterpret_cast<uint16_t*>(fresh)[l] = (uint16_t)codes;
+          reinterpret_cast<uint16_t*>(warp ? p.v_c : p.k_c)[row * (D / 4) + l] = (uint16_t)codes;
         }
-        load4(reinterpret_cast<const T*>(p.v_new) + (int64_t)u * D + first, x);
-        quantise4<D>(x, codes, par);
-        if (grp == 0) {
-          vc[(int64_t)view.new_row * (D / 4)] = (uint16_t)codes;
-          if (lane < R::NG) vp[(int64_t)view.new_row * R::NG] = par;
+        if (lane < NG) {
+          reinterpret_cast<uint32_t*>(fresh + R::CODE_BYTES)[l] = par;
+          reinterpret_cast<uint32_t*>(warp ? p.v_par : p.k_par)[row * NG + l] = par;
         }
       }
       __syncthreads();
     }
-    float qr[G][4], m[G], l[G], o[G][4];
+
+    // queries as B operands: products j = 0, 1 of group G pair element 8 t + 2 j + {0, 1} with 8 t + 4 + 2 j + {0, 1}; and their sums
+    uint32_t qb[NH][TERMS][NG][2][2];
+    float qsum[NH][NG][2];
 #pragma unroll
-    for (int i = 0; i < G; ++i) {
-      m[i] = -INFINITY;
-      l[i] = 0.f;
+    for (int n = 0; n < NH; ++n)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) qr[i][c] = o[i][c] = 0.f;
-      if (i < p.g) load4(reinterpret_cast<const T*>(p.q) + ((int64_t)bl * p.Hq + h * p.g + i) * D + first, qr[i]);
+      for (int G = 0; G < NG; ++G) {
+        float x[8], sum = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) qr[i][c] *= p.scale2;
-    }
-    for (int r0 = row_begin; r0 < row_end; r0 += GROUPS * U) {
-      float sc[G][U], vf[U][4];
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        const int64_t r = min(r0 + GROUPS * j + grp, row_end - 1);
-        float kf[4];
-        values4(kc[r * (D / 4)], kp[r * R::NG], kf);
-        values4(vc[r * (D / 4)], vp[r * R::NG], vf[j]);
-#pragma unroll
-        for (int i = 0; i < G; ++i) sc[i][j] = qr[i][0] * kf[0] + qr[i][1] * kf[1] + qr[i][2] * kf[2] + qr[i][3] * kf[3];
-      }
-#pragma unroll
-      for (int sh = LANES / 2; sh >= 1; sh >>= 1)
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-          for (int j = 0; j < U; ++j) sc[i][j] += __shfl_xor_sync(0xffffffffu, sc[i][j], sh);
-#pragma unroll
-      for (int i = 0; i < G; ++i) {
-        float mn = m[i];
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-          const int r = r0 + GROUPS * j + grp;
-          if (kTrack && lane == i && i < p.g && r < row_end) p.scores[(off + r) * p.g + i] = sc[i][j];
-          if (r >= row_end) sc[i][j] = -INFINITY;
-          mn = fmaxf(mn, sc[i][j]);
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        if (8 * n + gid < p.g) {
+          const T* q = reinterpret_cast<const T*>(p.q) + ((int64_t)bl * p.Hq + h * p.g + 8 * n + gid) * D + 32 * G + 8 * t;
+          load4(q, *reinterpret_cast<float(*)[4]>(x));
+          load4(q + 4, *reinterpret_cast<float(*)[4]>(x + 4));
         }
-        const float base = mn == -INFINITY ? 0.f : mn;
-        const float f = fast_ex2(m[i] - base);
-        l[i] *= f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[i][c] *= f;
-        m[i] = mn;
+        for (int e = 0; e < 8; ++e) sum += x[e];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        qsum[n][G][0] = __shfl_sync(0xffffffffu, sum, 8 * t);  // heads 2 t, 2 t + 1
+        qsum[n][G][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-          const float w = fast_ex2(sc[i][j] - base);
-          l[i] += w;
-          if (r0 + GROUPS * j + grp < row_end) {  // (the row read in its place may hold anything)
+        for (int term = 0; term < TERMS; ++term)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) o[i][c] = fmaf(w, vf[j][c], o[i][c]);
+          for (int j = 0; j < 2; ++j) {
+            qb[n][term][G][j][0] = next_term(x[2 * j], x[2 * j + 4]);
+            qb[n][term][G][j][1] = next_term(x[2 * j + 1], x[2 * j + 5]);
+          }
+      }
+
+    float m[NH][2], l[NH][2];
+    float o[NH][NG][2][4], ones[NH][NG][4], mids[NH][NG][2];
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+      for (int G = 0; G < NG; ++G) {
+        mids[n][G][0] = mids[n][G][1] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ones[n][G][c] = o[n][G][0][c] = o[n][G][1][c] = 0.f;
+      }
+    }
+    for (int it = 0;; ++it) {
+      const int r = r_first + kTile * kWarps * it;
+      if (r >= row_end) break;
+      const int ahead = r + kTile * kWarps * (kAhead - 1);
+      if (ahead < row_end) load_tile(ahead, (it + kAhead - 1) % kAhead);
+      cp_async_commit();
+      cp_async_wait<kAhead - 1>();
+      __syncwarp();
+      unsigned char* st = ring + it % kAhead * QT::STAGE;
+      if (view.new_row >= r && view.new_row < r + kTile) {
+        const int row = view.new_row - r;
+        const uint32_t* fresh = reinterpret_cast<const uint32_t*>(dsmem + QT::FRESH);
+        constexpr int CW = R::CODE_BYTES / 4;
+        if (lane < CW) {
+          reinterpret_cast<uint32_t*>(st + QT::K_CODE)[row * CW + lane] = fresh[lane];
+          reinterpret_cast<uint32_t*>(st + QT::V_CODE)[row * CW + lane] = fresh[CW + NG + lane];
+        }
+        if (lane < NG) {
+          reinterpret_cast<uint32_t*>(st + QT::K_PAR)[row * NG + lane] = fresh[CW + lane];
+          reinterpret_cast<uint32_t*>(st + QT::V_PAR)[row * NG + lane] = fresh[2 * CW + NG + lane];
+        }
+        __syncwarp();
+      }
+
+      // logits of row slots gid (c = 0, 1) and gid + 8 (c = 2, 3) of both halves, heads 2 t (c even) and 2 t + 1
+      float s[NH][2][4];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t kw[2][KW], kp[2][NG];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = 16 * half + 8 * e + slot_row(gid);
+#pragma unroll
+          for (int x = 0; x < KW; ++x) kw[e][x] = reinterpret_cast<const uint32_t*>(st + QT::K_CODE)[row * (D / 8) + t * KW + x];
+#pragma unroll
+          for (int G = 0; G < NG; ++G) kp[e][G] = reinterpret_cast<const uint32_t*>(st + QT::K_PAR)[row * NG + G];
+        }
+#pragma unroll
+        for (int n = 0; n < NH; ++n) s[n][half][0] = s[n][half][1] = s[n][half][2] = s[n][half][3] = 0.f;
+#pragma unroll
+        for (int G = 0; G < NG; ++G) {
+          uint32_t a[2][4];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)  // elements 8 t .. + 3 of the group in the low half, + 4 .. + 7 in the high
+            operands<kExact>(__byte_perm(kw[e][G / 2], kw[e][KW / 2 + G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
+          const uint32_t a0[4] = {a[0][0], a[1][0], a[0][1], a[1][1]}, a1[4] = {a[0][2], a[1][2], a[0][3], a[1][3]};
+          const float step[2] = {bf16_lo(kp[0][G]), bf16_lo(kp[1][G])}, mid[2] = {bf16_hi(kp[0][G]), bf16_hi(kp[1][G])};
+#pragma unroll
+          for (int n = 0; n < NH; ++n) {
+            float c[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[j] = kExact ? 0.f : -23.5f * qsum[n][G][j & 1];
+#pragma unroll
+            for (int term = TERMS - 1; term >= 0; --term) {
+              mma_bf16_16816(c, a0, qb[n][term][G][0][0], qb[n][term][G][0][1]);
+              mma_bf16_16816(c, a1, qb[n][term][G][1][0], qb[n][term][G][1][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              s[n][half][j] = fmaf(step[j >> 1], c[j], fmaf(mid[j >> 1], qsum[n][G][j & 1], s[n][half][j]));
           }
         }
       }
-    }
+      const bool whole = r + kTile <= row_end;
 #pragma unroll
-    for (int i = 0; i < G; ++i) {
-      if (lane == 0) {
-        s_m[grp * G + i] = m[i];
-        s_l[grp * G + i] = l[i];
+      for (int n = 0; n < NH; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int row = r + 16 * half + 8 * (j >> 1) + slot_row(gid), head = 8 * n + 2 * t + (j & 1);
+            s[n][half][j] *= p.scale2;
+            if (kTrack && row < row_end && head < p.g) p.scores[(off + row) * p.g + head] = s[n][half][j];
+            if (!whole && row >= row_end) s[n][half][j] = -INFINITY;
+          }
+      // one softmax step; the weights become w, the sums of the steps before get their factor
+#pragma unroll
+      for (int n = 0; n < NH; ++n) {
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float mx = fmaxf(fmaxf(s[n][0][e], s[n][0][e + 2]), fmaxf(s[n][1][e], s[n][1][e + 2]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          const float mn = fmaxf(m[n][e], mx), base = mn == -INFINITY ? 0.f : mn;
+          f[e] = fast_ex2(m[n][e] - base);
+          m[n][e] = mn;
+          float sum = 0.f;
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) sum += s[n][half][2 * j + e] = fast_ex2(s[n][half][2 * j + e] - base);
+          l[n][e] = l[n][e] * f[e] + sum;
+        }
+        if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
+#pragma unroll
+          for (int G = 0; G < NG; ++G) {
+            mids[n][G][0] *= f[0];
+            mids[n][G][1] *= f[1];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              ones[n][G][c] *= f[c & 1];
+              o[n][G][0][c] *= f[c & 1];
+              o[n][G][1][c] *= f[c & 1];
+            }
+          }
+        }
       }
-      *reinterpret_cast<float4*>(s_o + (grp * G + i) * D + first) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t vw[4][VW], vp[2][NG];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // rows of slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+          const int row = 16 * half + 8 * (e >> 1) + slot_row(2 * t + (e & 1));
+#pragma unroll
+          for (int x = 0; x < VW; ++x) vw[e][x] = reinterpret_cast<const uint32_t*>(st + QT::V_CODE)[row * (D / 8) + gid * VW + x];
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int G = 0; G < NG; ++G)
+            vp[e][G] = reinterpret_cast<const uint32_t*>(st + QT::V_PAR)[(16 * half + 8 * e + slot_row(gid)) * NG + G];
+#pragma unroll
+        for (int G = 0; G < NG; ++G) {
+          uint32_t a[2][4];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            operands<kExact>(__byte_perm(vw[2 * e][G / 2], vw[2 * e + 1][G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
+          const uint32_t a0[4] = {a[0][0], a[0][1], a[1][0], a[1][1]}, a1[4] = {a[0][2], a[0][3], a[1][2], a[1][3]};
+          const uint32_t one[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+          const float step[2] = {bf16_lo(vp[0][G]), bf16_lo(vp[1][G])}, mid[2] = {bf16_hi(vp[0][G]), bf16_hi(vp[1][G])};
+#pragma unroll
+          for (int n = 0; n < NH; ++n) {
+            float w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              w[j] = s[n][half][j] * step[j >> 1];
+              mids[n][G][j & 1] = fmaf(s[n][half][j], mid[j >> 1], mids[n][G][j & 1]);
+            }
+#pragma unroll
+            for (int term = 0; term < TERMS; ++term) {
+              const uint32_t b0 = transposed(next_term(w[0], w[1])), b1 = transposed(next_term(w[2], w[3]));
+              mma_bf16_16816(o[n][G][0], a0, b0, b1);
+              mma_bf16_16816(o[n][G][1], a1, b0, b1);
+              if (!kExact) mma_bf16_16816(ones[n][G], one, b0, b1);
+            }
+          }
+        }
+      }
+      __syncwarp();  // the stage is refilled from here on
+    }
+    cp_async_wait<0>();
+    __syncwarp();
+    // the warp's state into its own area: o [8 NH][OPITCH], m [8 NH], l [8 NH]
+    float* sm = so + 8 * NH * OPITCH;
+#pragma unroll
+    for (int n = 0; n < NH; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int head = 8 * n + 2 * t + e;
+#pragma unroll
+        for (int sh = 4; sh <= 16; sh *= 2) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], sh);
+        if (gid == 0) {
+          sm[head] = m[n][e];
+          sm[8 * NH + head] = l[n][e];
+        }
+#pragma unroll
+        for (int G = 0; G < NG; ++G) {
+          float add = mids[n][G][e];
+#pragma unroll
+          for (int sh = 4; sh <= 16; sh *= 2) add += __shfl_xor_sync(0xffffffffu, add, sh);
+          if (!kExact) add = fmaf(-23.5f, ones[n][G][e], add);
+          *reinterpret_cast<float4*>(so + head * OPITCH + 32 * G + 4 * gid) = make_float4(
+              o[n][G][0][e] + add, o[n][G][0][e + 2] + add, o[n][G][1][e] + add, o[n][G][1][e + 2] + add);
+        }
+      }
+    __syncthreads();
+    // (every thread sums what it reads before anything is written: the block's result lies in the second warp's area)
+    constexpr int PER = (8 * NH * D + NT - 1) / NT;
+    float O[PER], M[PER], L[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int x = threadIdx.x + j * NT, i = x / D, c = x % D;
+      if (i >= p.g) break;
+      float mw[kWarps];
+      M[j] = -INFINITY;
+      O[j] = L[j] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        mw[w] = reinterpret_cast<const float*>(dsmem + w * QT::WARP)[8 * NH * OPITCH + i];
+        M[j] = fmaxf(M[j], mw[w]);
+      }
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float* wo = reinterpret_cast<const float*>(dsmem + w * QT::WARP);
+        const float fw = part_weight(mw[w], M[j]);
+        L[j] += wo[8 * NH * OPITCH + 8 * NH + i] * fw;
+        O[j] += wo[i * OPITCH + c] * fw;
+      }
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < p.g * D; x += NT) {
-      const int i = x / D, c = x % D;
-      float M = -INFINITY, Lsum = 0.f, O = 0.f;
 #pragma unroll
-      for (int gq = 0; gq < GROUPS; ++gq) M = fmaxf(M, s_m[gq * G + i]);
-#pragma unroll
-      for (int gq = 0; gq < GROUPS; ++gq) {
-        const float f = part_weight(s_m[gq * G + i], M);
-        Lsum += s_l[gq * G + i] * f;
-        O += s_o[(gq * G + i) * D + c] * f;
-      }
-      b_o[i * D + c] = O;
+    for (int j = 0; j < PER; ++j) {
+      const int x = threadIdx.x + j * NT, i = x / D, c = x % D;
+      if (i >= p.g) break;
+      bo[x] = O[j];
       if (c == 0) {
-        b_m[i] = M;
-        b_l[i] = Lsum;
+        bo[8 * NH * D + i] = M[j];
+        bo[8 * NH * D + 8 * NH + i] = L[j];
       }
     }
     __syncthreads();
   }
-  finish_segment<T, D, NT, true>(p, b_o, b_m, b_l, fac, u, y, slot, nb, view);
+  finish_segment<T, D, NT, true>(p, bo, bo + 8 * NH * D, bo + 8 * NH * D + 8 * NH, reinterpret_cast<float*>(dsmem), u, y, slot, nb, view);
 }
 
 template <typename T, int D>
@@ -145,25 +422,25 @@ int run(DecodeParams p, const madakv_config& c, int splits, cudaStream_t st) {
   if (p.g > (sizeof(T) == 2 ? 16 : 8)) return MADAKV_EUNSUPPORTED;
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, longest = c.max_seq_len + (int64_t)c.max_new_tokens;
   const int64_t rows = p.capacity / units < longest ? p.capacity / units : longest;
-  const int64_t want = 3 * rows / 512 + 1, most = 888 / p.n_sel < 1 ? 1 : 888 / p.n_sel < kDecodeSlots ? 888 / p.n_sel : kDecodeSlots;
+  const int resident = 148 * (p.g <= 8 ? 3 : 2);
+  const int64_t want = 3 * rows / 256 + 1, most = resident / p.n_sel < 1 ? 1 : resident / p.n_sel < kDecodeSlots ? resident / p.n_sel : kDecodeSlots;
   p.slots = (int)(want < most ? want : most);
   if (p.slots > splits) p.slots = splits;
   if (p.n_sel > kCounters) p.slots = 1;
-  p.min_rows = 256;
+  p.min_rows = 128;
   p.part_ml = reinterpret_cast<float2*>(p.part + (int64_t)c.batch * c.n_layers * c.n_q_heads * p.slots * D);
-  auto go = [&](auto heads) {
-    constexpr int G = decltype(heads)::value;
-    const dim3 grid((unsigned)p.n_sel * p.slots);
-    if (p.scores)
-      launch_pdl(decode_quant_kernel<T, D, G, true>, grid, dim3(NT), 0, st, p);
-    else
-      launch_pdl(decode_quant_kernel<T, D, G, false>, grid, dim3(NT), 0, st, p);
+  auto go = [&](auto groups, auto track) {
+    auto kernel = decode_quant_kernel<T, D, decltype(groups)::value, decltype(track)::value>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, QuantTile<D>::BYTES) != cudaSuccess) return (int)MADAKV_ECUDA;
+    launch_pdl(kernel, dim3((unsigned)p.n_sel * p.slots), dim3(NT), QuantTile<D>::BYTES, st, p);
     return launch_status();
   };
-  if (p.g <= 2) return go(std::integral_constant<int, 2>());
-  if (p.g <= 4) return go(std::integral_constant<int, 4>());
-  if (p.g <= 8) return go(std::integral_constant<int, 8>());
-  if constexpr (sizeof(T) == 2) return go(std::integral_constant<int, 16>());
+  constexpr std::integral_constant<int, 1> one;
+  if (p.g <= 8) return p.scores ? go(one, std::true_type()) : go(one, std::false_type());
+  if constexpr (sizeof(T) == 2) {
+    constexpr std::integral_constant<int, 2> two;
+    return p.scores ? go(two, std::true_type()) : go(two, std::false_type());
+  }
   return MADAKV_EUNSUPPORTED;
 }
 
