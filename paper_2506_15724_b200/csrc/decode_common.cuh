@@ -213,7 +213,7 @@ __device__ __forceinline__ void finish_segment(const DecodeParams& p, const floa
   if (threadIdx.x == 0) finish_append(p, u, view);
   // weights of the partials, and every head's maximum and sum; the first partials are on their way meanwhile
   __shared__ float s_l[16];
-  constexpr int kFirst = 8, kHeads = 16 * 32 / NTHR;  // heads per warp at most
+  constexpr int kFirst = 8, kHeads = (16 * 32 + NTHR - 1) / NTHR;  // heads per warp at most
   float2 ml[kHeads];
 #pragma unroll
   for (int j = 0; j < kHeads; ++j) {

@@ -1,15 +1,16 @@
 // Stage 5 on a cache in 4 bits: cache append (Eq. 4, the row quantised on the way) and decode attention (Eq. 5).
 //
 // Bound by HBM at 160 bytes a row (d = 128) only if little is done per code: an SM gets a row of K and V, 256 codes, in seven clocks.
-// So the codes go into the tensor cores as they are and the groups' (step, mid) are applied to sums:
-//   logits   q . k = sum over groups of step sum q (code - 7.5) + mid sum q, the inner sums by m16n8k16 products of 16 rows with 8 heads;
-//            a row's step and mid meet four numbers per thread and group
+// So the codes go into the tensor cores as they are and the groups' (step, mid) are applied to sums.
+//   logits   q . k = sum over groups of step sum q code + (mid - 7.5 step) sum q, the sums over codes by m16n8k16 products of 16 rows
+//            with 8 heads; a row's step meets four numbers per thread and group. The second part is one more product, of the rows'
+//            (step, mid) words as they lie in the cache with multiples of the queries' sums in three bf16 terms.
 //   values   sum of w v = sum of (w step) (code - 7.5) + w mid: the weights take the step of every group before they are rounded to
 //            bf16 for the product with the codes; mid is summed up in fp32
 // A code becomes an operand by a shift and one logical operation: its four bits are bits 3-6 of a bf16 mantissa under the exponent of
-// 16, which makes 16 + code. 23.5 times the sum of the other operand is taken off again: of the queries by where the product's
-// accumulator starts, of the weights by one more product, with ones, per group. The order of codes in a row is that of the operands: a
-// lane's words are one piece of 16 bytes (K) or 8 (V), pairs along d for K, and of two rows for V.
+// 16, which makes 16 + code. 23.5 times the sum of the other operand is taken off again: of the queries together with the mids, of
+// the weights by one more product, with ones, per group. The order of codes in a row is that of the operands: a lane's words are
+// one piece of 16 bytes (K) or 8 (V) a row, pairs along d for K, and of two rows for V.
 // fp32 (queries and weights): three bf16 terms each, whose products are exact and whose sum is fp32 again; the operands are
 // code - 7.5 then, so that no sum loses bits to the 23.5.
 // A warp has tiles of 32 rows of its own, read ahead into a ring in shared memory by asynchronous copies.
@@ -21,18 +22,19 @@
 namespace madakv {
 namespace {
 
-constexpr int kWarps = 4, NT = 32 * kWarps;
 constexpr int kTile = 32;    // rows of a warp at a time
 constexpr int kAhead = 3;    // stages of a warp's ring
 
-template <int D>
+template <int D, int kWarps>
 struct QuantTile {
   using R = QuantRow<D>;
   static constexpr int K_CODE = 0, K_PAR = kTile * R::CODE_BYTES, V_CODE = K_PAR + kTile * R::PAR_BYTES,
                        V_PAR = V_CODE + kTile * R::CODE_BYTES, STAGE = V_PAR + kTile * R::PAR_BYTES;
   static constexpr int WARP = kAhead * STAGE;
   static constexpr int FRESH = kWarps * WARP;  // the appended row: codes and parameters of K, then of V
-  static constexpr int BYTES = FRESH + 2 * (R::CODE_BYTES + R::PAR_BYTES);
+  static constexpr int QUERIES = FRESH + 2 * (R::CODE_BYTES + R::PAR_BYTES);  // operands of up to 16 heads in bf16 or 8 in fp32
+  static_assert(QUERIES % 16 == 0, "read in 16-byte pieces");
+  static constexpr int query_bytes(int sets) { return sets * R::NG * 512; }
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
@@ -70,6 +72,30 @@ __device__ __forceinline__ void operands(uint32_t x, uint32_t (&r)[4]) {
     }
   }
 }
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+// (a0, a1) += k (b0, b1), and (a0, a1) = k (b0, b1), as one instruction each.
+__device__ __forceinline__ void fma_pair(float& a0, float& a1, float k, float b0, float b1) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_of(k, k)), "l"(pair_of(b0, b1)), "l"(pair_of(a0, a1)));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(r));
+}
+__device__ __forceinline__ void mul_pair(float& a0, float& a1, float k, float b0, float b1) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_of(k, k)), "l"(pair_of(b0, b1)));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(r));
+}
+// A product whose sums start from zero.
+__device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 // The n-th bf16 term of x and y (0: the nearest; what is left goes on to the next).
 __device__ __forceinline__ uint32_t next_term(float& x, float& y) {
   const uint32_t w = pack_bf16x2(x, y);
@@ -79,10 +105,11 @@ __device__ __forceinline__ uint32_t next_term(float& x, float& y) {
 }
 
 // NH: groups of eight query heads.
-template <typename T, int D, int NH, bool kTrack>
-__global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const __grid_constant__ DecodeParams p) {
+template <typename T, int D, int NH, int kWarps, bool kTrack>
+__global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2) decode_quant_kernel(const __grid_constant__ DecodeParams p) {
   using R = QuantRow<D>;
-  using QT = QuantTile<D>;
+  using QT = QuantTile<D, kWarps>;
+  constexpr int NT = 32 * kWarps;
   constexpr int NG = R::NG;
   constexpr bool kExact = sizeof(T) == 4;
   constexpr int TERMS = kExact ? 3 : 1;
@@ -109,8 +136,25 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
                           (const char*)p.v_c + off * R::CODE_BYTES, (const char*)p.v_par + off * R::PAR_BYTES};
     unsigned char* ring = dsmem + warp * QT::WARP;
     const uint32_t ring_a = smem_addr(ring);
+    const bool owner = view.new_row >= row_begin && view.new_row < row_end;
     auto load_tile = [&](int r, int stage) {
       const uint32_t dst = ring_a + stage * QT::STAGE;
+      if (r + kTile <= row_end && !(owner && r + kTile > view.new_row)) {  // whole: each array is one stretch of bytes
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int bytes = a % 2 ? R::PAR_BYTES : R::CODE_BYTES, piece = bytes < 16 ? 8 : 16;
+          const uint32_t to = dst + (a == 0 ? QT::K_CODE : a == 1 ? QT::K_PAR : a == 2 ? QT::V_CODE : QT::V_PAR) + lane * piece;
+          const char* from = src[a] + (int64_t)r * bytes + lane * piece;
+#pragma unroll
+          for (int x = 0; x < kTile * bytes / (32 * piece); ++x) {
+            if (piece == 16)
+              cp_async16(to + x * 32 * piece, from + x * 32 * piece, true);
+            else
+              cp_async8(to + x * 32 * piece, from + x * 32 * piece, true);
+          }
+        }
+        return;
+      }
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         const int bytes = a % 2 ? R::PAR_BYTES : R::CODE_BYTES;
@@ -136,7 +180,7 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
       cp_async_commit();
     }
     // the appended row: quantised into the cache and, for the tile that holds it, into shared memory
-    if (view.new_row >= row_begin && view.new_row < row_end) {
+    if (owner) {
       if (warp < 2) {
         const int l = lane % R::LANES, G = l % NG;
         float x[4];
@@ -158,10 +202,12 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
     }
 
     // queries as B operands: products j = 0, 1 of group G pair element 8 t + 2 j + {0, 1} with 8 t + 4 + 2 j + {0, 1}; and their sums
-    uint32_t qb[NH][TERMS][NG][2][2];
-    float qsum[NH][NG][2];
+    // (the same for all warps: they lie in shared memory, 16 bytes of every lane together)
+    uint4* qb = reinterpret_cast<uint4*>(dsmem + QT::QUERIES) + lane;
+    uint32_t qm[NH][3];  // the sums as operands against (step, mid) pairs, in three terms: lane t has group t's
 #pragma unroll
-    for (int n = 0; n < NH; ++n)
+    for (int n = 0; n < NH; ++n) {
+      float own_sum = 0.f;
 #pragma unroll
       for (int G = 0; G < NG; ++G) {
         float x[8], sum = 0.f;
@@ -176,17 +222,24 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
         for (int e = 0; e < 8; ++e) sum += x[e];
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        qsum[n][G][0] = __shfl_sync(0xffffffffu, sum, 8 * t);  // heads 2 t, 2 t + 1
-        qsum[n][G][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+        if (t == G) own_sum = sum;
 #pragma unroll
-        for (int term = 0; term < TERMS; ++term)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            qb[n][term][G][j][0] = next_term(x[2 * j], x[2 * j + 4]);
-            qb[n][term][G][j][1] = next_term(x[2 * j + 1], x[2 * j + 5]);
-          }
+        for (int term = 0; term < TERMS; ++term) {
+          uint4 w;
+          w.x = next_term(x[0], x[4]);
+          w.y = next_term(x[1], x[5]);
+          w.z = next_term(x[2], x[6]);
+          w.w = next_term(x[3], x[7]);
+          if (warp == 0) qb[((n * TERMS + term) * NG + G) * 32] = w;
+        }
       }
+#pragma unroll
+      float off_sum = kExact ? 0.f : -23.5f * own_sum;
+#pragma unroll
+      for (int term = 0; term < 3; ++term) qm[n][term] = next_term(off_sum, own_sum);
+    }
 
+    __syncthreads();
     float m[NH][2], l[NH][2];
     float o[NH][NG][2][4], ones[NH][NG][4], mids[NH][NG][2];
 #pragma unroll
@@ -228,7 +281,7 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
       float s[NH][2][4];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        uint32_t kw[2][KW], kp[2][NG];
+        uint32_t kw[2][KW], kp[2][NG], own_par[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int row = 16 * half + 8 * e + slot_row(gid);
@@ -236,9 +289,14 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
           for (int x = 0; x < KW; ++x) kw[e][x] = reinterpret_cast<const uint32_t*>(st + QT::K_CODE)[row * (D / 8) + t * KW + x];
 #pragma unroll
           for (int G = 0; G < NG; ++G) kp[e][G] = reinterpret_cast<const uint32_t*>(st + QT::K_PAR)[row * NG + G];
+          own_par[e] = reinterpret_cast<const uint32_t*>(st + QT::K_PAR)[row * NG + t % NG];
         }
+        const uint32_t ap[4] = {own_par[0], own_par[1], own_par[0], own_par[1]};
 #pragma unroll
-        for (int n = 0; n < NH; ++n) s[n][half][0] = s[n][half][1] = s[n][half][2] = s[n][half][3] = 0.f;
+        for (int n = 0; n < NH; ++n) {  // sum over groups of (mid - 23.5 step) sum q
+          mma_first(s[n][half], ap, qm[n][2], 0u);
+          mma_bf16_16816(s[n][half], ap, qm[n][0], qm[n][1]);
+        }
 #pragma unroll
         for (int G = 0; G < NG; ++G) {
           uint32_t a[2][4];
@@ -246,35 +304,47 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
           for (int e = 0; e < 2; ++e)  // elements 8 t .. + 3 of the group in the low half, + 4 .. + 7 in the high
             operands<kExact>(__byte_perm(kw[e][G / 2], kw[e][KW / 2 + G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
           const uint32_t a0[4] = {a[0][0], a[1][0], a[0][1], a[1][1]}, a1[4] = {a[0][2], a[1][2], a[0][3], a[1][3]};
-          const float step[2] = {bf16_lo(kp[0][G]), bf16_lo(kp[1][G])}, mid[2] = {bf16_hi(kp[0][G]), bf16_hi(kp[1][G])};
 #pragma unroll
           for (int n = 0; n < NH; ++n) {
             float c[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) c[j] = kExact ? 0.f : -23.5f * qsum[n][G][j & 1];
-#pragma unroll
             for (int term = TERMS - 1; term >= 0; --term) {
-              mma_bf16_16816(c, a0, qb[n][term][G][0][0], qb[n][term][G][0][1]);
-              mma_bf16_16816(c, a1, qb[n][term][G][1][0], qb[n][term][G][1][1]);
+              const uint4 q = qb[((n * TERMS + term) * NG + G) * 32];
+              if (term == TERMS - 1)
+                mma_first(c, a0, q.x, q.y);
+              else
+                mma_bf16_16816(c, a0, q.x, q.y);
+              mma_bf16_16816(c, a1, q.z, q.w);
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              s[n][half][j] = fmaf(step[j >> 1], c[j], fmaf(mid[j >> 1], qsum[n][G][j & 1], s[n][half][j]));
+            fma_pair(s[n][half][0], s[n][half][1], bf16_lo(kp[0][G]), c[0], c[1]);
+            fma_pair(s[n][half][2], s[n][half][3], bf16_lo(kp[1][G]), c[2], c[3]);
           }
         }
       }
-      const bool whole = r + kTile <= row_end;
-#pragma unroll
-      for (int n = 0; n < NH; ++n)
+      if constexpr (kTrack) {
+        float* dst = p.scores + (off + r + slot_row(gid)) * p.g + 2 * t;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int row = r + 16 * half + 8 * (j >> 1) + slot_row(gid), head = 8 * n + 2 * t + (j & 1);
-            s[n][half][j] *= p.scale2;
-            if (kTrack && row < row_end && head < p.g) p.scores[(off + row) * p.g + head] = s[n][half][j];
-            if (!whole && row >= row_end) s[n][half][j] = -INFINITY;
-          }
+          for (int e = 0; e < 2; ++e, dst += 8 * p.g)
+            if (r + 16 * half + 8 * e + slot_row(gid) < row_end) {
+#pragma unroll
+              for (int n = 0; n < NH; ++n) {
+                if (8 * n + 2 * t < p.g) dst[8 * n] = s[n][half][2 * e] * p.scale2;
+                if (8 * n + 2 * t + 1 < p.g) dst[8 * n + 1] = s[n][half][2 * e + 1] * p.scale2;
+              }
+            }
+      }
+      if (r + kTile > row_end) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (r + 16 * half + 8 * e + slot_row(gid) >= row_end) {
+#pragma unroll
+              for (int n = 0; n < NH; ++n) s[n][half][2 * e] = s[n][half][2 * e + 1] = -INFINITY;
+            }
+      }
       // one softmax step; the weights become w, the sums of the steps before get their factor
 #pragma unroll
       for (int n = 0; n < NH; ++n) {
@@ -285,14 +355,14 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          const float mn = fmaxf(m[n][e], mx), base = mn == -INFINITY ? 0.f : mn;
-          f[e] = fast_ex2(m[n][e] - base);
+          const float mn = fmaxf(m[n][e], mx), base = mn == -INFINITY ? 0.f : mn * p.scale2;
+          f[e] = fast_ex2(fmaf(m[n][e], p.scale2, -base));
           m[n][e] = mn;
           float sum = 0.f;
 #pragma unroll
           for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) sum += s[n][half][2 * j + e] = fast_ex2(s[n][half][2 * j + e] - base);
+            for (int j = 0; j < 2; ++j) sum += s[n][half][2 * j + e] = fast_ex2(fmaf(s[n][half][2 * j + e], p.scale2, -base));
           l[n][e] = l[n][e] * f[e] + sum;
         }
         if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
@@ -335,11 +405,10 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
 #pragma unroll
           for (int n = 0; n < NH; ++n) {
             float w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              w[j] = s[n][half][j] * step[j >> 1];
-              mids[n][G][j & 1] = fmaf(s[n][half][j], mid[j >> 1], mids[n][G][j & 1]);
-            }
+            mul_pair(w[0], w[1], step[0], s[n][half][0], s[n][half][1]);
+            mul_pair(w[2], w[3], step[1], s[n][half][2], s[n][half][3]);
+            fma_pair(mids[n][G][0], mids[n][G][1], mid[0], s[n][half][0], s[n][half][1]);
+            fma_pair(mids[n][G][0], mids[n][G][1], mid[1], s[n][half][2], s[n][half][3]);
 #pragma unroll
             for (int term = 0; term < TERMS; ++term) {
               const uint32_t b0 = transposed(next_term(w[0], w[1])), b1 = transposed(next_term(w[2], w[3]));
@@ -364,7 +433,7 @@ __global__ void __launch_bounds__(NT, NH == 1 ? 3 : 2) decode_quant_kernel(const
 #pragma unroll
         for (int sh = 4; sh <= 16; sh *= 2) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], sh);
         if (gid == 0) {
-          sm[head] = m[n][e];
+          sm[head] = m[n][e] * p.scale2;
           sm[8 * NH + head] = l[n][e];
         }
 #pragma unroll
@@ -423,24 +492,32 @@ int run(DecodeParams p, const madakv_config& c, int splits, cudaStream_t st) {
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, longest = c.max_seq_len + (int64_t)c.max_new_tokens;
   const int64_t rows = p.capacity / units < longest ? p.capacity / units : longest;
   const int resident = 148 * (p.g <= 8 ? 3 : 2);
-  const int64_t want = 3 * rows / 256 + 1, most = resident / p.n_sel < 1 ? 1 : resident / p.n_sel < kDecodeSlots ? resident / p.n_sel : kDecodeSlots;
+  // few long segments: one block of as many warps as fit an SM, so that all SMs get the same share (8 segments of 131071 rows: 51 us,
+  // 32 blocks of four warps for each of them 75)
+  const bool big = p.n_sel <= 20 && p.n_sel * rows >= 148 * 768;
+  const int blocks = big ? 148 : resident;
+  const int64_t want = 3 * rows / 256 + 1, most = blocks / p.n_sel < 1 ? 1 : blocks / p.n_sel < kDecodeSlots ? blocks / p.n_sel : kDecodeSlots;
   p.slots = (int)(want < most ? want : most);
   if (p.slots > splits) p.slots = splits;
   if (p.n_sel > kCounters) p.slots = 1;
   p.min_rows = 128;
   p.part_ml = reinterpret_cast<float2*>(p.part + (int64_t)c.batch * c.n_layers * c.n_q_heads * p.slots * D);
-  auto go = [&](auto groups, auto track) {
-    auto kernel = decode_quant_kernel<T, D, decltype(groups)::value, decltype(track)::value>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, QuantTile<D>::BYTES) != cudaSuccess) return (int)MADAKV_ECUDA;
-    launch_pdl(kernel, dim3((unsigned)p.n_sel * p.slots), dim3(NT), QuantTile<D>::BYTES, st, p);
+  auto go = [&](auto groups, auto warps, auto track) {
+    constexpr int W = decltype(warps)::value;
+    auto kernel = decode_quant_kernel<T, D, decltype(groups)::value, W, decltype(track)::value>;
+    constexpr int bytes = QuantTile<D, W>::QUERIES + QuantTile<D, W>::query_bytes(sizeof(T) == 4 ? 3 : decltype(groups)::value);
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return (int)MADAKV_ECUDA;
+    launch_pdl(kernel, dim3((unsigned)p.n_sel * p.slots), dim3(32 * W), bytes, st, p);
     return launch_status();
   };
+  auto sized = [&](auto groups, auto warps) { return p.scores ? go(groups, warps, std::true_type()) : go(groups, warps, std::false_type()); };
   constexpr std::integral_constant<int, 1> one;
-  if (p.g <= 8) return p.scores ? go(one, std::true_type()) : go(one, std::false_type());
-  if constexpr (sizeof(T) == 2) {
-    constexpr std::integral_constant<int, 2> two;
-    return p.scores ? go(two, std::true_type()) : go(two, std::false_type());
-  }
+  constexpr std::integral_constant<int, 2> two;
+  constexpr std::integral_constant<int, 4> four;
+  constexpr std::integral_constant<int, 8> eight;
+  constexpr std::integral_constant<int, 12> twelve;
+  if (p.g <= 8) return big ? sized(one, twelve) : sized(one, four);
+  if constexpr (sizeof(T) == 2) return big ? sized(two, eight) : sized(two, four);
   return MADAKV_EUNSUPPORTED;
 }
 
