@@ -1,7 +1,14 @@
 // Stage 4b with a cache in 4 bits: gather the kept K/V rows and quantise them on the way; and the way back for single rows.
 //
-// A row is shared by D / 4 lanes of a warp, four elements each, in the order of the row's 16-bit words: a warp reads whole rows of
-// the source and writes whole rows of codes.
+// A row is shared by lanes of 16 bytes: with 8 (bf16) or 4 (fp32) elements each, 4 or 8 lanes hold a group. HBM takes 29 clocks of an
+// SM for a row of K and V (d = 128, bf16: 672 bytes), so that a partition has 116 issue slots for 8 elements of every lane. What keeps
+// to that:
+//   - a thread has two rows of K and of V at a time. Their groups' extremes meet in log2(lanes) exchanges; then each lane of a group
+//     works out (step, mid) for one of the four, and they are handed round: the division is made once per group, not per lane
+//   - a code is one fused multiply-add: (x - mid) / step + 8 in units of 2^-16, rounded to a whole number by the constant it is added
+//     to. It is off by less than 0.6 units, so the bits above the 16th are the code unless the lower 16 are all zero: then x is on or
+//     next to a border, and the exact products of step decide. Groups with elements outside the sixteen cells (a mid that is large
+//     beside step and was rounded), with extreme steps or without one go the exact way altogether.
 #include <type_traits>
 
 #include "quant.cuh"
@@ -26,10 +33,111 @@ struct CompactQuantParams {
   int L, Hkv, n_max, headroom, blocks;             // blocks per unit
 };
 
+template <typename T>
+struct Lane16;
+template <>
+struct Lane16<float> {
+  static constexpr int N = 4;
+  __device__ static void values(const uint4& v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  __device__ static void extremes(const uint4& v, float& lo, float& hi) {
+    float x[4];
+    values(v, x);
+    lo = min_nan(min_nan(x[0], x[1]), min_nan(x[2], x[3]));
+    hi = max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3]));
+#pragma unroll
+    for (int off = 1; off < 8; off *= 2) {
+      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, off));
+      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, off));
+    }
+  }
+  __device__ static uint32_t par(float lo, float hi) { return group_par(lo, hi); }
+};
+template <>
+struct Lane16<__nv_bfloat16> {
+  static constexpr int N = 8;
+  __device__ static void values(const uint4& v, float (&x)[8]) {
+    x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
+    x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
+  }
+  __device__ static __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
+  __device__ static void extremes(const uint4& v, float& lo, float& hi) {
+    __nv_bfloat162 a = __hmin2_nan(__hmin2_nan(two(v.x), two(v.y)), __hmin2_nan(two(v.z), two(v.w)));
+    const __nv_bfloat162 b = __hmax2_nan(__hmax2_nan(two(v.x), two(v.y)), __hmax2_nan(two(v.z), two(v.w)));
+    // (least, -largest) in one word: both get smaller
+    a = __halves2bfloat162(__hmin_nan(__low2bfloat16(a), __high2bfloat16(a)), __hneg(__hmax_nan(__low2bfloat16(b), __high2bfloat16(b))));
+#pragma unroll
+    for (int off = 1; off < 4; off *= 2) a = __hmin2_nan(a, __shfl_xor_sync(0xffffffffu, a, off));
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&a);
+    lo = bf16_lo(w);
+    hi = -bf16_hi(w);
+  }
+  // group_par() in fp32. The sum and the difference of two bf16 numbers are exact or so far from a tie of the roundings that follow that
+  // they might be; halves where they would overflow.
+  __device__ static uint32_t par(float lo, float hi) {
+    const bool huge = hi > 1e38f || lo < -1e38f;
+    const float h = huge ? 0.5f : 1.f, sum = __fadd_rn(h * lo, h * hi), diff = __fsub_rn(h * hi, h * lo);
+    const float mid = huge ? sum : 0.5f * sum, step = __fdiv_rn(diff, huge ? 7.5f : 15.f);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(step, mid);
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&r);
+    return isfinite(bf16_lo(w)) && isfinite(bf16_hi(w)) ? w : 0x7fc07fc0u;
+  }
+};
+
+constexpr float kUnit = 65536.f;             // 2^16 units to a code
+constexpr float kWhole = 12582912.f;         // 1.5 2^23: a float added to it is rounded to a whole number in its lower bits
+
+// 65536 / step where the fast way holds for the group, else NaN.
+__device__ __forceinline__ float units_per(uint32_t par, float lo, float hi) {
+  const float step = bf16_lo(par), mid = bf16_hi(par);
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
+  const float a = fmaf(lo - mid, inv, 8.f), b = fmaf(hi - mid, inv, 8.f);
+  return step > 1e-30f && step < 1e30f && a > 0.001f && b < 15.999f ? kUnit * inv : NAN;
+}
+
+// The codes of a lane's N elements, four in each half of the word.
+template <int N>
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[N], uint32_t par, float units) {
+  const float step = bf16_lo(par), mid = bf16_hi(par);
+  uint32_t t[N];
+  uint32_t least = 0xffffffffu;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    t[e] = __float_as_uint(fmaf(x[e] - mid, units, 8.f * kUnit + kWhole));
+    least = min(least, t[e] & 0xffffu);
+  }
+  if (!(units == units)) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) t[e] = code_of(x[e], step, mid) << 16;
+  } else if (least == 0) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if ((t[e] & 0xffffu) == 0) {
+        // d + rest = x - mid exactly; the border is an exact product
+        const float d = x[e] - mid, y = d - x[e], rest = (x[e] - (d - y)) + (-mid - y);
+        const float border = (__uint_as_float(t[e]) - (8.f * kUnit + kWhole)) * (1.f / kUnit) * step;
+        if (d < border || (d == border && rest < 0.f)) t[e] -= 0x10000u;
+      }
+  }
+  uint32_t half[2] = {0u, 0u};
+#pragma unroll
+  for (int e = 0; e < N; e += 4) {
+    const uint32_t a = __byte_perm(t[e], t[e + 1], 0x7632) & 0x000f000fu, b = __byte_perm(t[e + 2], t[e + 3], 0x7632) & 0x000f000fu;
+    const uint32_t c = a + b * 256u;  // codes 0 and 2 in the bytes of the low half, 1 and 3 in those of the high half
+    half[e / 4] = c | c >> 12;
+  }
+  return __byte_perm(half[0], half[1], 0x5410);
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(NT) compact_quant_kernel(const __grid_constant__ CompactQuantParams p) {
   using R = QuantRow<D>;
-  constexpr int RPB = NT / R::LANES;  // rows of the block at a time
+  using V = Lane16<T>;
+  constexpr int LPR = D / V::N;   // lanes per row
+  constexpr int GL = 32 / V::N;   // lanes per group: 4 or 8
+  constexpr int SPAN = NT / LPR;  // rows of the block's threads side by side
   pdl_wait();
   pdl_go();
   const int u = blockIdx.x / p.blocks, x = blockIdx.x % p.blocks;
@@ -38,28 +146,54 @@ __global__ void __launch_bounds__(NT) compact_quant_kernel(const __grid_constant
   // a segment that selection refused (MADAKV_ECAPACITY: it would end beyond the cache) has no index list: skip it
   if (off < 0 || off + len + p.headroom > p.capacity) return;
   const int h = u % p.Hkv, l = (u / p.Hkv) % p.L, b = u / (p.Hkv * p.L);
-  const int lane = threadIdx.x % R::LANES, sub = threadIdx.x / R::LANES;
-  const int G = lane % R::NG, i = lane / R::NG;
-  const int64_t src_base = b * p.stride_b + l * p.stride_l + h * p.stride_h + (32 * G + 4 * i) * (int)sizeof(T);
-  for (int row0 = x * RPB; row0 < len; row0 += p.blocks * RPB) {  // (all lanes of a warp stay: they exchange extremes)
-    const int r = row0 + sub;
-    int idx = r < len ? p.kept_idx[off + r] : -1;
-    if (idx >= p.n_max) idx = -1;
-    float kx[4] = {0.f, 0.f, 0.f, 0.f}, vx[4] = {0.f, 0.f, 0.f, 0.f};
-    if (idx >= 0) {
-      load4(reinterpret_cast<const T*>(p.k + src_base + (int64_t)idx * p.stride_t), kx);
-      load4(reinterpret_cast<const T*>(p.v + src_base + (int64_t)idx * p.stride_t), vx);
+  const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
+  const int G = lane / GL, in_group = lane % GL;
+  const int64_t src_base = b * p.stride_b + l * p.stride_l + h * p.stride_h + lane * 16;
+  for (int row0 = x * 2 * SPAN; row0 < len; row0 += p.blocks * 2 * SPAN) {  // (all lanes of a warp stay: they exchange extremes)
+    int idx[2];
+    uint4 raw[4];  // K and V of the first row, of the second
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int r = row0 + j * SPAN + sub;
+      idx[j] = r < len ? __ldg(p.kept_idx + off + r) : -1;
+      if (idx[j] >= p.n_max) idx[j] = -1;
     }
-    uint32_t kc, kp, vc, vp;
-    quantise4<D>(kx, kc, kp);
-    quantise4<D>(vx, vc, vp);
-    if (idx >= 0) {
-      const int64_t dst = off + r;
-      reinterpret_cast<uint16_t*>(p.k_code)[dst * (D / 4) + lane] = (uint16_t)kc;
-      reinterpret_cast<uint16_t*>(p.v_code)[dst * (D / 4) + lane] = (uint16_t)vc;
-      if (i == 0) {
-        p.k_par[dst * R::NG + G] = kp;
-        p.v_par[dst * R::NG + G] = vp;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      raw[2 * j] = raw[2 * j + 1] = make_uint4(0u, 0u, 0u, 0u);
+      if (idx[j] >= 0) {
+        const int64_t src = src_base + (int64_t)idx[j] * p.stride_t;
+        raw[2 * j] = __ldg(reinterpret_cast<const uint4*>(p.k + src));
+        raw[2 * j + 1] = __ldg(reinterpret_cast<const uint4*>(p.v + src));
+      }
+    }
+    float lo = 0.f, hi = 0.f;  // of the lane's own one of the four
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float a, c;
+      V::extremes(raw[j], a, c);
+      if (in_group % 4 == j) lo = a, hi = c;
+    }
+    const uint32_t own = V::par(lo, hi);
+    const float own_units = units_per(own, lo, hi);
+    if (in_group < 4) {
+      const int j = in_group / 2;
+      if (idx[j] >= 0) (in_group % 2 ? p.v_par : p.k_par)[(off + row0 + j * SPAN + sub) * R::NG + G] = own;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float e[V::N];
+      V::values(raw[j], e);
+      const uint32_t codes = codes_of(e, __shfl_sync(0xffffffffu, own, j, 4), __shfl_sync(0xffffffffu, own_units, j, 4));
+      // two half-words of neighbouring groups make a word: the lanes GL apart exchange what the other one stores
+      const bool odd = G % 2;
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, V::N == 4 ? codes : odd ? codes : codes >> 16, GL);
+      uint32_t* dst = reinterpret_cast<uint32_t*>(j % 2 ? p.v_code : p.k_code) + (off + row0 + j / 2 * SPAN + sub) * (D / 8);
+      if (idx[j / 2] < 0) continue;
+      if constexpr (V::N == 8) {  // elements 8 in_group .. + 3 are half-word 2 in_group, + 4 .. + 7 the next
+        dst[(2 * in_group + odd) * (R::NG / 2) + G / 2] = odd ? __byte_perm(got, codes, 0x7610) : __byte_perm(codes, got, 0x5410);
+      } else if (!odd) {
+        dst[in_group * (R::NG / 2) + G / 2] = __byte_perm(codes, got, 0x5410);
       }
     }
   }
@@ -76,28 +210,50 @@ struct ExpandParams {
   int64_t n_rows, capacity;
 };
 
-__device__ __forceinline__ void store4(float* p, const float (&x)[4]) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4]) {
-  const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
-  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+__device__ __forceinline__ void store16(float* p, const float (&x)[4]) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&a);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// fp32 values of four codes in a half-word: a code's bits under an exponent that makes them the integer part, then one subtraction and
+// one fused multiply-add, the only rounding.
+__device__ __forceinline__ void values4(uint32_t codes, float step, float mid, float* x) {
+  const uint32_t y = codes << 4;
+  x[0] = fmaf(__uint_as_float((y & 0xf0u) | 0x49000000u) - 524295.5f, step, mid);      // 2^19 + code, in units of 2^-4
+  x[1] = fmaf(__uint_as_float((y & 0xf00u) | 0x47000000u) - 32775.5f, step, mid);      // 2^15
+  x[2] = fmaf(__uint_as_float((y & 0xf000u) | 0x45000000u) - 2055.5f, step, mid);      // 2^11
+  x[3] = fmaf(__uint_as_float((y & 0xf0000u) | 0x43000000u) - 135.5f, step, mid);      // 2^7
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(NT) expand_quant_kernel(const __grid_constant__ ExpandParams p) {
   using R = QuantRow<D>;
-  constexpr int RPB = NT / R::LANES;
+  constexpr int N = Lane16<T>::N, LPR = D / N, GL = 32 / N, SPAN = NT / LPR;
   pdl_wait();
   pdl_go();
-  const int lane = threadIdx.x % R::LANES, G = lane % R::NG, i = lane / R::NG;
-  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / R::LANES; r < p.n_rows; r += (int64_t)gridDim.x * RPB) {
+  const int lane = threadIdx.x % LPR, G = lane / GL, in_group = lane % GL;
+  for (int64_t r = (int64_t)blockIdx.x * SPAN + threadIdx.x / LPR; r < p.n_rows; r += (int64_t)gridDim.x * SPAN) {
     const int64_t row = p.rows ? p.rows[r] : r;
-    float kx[4] = {0.f, 0.f, 0.f, 0.f}, vx[4] = {0.f, 0.f, 0.f, 0.f};
-    if (row >= 0 && row < p.capacity) {
-      values4(reinterpret_cast<const uint16_t*>(p.k_code)[row * (D / 4) + lane], p.k_par[row * R::NG + G], kx);
-      values4(reinterpret_cast<const uint16_t*>(p.v_code)[row * (D / 4) + lane], p.v_par[row * R::NG + G], vx);
+    const bool there = row >= 0 && row < p.capacity;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint16_t* code = reinterpret_cast<const uint16_t*>(j ? p.v_code : p.k_code) + row * (D / 4) + G;
+      float x[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = 0.f;
+      if (there) {
+        const uint32_t par = (j ? p.v_par : p.k_par)[row * R::NG + G];
+#pragma unroll
+        for (int e = 0; e < N; e += 4) values4(code[(N / 4 * in_group + e / 4) * R::NG], bf16_lo(par), bf16_hi(par), x + e);
+      }
+      store16(reinterpret_cast<T*>(j ? p.v_out : p.k_out) + r * D + lane * N, x);
     }
-    store4(reinterpret_cast<T*>(p.k_out) + r * D + 32 * G + 4 * i, kx);
-    store4(reinterpret_cast<T*>(p.v_out) + r * D + 32 * G + 4 * i, vx);
   }
 }
 
@@ -137,7 +293,7 @@ int launch_compact_quant(const madakv_config& c, const void* k, const void* v, m
   p.n_max = c.max_seq_len;
   p.headroom = c.max_new_tokens;
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, rows = capacity / units + 1;
-  const int64_t per_block = 32, want = (rows + per_block - 1) / per_block, most = ((1 << 20) + units - 1) / units;
+  const int64_t per_block = 64, want = (rows + per_block - 1) / per_block, most = ((1 << 20) + units - 1) / units;
   p.blocks = (int)(want < most ? want : most);
   if (units * p.blocks > 0x7fffffff) return MADAKV_EUNSUPPORTED;
   return for_type(c, [&](auto t, auto d) {
@@ -148,7 +304,7 @@ int launch_compact_quant(const madakv_config& c, const void* k, const void* v, m
 int launch_expand_quant(const madakv_config& c, const int64_t* rows, int64_t n_rows, const uint8_t* k_code, const void* k_par,
                         const uint8_t* v_code, const void* v_par, int64_t capacity, void* k_out, void* v_out, cudaStream_t st) {
   const ExpandParams p{rows, k_code, v_code, (const uint32_t*)k_par, (const uint32_t*)v_par, k_out, v_out, n_rows, capacity};
-  const int64_t rpb = NT / (c.head_dim / 4), want = (n_rows + rpb - 1) / rpb;
+  const int64_t rpb = NT / (c.head_dim * elem_bytes(c) / 16), want = (n_rows + rpb - 1) / rpb;
   const unsigned grid = (unsigned)(want < (1 << 20) ? want : (1 << 20));
   return for_type(c, [&](auto t, auto d) {
     launch_pdl(expand_quant_kernel<decltype(t), decltype(d)::value>, dim3(grid), dim3(NT), 0, st, p);

@@ -71,12 +71,5 @@ __device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&x)[4]) {
   x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
 }
 
-// fp32 values of a lane's four codes.
-__device__ __forceinline__ void values4(uint32_t codes, uint32_t par, float (&x)[4]) {
-  const float step = bf16_lo(par), mid = bf16_hi(par);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = fmaf((float)((codes >> (4 * e)) & 15u) - 7.5f, step, mid);
-}
-
 }  // namespace
 }  // namespace madakv
