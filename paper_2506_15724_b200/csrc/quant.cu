@@ -6,8 +6,10 @@
 //   - a thread has two rows of K and of V at a time. Their groups' extremes meet in log2(lanes) exchanges; then each lane of a group
 //     works out (step, mid) for one of the four, and they are handed round: the division is made once per group, not per lane
 //   - a code is one fused multiply-add: (x - mid) / step + 8 in units of 2^-16, rounded to a whole number by the constant it is added
-//     to. It is off by less than 0.6 units, so the bits above the 16th are the code unless the lower 16 are all zero: then x is on or
-//     next to a border, and the exact products of step decide. Groups with elements outside the sixteen cells (a mid that is large
+//     to. It is off by less than 0.6 units, so the bits above the 16th are the code unless the lower 16 are all zero: then x is on
+//     a border, and the bits are right, or just below one. bf16 numbers that are no smaller than step / 256 cannot be that near to a
+//     border without being on it (x, mid and step are multiples of step 2^-15), which spares most of them a closer look (every other
+//     warp has an element on a border); the others, and fp32, are decided by the exact products of step. Groups with elements outside the sixteen cells (a mid that is large
 //     beside step and was rounded), with extreme steps or without one go the exact way altogether.
 #include <type_traits>
 
@@ -33,6 +35,12 @@ struct CompactQuantParams {
   int L, Hkv, n_max, headroom, blocks;             // blocks per unit
 };
 
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 template <typename T>
 struct Lane16;
 template <>
@@ -53,6 +61,7 @@ struct Lane16<float> {
     }
   }
   __device__ static uint32_t par(float lo, float hi) { return group_par(lo, hi); }
+  __device__ static bool may_touch(const uint4&, uint32_t) { return true; }
 };
 template <>
 struct Lane16<__nv_bfloat16> {
@@ -83,6 +92,12 @@ struct Lane16<__nv_bfloat16> {
     const uint32_t w = *reinterpret_cast<const uint32_t*>(&r);
     return isfinite(bf16_lo(w)) && isfinite(bf16_hi(w)) ? w : 0x7fc07fc0u;
   }
+  // Whether an element (or mid, unless it is 0) is smaller than step / 256. (Magnitudes compare as their bits.)
+  __device__ static bool may_touch(const uint4& v, uint32_t par) {
+    const uint32_t m = min_u16x2(min_u16x2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), min_u16x2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    const uint32_t below = (par & 0xffffu) - 0x400u, mid = (par >> 16) & 0x7fffu;
+    return min(m & 0xffffu, m >> 16) < below || (mid < below && mid != 0u);
+  }
 };
 
 constexpr float kUnit = 65536.f;             // 2^16 units to a code
@@ -97,21 +112,23 @@ __device__ __forceinline__ float units_per(uint32_t par, float lo, float hi) {
   return step > 1e-30f && step < 1e30f && a > 0.001f && b < 15.999f ? kUnit * inv : NAN;
 }
 
-// The codes of a lane's N elements, four in each half of the word.
-template <int N>
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[N], uint32_t par, float units) {
+// The codes of a lane's elements, four in each half of the word.
+template <typename T>
+__device__ __forceinline__ uint32_t codes_of(const uint4& raw, uint32_t par, float units) {
+  constexpr int N = Lane16<T>::N;
   const float step = bf16_lo(par), mid = bf16_hi(par);
+  float x[N];
+  Lane16<T>::values(raw, x);
   uint32_t t[N];
-  uint32_t least = 0xffffffffu;
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    t[e] = __float_as_uint(fmaf(x[e] - mid, units, 8.f * kUnit + kWhole));
-    least = min(least, t[e] & 0xffffu);
-  }
+  for (int e = 0; e < N; ++e) t[e] = __float_as_uint(fmaf(x[e] - mid, units, 8.f * kUnit + kWhole));
+  uint32_t least = __byte_perm(t[0], t[1], 0x5410);
+#pragma unroll
+  for (int e = 2; e < N; e += 2) least = min_u16x2(least, __byte_perm(t[e], t[e + 1], 0x5410));
   if (!(units == units)) {
 #pragma unroll
     for (int e = 0; e < N; ++e) t[e] = code_of(x[e], step, mid) << 16;
-  } else if (least == 0) {
+  } else if (((least & 0xffffu) == 0 || least < 0x10000u) && Lane16<T>::may_touch(raw, par)) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
       if ((t[e] & 0xffffu) == 0) {
@@ -132,7 +149,7 @@ __device__ __forceinline__ uint32_t codes_of(const float (&x)[N], uint32_t par, 
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(NT) compact_quant_kernel(const __grid_constant__ CompactQuantParams p) {
+__global__ void __launch_bounds__(NT, 4) compact_quant_kernel(const __grid_constant__ CompactQuantParams p) {
   using R = QuantRow<D>;
   using V = Lane16<T>;
   constexpr int LPR = D / V::N;   // lanes per row
@@ -182,9 +199,7 @@ __global__ void __launch_bounds__(NT) compact_quant_kernel(const __grid_constant
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      float e[V::N];
-      V::values(raw[j], e);
-      const uint32_t codes = codes_of(e, __shfl_sync(0xffffffffu, own, j, 4), __shfl_sync(0xffffffffu, own_units, j, 4));
+      const uint32_t codes = codes_of<T>(raw[j], __shfl_sync(0xffffffffu, own, j, 4), __shfl_sync(0xffffffffu, own_units, j, 4));
       // two half-words of neighbouring groups make a word: the lanes GL apart exchange what the other one stores
       const bool odd = G % 2;
       const uint32_t got = __shfl_xor_sync(0xffffffffu, V::N == 4 ? codes : odd ? codes : codes >> 16, GL);
