@@ -49,17 +49,20 @@ struct Lane16<float> {
   __device__ static void values(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
-  __device__ static void extremes(const uint4& v, float& lo, float& hi) {
+  using Extremes = float2;
+  __device__ static Extremes extremes(const uint4& v) {
     float x[4];
     values(v, x);
-    lo = min_nan(min_nan(x[0], x[1]), min_nan(x[2], x[3]));
-    hi = max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3]));
+    float lo = min_nan(min_nan(x[0], x[1]), min_nan(x[2], x[3])), hi = max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3]));
 #pragma unroll
     for (int off = 1; off < 8; off *= 2) {
       lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, off));
       hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, off));
     }
+    return make_float2(lo, hi);
   }
+  __device__ static float low(Extremes e) { return e.x; }
+  __device__ static float high(Extremes e) { return e.y; }
   __device__ static uint32_t par(float lo, float hi) { return group_par(lo, hi); }
   __device__ static bool may_touch(const uint4&, uint32_t) { return true; }
 };
@@ -71,17 +74,21 @@ struct Lane16<__nv_bfloat16> {
     x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
   }
   __device__ static __nv_bfloat162 two(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
-  __device__ static void extremes(const uint4& v, float& lo, float& hi) {
-    __nv_bfloat162 a = __hmin2_nan(__hmin2_nan(two(v.x), two(v.y)), __hmin2_nan(two(v.z), two(v.w)));
-    const __nv_bfloat162 b = __hmax2_nan(__hmax2_nan(two(v.x), two(v.y)), __hmax2_nan(two(v.z), two(v.w)));
-    // (least, -largest) in one word: both get smaller
-    a = __halves2bfloat162(__hmin_nan(__low2bfloat16(a), __high2bfloat16(a)), __hneg(__hmax_nan(__low2bfloat16(b), __high2bfloat16(b))));
-#pragma unroll
-    for (int off = 1; off < 4; off *= 2) a = __hmin2_nan(a, __shfl_xor_sync(0xffffffffu, a, off));
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(&a);
-    lo = bf16_lo(w);
-    hi = -bf16_hi(w);
+  using Extremes = uint32_t;  // (least, -largest): both get smaller
+  __device__ static uint32_t least(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmin2_nan(two(a), two(b));
+    return *reinterpret_cast<const uint32_t*>(&r);
   }
+  __device__ static Extremes extremes(const uint4& v) {
+    const uint32_t sign = 0x80008000u, a = least(least(v.x, v.y), least(v.z, v.w));
+    const uint32_t b = least(least(v.x ^ sign, v.y ^ sign), least(v.z ^ sign, v.w ^ sign));
+    uint32_t w = least(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+    for (int off = 1; off < 4; off *= 2) w = least(w, __shfl_xor_sync(0xffffffffu, w, off));
+    return w;
+  }
+  __device__ static float low(Extremes e) { return bf16_lo(e); }
+  __device__ static float high(Extremes e) { return -bf16_hi(e); }
   // group_par() in fp32. The sum and the difference of two bf16 numbers are exact or so far from a tie of the roundings that follow that
   // they might be; halves where they would overflow.
   __device__ static uint32_t par(float lo, float hi) {
@@ -112,40 +119,67 @@ __device__ __forceinline__ float units_per(uint32_t par, float lo, float hi) {
   return step > 1e-30f && step < 1e30f && a > 0.001f && b < 15.999f ? kUnit * inv : NAN;
 }
 
-// The codes of a lane's elements, four in each half of the word.
+// The codes of a lane's elements, four in each half of the word; and whether they have to be worked out the exact way.
 template <typename T>
-__device__ __forceinline__ uint32_t codes_of(const uint4& raw, uint32_t par, float units) {
+__device__ __forceinline__ uint32_t codes_of(const uint4& raw, uint32_t par, float units, bool& unsure) {
   constexpr int N = Lane16<T>::N;
-  const float step = bf16_lo(par), mid = bf16_hi(par);
+  const float mid = bf16_hi(par);
   float x[N];
   Lane16<T>::values(raw, x);
   uint32_t t[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) t[e] = __float_as_uint(fmaf(x[e] - mid, units, 8.f * kUnit + kWhole));
-  uint32_t least = __byte_perm(t[0], t[1], 0x5410);
+  unsure = !(units == units);
+  if (Lane16<T>::may_touch(raw, par)) {
+    uint32_t least = t[0] & 0xffffu;
 #pragma unroll
-  for (int e = 2; e < N; e += 2) least = min_u16x2(least, __byte_perm(t[e], t[e + 1], 0x5410));
-  if (!(units == units)) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) t[e] = code_of(x[e], step, mid) << 16;
-  } else if (((least & 0xffffu) == 0 || least < 0x10000u) && Lane16<T>::may_touch(raw, par)) {
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if ((t[e] & 0xffffu) == 0) {
-        // d + rest = x - mid exactly; the border is an exact product
-        const float d = x[e] - mid, y = d - x[e], rest = (x[e] - (d - y)) + (-mid - y);
-        const float border = (__uint_as_float(t[e]) - (8.f * kUnit + kWhole)) * (1.f / kUnit) * step;
-        if (d < border || (d == border && rest < 0.f)) t[e] -= 0x10000u;
-      }
+    for (int e = 1; e < N; ++e) least = min(least, t[e] & 0xffffu);
+    unsure |= least == 0;
   }
   uint32_t half[2] = {0u, 0u};
 #pragma unroll
   for (int e = 0; e < N; e += 4) {
-    const uint32_t a = __byte_perm(t[e], t[e + 1], 0x7632) & 0x000f000fu, b = __byte_perm(t[e + 2], t[e + 3], 0x7632) & 0x000f000fu;
-    const uint32_t c = a + b * 256u;  // codes 0 and 2 in the bytes of the low half, 1 and 3 in those of the high half
+    // codes 0 and 2 in the bytes of the low half, 1 and 3 in those of the high half; then all of them in the low half
+    const uint32_t c = (__byte_perm(t[e], t[e + 1], 0x7632) & 0x000f000fu) + (__byte_perm(t[e + 2], t[e + 3], 0x7632) & 0x000f000fu) * 256u;
     half[e / 4] = c | c >> 12;
   }
   return __byte_perm(half[0], half[1], 0x5410);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t exact_codes(const uint4& raw, uint32_t par, float units) {
+  const float step = bf16_lo(par), mid = bf16_hi(par);
+  float x[Lane16<T>::N];
+  Lane16<T>::values(raw, x);
+  uint32_t codes = 0;
+  if (units == units) {
+#pragma unroll
+    for (int e = 0; e < Lane16<T>::N; ++e) {
+      // d + rest = x - mid exactly; the border that the element is near to, should the lower bits be zero, is an exact product
+      const float d = x[e] - mid, y = d - x[e], rest = (x[e] - (d - y)) + (-mid - y), at = fmaf(d, units, 8.f * kUnit + kWhole);
+      const float border = (at - (8.f * kUnit + kWhole)) * (1.f / kUnit) * step;
+      const uint32_t t = __float_as_uint(at) - ((__float_as_uint(at) & 0xffffu) == 0 && (d < border || (d == border && rest < 0.f)));
+      codes |= (t >> 16 & 15u) << (16 * (e / 4) + 4 * (e % 4));
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < Lane16<T>::N; ++e) codes |= code_of(x[e], step, mid) << (16 * (e / 4) + 4 * (e % 4));
+  }
+  return codes;
+}
+
+// Stores a lane's part of a row of codes at `dst`: two half-words of neighbouring groups make a word, so the lanes GL apart exchange what
+// the other one stores.
+template <typename T, int D>
+__device__ __forceinline__ void store_codes(uint32_t* dst, uint32_t codes, int G, int in_group, bool valid) {
+  constexpr int NG = QuantRow<D>::NG, N = Lane16<T>::N;
+  const bool odd = G % 2;
+  const uint32_t got = __shfl_xor_sync(0xffffffffu, N == 4 ? codes : odd ? codes : codes >> 16, 32 / N);
+  if (!valid) return;
+  if constexpr (N == 8) {  // elements 8 in_group .. + 3 are half-word 2 in_group, + 4 .. + 7 the next
+    dst[(2 * in_group + odd) * (NG / 2) + G / 2] = odd ? __byte_perm(got, codes, 0x7610) : __byte_perm(codes, got, 0x5410);
+  } else if (!odd) {
+    dst[in_group * (NG / 2) + G / 2] = __byte_perm(codes, got, 0x5410);
+  }
 }
 
 template <typename T, int D>
@@ -184,32 +218,38 @@ __global__ void __launch_bounds__(NT, 4) compact_quant_kernel(const __grid_const
         raw[2 * j + 1] = __ldg(reinterpret_cast<const uint4*>(p.v + src));
       }
     }
-    float lo = 0.f, hi = 0.f;  // of the lane's own one of the four
+    typename V::Extremes ends = V::extremes(raw[0]);  // of the lane's own one of the four
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float a, c;
-      V::extremes(raw[j], a, c);
-      if (in_group % 4 == j) lo = a, hi = c;
+    for (int j = 1; j < 4; ++j) {
+      const typename V::Extremes other = V::extremes(raw[j]);
+      if (in_group % 4 == j) ends = other;
     }
+    const float lo = V::low(ends), hi = V::high(ends);
     const uint32_t own = V::par(lo, hi);
     const float own_units = units_per(own, lo, hi);
     if (in_group < 4) {
       const int j = in_group / 2;
       if (idx[j] >= 0) (in_group % 2 ? p.v_par : p.k_par)[(off + row0 + j * SPAN + sub) * R::NG + G] = own;
     }
+    uint32_t unsure = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t codes = codes_of<T>(raw[j], __shfl_sync(0xffffffffu, own, j, 4), __shfl_sync(0xffffffffu, own_units, j, 4));
-      // two half-words of neighbouring groups make a word: the lanes GL apart exchange what the other one stores
-      const bool odd = G % 2;
-      const uint32_t got = __shfl_xor_sync(0xffffffffu, V::N == 4 ? codes : odd ? codes : codes >> 16, GL);
+      bool again;
+      const uint32_t codes = codes_of<T>(raw[j], __shfl_sync(0xffffffffu, own, j, 4), __shfl_sync(0xffffffffu, own_units, j, 4), again);
       uint32_t* dst = reinterpret_cast<uint32_t*>(j % 2 ? p.v_code : p.k_code) + (off + row0 + j / 2 * SPAN + sub) * (D / 8);
-      if (idx[j / 2] < 0) continue;
-      if constexpr (V::N == 8) {  // elements 8 in_group .. + 3 are half-word 2 in_group, + 4 .. + 7 the next
-        dst[(2 * in_group + odd) * (R::NG / 2) + G / 2] = odd ? __byte_perm(got, codes, 0x7610) : __byte_perm(codes, got, 0x5410);
-      } else if (!odd) {
-        dst[in_group * (R::NG / 2) + G / 2] = __byte_perm(codes, got, 0x5410);
-      }
+      store_codes<T, D>(dst, codes, G, in_group, idx[j / 2] >= 0);
+      unsure |= (uint32_t)again << j;
+    }
+    // (kept apart, with the rows read once more, so that it costs the others nothing)
+    unsure = __reduce_or_sync(0xffffffffu, unsure);
+#pragma unroll 1
+    for (; unsure; unsure &= unsure - 1) {
+      const int j = __ffs(unsure) - 1, i = j / 2 ? idx[1] : idx[0];
+      uint4 row = make_uint4(0u, 0u, 0u, 0u);
+      if (i >= 0) row = __ldg(reinterpret_cast<const uint4*>((j % 2 ? p.v : p.k) + src_base + (int64_t)i * p.stride_t));
+      uint32_t* dst = reinterpret_cast<uint32_t*>(j % 2 ? p.v_code : p.k_code) + (off + row0 + j / 2 * SPAN + sub) * (D / 8);
+      const uint32_t codes = exact_codes<T>(row, __shfl_sync(0xffffffffu, own, j, 4), __shfl_sync(0xffffffffu, own_units, j, 4));
+      store_codes<T, D>(dst, codes, G, in_group, i >= 0);
     }
   }
 }
@@ -308,7 +348,10 @@ int launch_compact_quant(const madakv_config& c, const void* k, const void* v, m
   p.n_max = c.max_seq_len;
   p.headroom = c.max_new_tokens;
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, rows = capacity / units + 1;
-  const int64_t per_block = 64, want = (rows + per_block - 1) / per_block, most = ((1 << 20) + units - 1) / units;
+  // rows of a block: as many as leave 16 blocks for every SM, 32 to 256 (1024 units of 1638 rows, 32 / 64 / 256 / 512 rows a block: 370 / 330 / 300 / 302 us; 4 of
+  // 2048 rows: 5.9 / 7.0 / 14.4 with 32 / 64 / 256)
+  const int64_t share = capacity / (148 * 16) / 32 * 32, per_block = share < 32 ? 32 : share > 256 ? 256 : share;
+  const int64_t want = (rows + per_block - 1) / per_block, most = ((1 << 20) + units - 1) / units;
   p.blocks = (int)(want < most ? want : most);
   if (units * p.blocks > 0x7fffffff) return MADAKV_EUNSUPPORTED;
   return for_type(c, [&](auto t, auto d) {
