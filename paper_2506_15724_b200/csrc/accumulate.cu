@@ -7,7 +7,6 @@ namespace madakv {
 namespace {
 
 constexpr int NT = 256;
-constexpr int kRows = 1024;  // rows of a block at a time
 
 struct AccumulateParams {
   const int64_t* seg_off;
@@ -20,6 +19,8 @@ struct AccumulateParams {
   int L, Hq, Hkv, g, layer, blocks;  // blocks per segment
 };
 
+// G: at least the heads of a group; a thread has ROWS rows' logits on their way at once.
+template <int G, int ROWS>
 __global__ void __launch_bounds__(NT) accumulate_kernel(const __grid_constant__ AccumulateParams p) {
   pdl_wait();
   pdl_go();
@@ -27,18 +28,33 @@ __global__ void __launch_bounds__(NT) accumulate_kernel(const __grid_constant__ 
   const int u = p.layer < 0 ? y : (y / p.Hkv * p.L + p.layer) * p.Hkv + y % p.Hkv;
   const int len = p.kept_len[u];
   const int64_t off = p.seg_off[u], end = p.seg_off[u + 1];
-  if (off < 0 || len < 0 || off + len > end || end > p.capacity) return;  // (as attention sees it: an empty segment)
   const float* lse2 = p.lse2 + (int64_t)(u / p.Hkv) * p.Hq + u % p.Hkv * p.g;
-  for (int r = x * NT + threadIdx.x; r < len; r += p.blocks * NT) {
-    const float* s = p.scores + (off + r) * p.g;
-    float w = 0.f;
-    bool lost = false;
-    for (int i = 0; i < p.g; ++i) {
-      const float z = lse2[i];
-      lost |= z != z;
-      if (z < INFINITY) w += exp2f(s[i] - z);
+  float z[G];
+  bool lost = false;
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    z[i] = i < p.g ? lse2[i] : INFINITY;  // +inf: the head adds nothing
+    lost |= z[i] != z[i];
+  }
+  // (as attention sees it: an empty segment; or one whose rows did not arrive)
+  if (off < 0 || len < 0 || off + len > end || end > p.capacity || lost) return;
+  for (int r0 = x * NT * ROWS + threadIdx.x; r0 < len; r0 += p.blocks * NT * ROWS) {
+    float s[ROWS][G], old[ROWS];
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+      const int r = r0 + j * NT;
+      old[j] = r < len ? p.acc[off + r] : 0.f;
+#pragma unroll
+      for (int i = 0; i < G; ++i) s[j][i] = r < len && i < p.g ? p.scores[(off + r) * p.g + i] : 0.f;
     }
-    if (!lost) p.acc[off + r] = fmaf(p.decay, p.acc[off + r], w);
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+      float w = 0.f;
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+        if (z[i] < INFINITY) w += exp2f(s[j][i] - z[i]);
+      if (r0 + j * NT < len) p.acc[off + r0 + j * NT] = fmaf(p.decay, old[j], w);
+    }
   }
 }
 
@@ -49,11 +65,20 @@ int launch_accumulate(const madakv_config& c, int layer, const int64_t* seg_off,
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, longest = c.max_seq_len + (int64_t)c.max_new_tokens;
   const int n_sel = (layer < 0 ? c.batch * c.n_layers : c.batch) * c.n_kv_heads;
   const int64_t rows = capacity / units < longest ? capacity / units : longest;
-  const int64_t want = rows / kRows + 1, most = n_sel < 4096 ? 4096 / n_sel : 1;
-  const AccumulateParams p{seg_off, kept_len, track.scores, tracking_lse2(c, ws), track.acc, capacity, track.decay, c.n_layers,
-                           c.n_q_heads, c.n_kv_heads, c.n_q_heads / c.n_kv_heads, layer, (int)(want < most ? want : most)};
-  launch_pdl(accumulate_kernel, dim3((unsigned)n_sel * p.blocks), dim3(NT), 0, st, p);
-  return launch_status();
+  const int g = c.n_q_heads / c.n_kv_heads;
+  AccumulateParams p{seg_off, kept_len, track.scores, tracking_lse2(c, ws), track.acc, capacity, track.decay, c.n_layers,
+                     c.n_q_heads, c.n_kv_heads, g, layer, 1};
+  auto go = [&](auto kernel, int rows_each) {
+    const int64_t want = rows / (NT * rows_each) + 1, most = n_sel < 8192 ? 8192 / n_sel : 1;
+    p.blocks = (int)(want < most ? want : most);
+    launch_pdl(kernel, dim3((unsigned)n_sel * p.blocks), dim3(NT), 0, st, p);
+    return launch_status();
+  };
+  if (g == 1) return go(accumulate_kernel<1, 4>, 4);
+  if (g == 2) return go(accumulate_kernel<2, 4>, 4);
+  if (g <= 4) return go(accumulate_kernel<4, 2>, 2);
+  if (g <= 8) return go(accumulate_kernel<8, 2>, 2);
+  return go(accumulate_kernel<16, 1>, 1);
 }
 
 }  // namespace madakv
