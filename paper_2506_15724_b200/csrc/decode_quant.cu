@@ -57,10 +57,11 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {  // an 8 x 8 matrix
 // 0, 3, 4, 7, so that neither the loads of K (all slots) nor of V (every other slot) meet more than twice in a bank.
 __device__ __forceinline__ int slot_row(int s) { return s ^ ((s >> 1) & 1); }
 
-// The four operand registers of eight codes, the e-th of either half-word: 16 + code, or code - 7.5.
-template <bool kExact>
+// The four operand registers of eight codes, the e-th of either half-word: 16 + code, or code - 7.5. kFirst128: 128 + code for e = 0,
+// which spares a shift, at five times the bits that the offset takes from a sum (V's, whose results are rounded to bf16).
+template <bool kExact, bool kFirst128 = false>
 __device__ __forceinline__ void operands(uint32_t x, uint32_t (&r)[4]) {
-  r[0] = ((x << 3) & 0x00780078u) | 0x41804180u;
+  r[0] = kFirst128 ? (x & 0x000f000fu) | 0x43004300u : ((x << 3) & 0x00780078u) | 0x41804180u;
   r[1] = ((x >> 1) & 0x00780078u) | 0x41804180u;
   r[2] = ((x >> 5) & 0x00780078u) | 0x41804180u;
   r[3] = ((x >> 9) & 0x00780078u) | 0x41804180u;
@@ -398,7 +399,7 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           uint32_t a[2][4];
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            operands<kExact>(__byte_perm(vw[2 * e][G / 2], vw[2 * e + 1][G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
+            operands<kExact, !kExact>(__byte_perm(vw[2 * e][G / 2], vw[2 * e + 1][G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
           const uint32_t a0[4] = {a[0][0], a[0][1], a[1][0], a[1][1]}, a1[4] = {a[0][2], a[0][3], a[1][2], a[1][3]};
           const uint32_t one[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
           const float step[2] = {bf16_lo(vp[0][G]), bf16_lo(vp[1][G])}, mid[2] = {bf16_hi(vp[0][G]), bf16_hi(vp[1][G])};
@@ -441,9 +442,10 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           float add = mids[n][G][e];
 #pragma unroll
           for (int sh = 4; sh <= 16; sh *= 2) add += __shfl_xor_sync(0xffffffffu, add, sh);
+          const float first = kExact ? add : fmaf(-135.5f, ones[n][G][e], add);
           if (!kExact) add = fmaf(-23.5f, ones[n][G][e], add);
           *reinterpret_cast<float4*>(so + head * OPITCH + 32 * G + 4 * gid) = make_float4(
-              o[n][G][0][e] + add, o[n][G][0][e + 2] + add, o[n][G][1][e] + add, o[n][G][1][e + 2] + add);
+              o[n][G][0][e] + first, o[n][G][0][e + 2] + add, o[n][G][1][e] + add, o[n][G][1][e + 2] + add);
         }
       }
     __syncthreads();

@@ -254,6 +254,8 @@ __global__ void __launch_bounds__(NT, 4) compact_quant_kernel(const __grid_const
   }
 }
 
+constexpr int kExpandRows = 2;  // of K and of V that a thread has on their way
+
 struct ExpandParams {
   const int64_t* rows;
   const uint8_t* k_code;
@@ -293,22 +295,36 @@ __global__ void __launch_bounds__(NT) expand_quant_kernel(const __grid_constant_
   pdl_wait();
   pdl_go();
   const int lane = threadIdx.x % LPR, G = lane / GL, in_group = lane % GL;
-  for (int64_t r = (int64_t)blockIdx.x * SPAN + threadIdx.x / LPR; r < p.n_rows; r += (int64_t)gridDim.x * SPAN) {
-    const int64_t row = p.rows ? p.rows[r] : r;
-    const bool there = row >= 0 && row < p.capacity;
+  for (int64_t r0 = (int64_t)blockIdx.x * SPAN * kExpandRows + threadIdx.x / LPR; r0 < p.n_rows; r0 += (int64_t)gridDim.x * SPAN * kExpandRows) {
+    int64_t row[kExpandRows];
+    uint32_t code[kExpandRows][2], par[kExpandRows][2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint16_t* code = reinterpret_cast<const uint16_t*>(j ? p.v_code : p.k_code) + row * (D / 4) + G;
-      float x[N];
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = 0.f;
-      if (there) {
-        const uint32_t par = (j ? p.v_par : p.k_par)[row * R::NG + G];
-#pragma unroll
-        for (int e = 0; e < N; e += 4) values4(code[(N / 4 * in_group + e / 4) * R::NG], bf16_lo(par), bf16_hi(par), x + e);
-      }
-      store16(reinterpret_cast<T*>(j ? p.v_out : p.k_out) + r * D + lane * N, x);
+    for (int i = 0; i < kExpandRows; ++i) {
+      const int64_t r = r0 + i * SPAN;
+      row[i] = r < p.n_rows ? (p.rows ? __ldg(p.rows + r) : r) : -1;
+      if (row[i] >= p.capacity) row[i] = -1;
     }
+#pragma unroll
+    for (int i = 0; i < kExpandRows; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        code[i][j] = par[i][j] = 0u;  // (zeros)
+        if (row[i] < 0) continue;
+        const uint16_t* half = reinterpret_cast<const uint16_t*>(j ? p.v_code : p.k_code) + row[i] * (D / 4) + N / 4 * in_group * R::NG + G;
+        code[i][j] = __ldg(half) | (N == 8 ? (uint32_t)__ldg(half + R::NG) << 16 : 0u);
+        par[i][j] = __ldg((j ? p.v_par : p.k_par) + row[i] * R::NG + G);
+      }
+#pragma unroll
+    for (int i = 0; i < kExpandRows; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int64_t r = r0 + i * SPAN;
+        if (r >= p.n_rows) continue;
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; e += 4) values4(code[i][j] >> (4 * e) & 0xffffu, bf16_lo(par[i][j]), bf16_hi(par[i][j]), x + e);
+        store16(reinterpret_cast<T*>(j ? p.v_out : p.k_out) + r * D + lane * N, x);
+      }
   }
 }
 
@@ -362,8 +378,8 @@ int launch_compact_quant(const madakv_config& c, const void* k, const void* v, m
 int launch_expand_quant(const madakv_config& c, const int64_t* rows, int64_t n_rows, const uint8_t* k_code, const void* k_par,
                         const uint8_t* v_code, const void* v_par, int64_t capacity, void* k_out, void* v_out, cudaStream_t st) {
   const ExpandParams p{rows, k_code, v_code, (const uint32_t*)k_par, (const uint32_t*)v_par, k_out, v_out, n_rows, capacity};
-  const int64_t rpb = NT / (c.head_dim * elem_bytes(c) / 16), want = (n_rows + rpb - 1) / rpb;
-  const unsigned grid = (unsigned)(want < (1 << 20) ? want : (1 << 20));
+  const int64_t rpb = NT / (c.head_dim * elem_bytes(c) / 16) * kExpandRows, want = (n_rows + rpb - 1) / rpb;
+  const unsigned grid = (unsigned)(want < 148 * 64 ? want : 148 * 64);
   return for_type(c, [&](auto t, auto d) {
     launch_pdl(expand_quant_kernel<decltype(t), decltype(d)::value>, dim3(grid), dim3(NT), 0, st, p);
   });
