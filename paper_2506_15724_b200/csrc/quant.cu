@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(NT, 4) compact_quant_kernel(const __grid_const
       const uint32_t codes = codes_of<T>(raw[j], __shfl_sync(0xffffffffu, own, j, 4), __shfl_sync(0xffffffffu, own_units, j, 4), again);
       uint32_t* dst = reinterpret_cast<uint32_t*>(j % 2 ? p.v_code : p.k_code) + (off + row0 + j / 2 * SPAN + sub) * (D / 8);
       store_codes<T, D>(dst, codes, G, in_group, idx[j / 2] >= 0);
-      unsure |= (uint32_t)again << j;
+      unsure |= (uint32_t)(again && idx[j / 2] >= 0) << j;
     }
     // (kept apart, with the rows read once more, so that it costs the others nothing)
     unsure = __reduce_or_sync(0xffffffffu, unsure);

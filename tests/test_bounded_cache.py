@@ -398,6 +398,42 @@ def test_decode_steps_equal_the_formula(dtype, d, g, units, lens, track, quant):
         check_step(cache, dtype, step, layer, before, out, lse, kn, vn, q, track, decay, position)
 
 
+# one block per SM for few long segments, in each number of warps that it has; one block per segment beyond the arrival counters
+@pytest.mark.gpu
+@pytest.mark.parametrize("track", [False, True])
+@pytest.mark.parametrize("dtype,d,g,units,lens", [("bf16", 64, 3, 1, [120001]), ("bf16", 64, 11, 2, [90000, 37003]), ("f32", 64, 2, 1, [115007]),
+                                                  ("bf16", 128, 1, 4, [29000, 0, 31000, 60001]), ("bf16", 64, 1, 17000, [i % 5 for i in range(17000)])])
+def test_decode_on_few_long_and_on_very_many_segments(dtype, d, g, units, lens, track):
+    cfg = config(dtype, 1, units, g, 1, d, max(lens) + 1, new=3)
+    cache = Cache(cfg, lens, seed=g)
+    pos = torch.tensor([123456], dtype=torch.int32, device="cuda")
+    q, kn, vn = cache.step(7)
+    before = (cache.kept_len.cpu().numpy(), cache.acc.cpu().numpy(), cache.kept_idx.cpu().numpy(), [a.clone() for a in cache.arrays])
+    out, lse = cache.decode(q, kn, vn, -1, cache.tracking(pos, 0.25) if track else ())
+    assert mk.madakv_poll_status(cache.ws) == 0
+    check_step(cache, dtype, 7, -1, before, out, lse, kn, vn, q, track, 0.25, [123456])
+
+
+@pytest.mark.gpu
+def test_tracking_where_rows_do_not_arrive(monkeypatch):
+    """The copies of cache rows are withheld: the waits run out, results are NaN, sums of weights stay as they were."""
+    lens = [300, 2000, 40]
+    cfg = config("bf16", 1, 3, 1, 1, 128, 2048)
+    cache = Cache(cfg, lens, quant=False)
+    q, kn, vn = cache.step(0)
+    acc = cache.acc.clone()
+    monkeypatch.setenv("MADAKV_TEST_HOLD_COPIES", "200000")
+    out, lse = cache.decode(q, kn, vn, track=(cache.acc, cache.scratch))
+    assert mk.madakv_poll_status(cache.ws) == mk.ETIMEOUT
+    monkeypatch.delenv("MADAKV_TEST_HOLD_COPIES")
+    assert out.isnan().all() and lse.isnan().all()
+    for a, n in zip(cache.off, lens):
+        acc[int(a) + n] = 0.0  # (the appended row's)
+    assert torch.equal(cache.acc, acc) and cache.kept_len.tolist() == [n + 1 for n in lens]
+    out, lse = cache.decode(q, None, None, track=(cache.acc, cache.scratch))
+    assert mk.madakv_poll_status(cache.ws) == 0 and not out.isnan().any() and (cache.acc > acc).any()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d,g,units,lens", ATTEND)
 def test_tracking_changes_nothing_of_the_attention(dtype, d, g, units, lens):
@@ -574,6 +610,35 @@ def test_evict_equals_the_rule(kind, dtype, d, quant, lens, limit, recent):
         assert cache.kept_len.tolist() == want
         for x, y in zip(state, before):
             assert torch.equal(x.view(torch.uint8), y[source].view(torch.uint8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d,quant", [("bf16", 128, False), ("bf16", 64, True)])
+@pytest.mark.parametrize("units,rows,longest", [(400, 300, 300), (320, 1500, 9000), (300, 1, 3), (5, 2500, 7000), (3, 9000, 30000)])
+def test_evict_in_every_size_of_block(dtype, d, quant, units, rows, longest):
+    """Calls of many segments, of segments that fit the registers and of longer ones beside them; half of them have rows too many."""
+    rng = np.random.RandomState(units + rows)
+    lens = rng.randint(rows // 2, rows + 1, size=units)
+    lens[units // 2] = longest
+    cfg = config(dtype, 1, units, 1, 1, d, longest + 1, new=2)
+    cache = Cache(cfg, lens, seed=units, quant=quant)
+    limit = np.where(rng.rand(units) < 0.5, lens - rng.randint(0, 70, size=units), rng.randint(0, rows + 1, size=units))
+    state = [cache.acc, cache.kept_idx, *cache.arrays]
+    before = [x.clone() for x in state]
+    acc, idx = cache.acc.cpu().numpy(), cache.kept_idx.cpu().numpy()
+    source, want = np.arange(cache.cap), []
+    for u, n in enumerate(lens.tolist()):
+        a = int(cache.off[u])
+        c, src = trimmed(acc[a:a + n + 1], idx[a:a + n + 1], n, limit[u], 5)
+        want.append(c)
+        source[a:a + c] = a + src[:c]
+    source = torch.from_numpy(source).cuda()
+    call = mk.madakv_evict_quant if quant else mk.madakv_evict
+    lim = torch.from_numpy(limit.astype(np.int32)).cuda()
+    call(cfg, -1, lim, 5, cache.acc, cache.kept_idx, cache.seg_off, cache.kept_len, *cache.arrays, cache.ws)
+    assert mk.madakv_poll_status(cache.ws) == 0 and cache.kept_len.tolist() == want
+    for x, y in zip(state, before):
+        assert torch.equal(x.view(torch.uint8), y[source].view(torch.uint8))
 
 
 @pytest.mark.gpu
