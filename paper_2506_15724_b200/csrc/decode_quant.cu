@@ -7,13 +7,15 @@
 //            (step, mid) words as they lie in the cache with multiples of the queries' sums in three bf16 terms.
 //   values   sum of w v = sum of (w step) (code - 7.5) + w mid: the weights take the step of every group before they are rounded to
 //            bf16 for the product with the codes; mid is summed up in fp32
-// A code becomes an operand by a shift and one logical operation: its four bits are bits 3-6 of a bf16 mantissa under the exponent of
-// 16, which makes 16 + code. 23.5 times the sum of the other operand is taken off again: of the queries together with the mids, of
-// the weights by one more product, with ones, per group. The order of codes in a row is that of the operands: a lane's words are
-// one piece of 16 bytes (K) or 8 (V) a row, pairs along d for K, and of two rows for V.
-// fp32 (queries and weights): three bf16 terms each, whose products are exact and whose sum is fp32 again; the operands are
-// code - 7.5 then, so that no sum loses bits to the 23.5.
+// K's codes become fp16 operands (k_operands) and the queries, scaled by a power of two per head, fp16 numbers, in which they are exact;
+// V's become bf16 (v_operands), whose range the weights times step need: 16 + code, and 23.5 times the sum of the weights is taken
+// off at the end, from one more product, with ones, per group. The order of codes in a row is that of the
+// operands: a lane's words are one piece of 16 bytes (K) or 8 (V) a row, pairs along d for K, and of two rows for V.
+// fp32: queries as three fp16 terms and weights as three bf16 terms, whose products are exact and whose sum is fp32 again; V's
+// operands are code - 7.5 then, so that no sum loses bits to the 23.5.
 // A warp has tiles of 32 rows of its own, read ahead into a ring in shared memory by asynchronous copies.
+#include <cuda_fp16.h>
+
 #include <type_traits>
 
 #include "decode_common.cuh"
@@ -34,7 +36,8 @@ struct QuantTile {
   static constexpr int FRESH = kWarps * WARP;  // the appended row: codes and parameters of K, then of V
   static constexpr int QUERIES = FRESH + 2 * (R::CODE_BYTES + R::PAR_BYTES);  // operands of up to 16 heads in bf16 or 8 in fp32
   static_assert(QUERIES % 16 == 0, "read in 16-byte pieces");
-  static constexpr int query_bytes(int sets) { return sets * R::NG * 512; }
+  // the queries of 8 NH heads: operands of every term, then [8 NH] scales and [8 NH][NG] sums
+  static constexpr int query_bytes(int NH, int terms) { return NH * (R::NG * terms * 512 + 32 + 32 * R::NG); }
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
@@ -57,11 +60,27 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {  // an 8 x 8 matrix
 // 0, 3, 4, 7, so that neither the loads of K (all slots) nor of V (every other slot) meet more than twice in a bank.
 __device__ __forceinline__ int slot_row(int s) { return s ^ ((s >> 1) & 1); }
 
-// The four operand registers of eight codes, the e-th of either half-word: 16 + code, or code - 7.5. kFirst128: 128 + code for e = 0,
-// which spares a shift, at five times the bits that the offset takes from a sum (V's, whose results are rounded to bf16).
-template <bool kExact, bool kFirst128 = false>
-__device__ __forceinline__ void operands(uint32_t x, uint32_t (&r)[4]) {
-  r[0] = kFirst128 ? (x & 0x000f000fu) | 0x43004300u : ((x << 3) & 0x00780078u) | 0x41804180u;
+// The four fp16 operand registers of eight codes, the e-th of either half-word: the codes themselves. Codes 0 and 1 stand in the lower
+// bits of a mantissa under the exponent of 1024 without a shift, codes 2 and 3 after one; an addition or a fused multiply-add, on a
+// pipe that has little else to do, takes the 1024 off.
+__device__ __forceinline__ void k_operands(uint32_t x, uint32_t (&r)[4]) {
+  const uint32_t y = x >> 8;
+  const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f), less = __floats2half2_rn(-64.f, -64.f), base = __floats2half2_rn(1024.f, 1024.f);
+  r[0] = (x & 0x000f000fu) | 0x64006400u;
+  r[1] = (x & 0x00f000f0u) | 0x64006400u;
+  r[2] = (y & 0x000f000fu) | 0x64006400u;
+  r[3] = (y & 0x00f000f0u) | 0x64006400u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __half2 v = *reinterpret_cast<__half2*>(&r[e]), c = e % 2 ? __hfma2(v, sixteenth, less) : __hsub2(v, base);
+    r[e] = *reinterpret_cast<const uint32_t*>(&c);
+  }
+}
+// The four bf16 operand registers of eight codes: 16 + code, or code - 7.5. (128 + code, which the lowest four bits give without a shift,
+// costs the sums of 130000 flat weights as much as the rounding of the result.)
+template <bool kExact>
+__device__ __forceinline__ void v_operands(uint32_t x, uint32_t (&r)[4]) {
+  r[0] = ((x << 3) & 0x00780078u) | 0x41804180u;
   r[1] = ((x >> 1) & 0x00780078u) | 0x41804180u;
   r[2] = ((x >> 5) & 0x00780078u) | 0x41804180u;
   r[3] = ((x >> 9) & 0x00780078u) | 0x41804180u;
@@ -72,6 +91,26 @@ __device__ __forceinline__ void operands(uint32_t x, uint32_t (&r)[4]) {
       r[e] = *reinterpret_cast<const uint32_t*>(&v);
     }
   }
+}
+// c (+)= a b in fp16.
+__device__ __forceinline__ void mma_codes(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_codes_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+// The nearest fp16 numbers of x and y; what is left of the two stays in them.
+__device__ __forceinline__ uint32_t next_halves(float& x, float& y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  x -= __low2float(h);
+  y -= __high2float(h);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ uint64_t pair_of(float x, float y) {
   uint64_t r;
@@ -199,48 +238,70 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           reinterpret_cast<uint32_t*>(warp ? p.v_par : p.k_par)[row * NG + l] = par;
         }
       }
-      __syncthreads();
     }
 
-    // queries as B operands: products j = 0, 1 of group G pair element 8 t + 2 j + {0, 1} with 8 t + 4 + 2 j + {0, 1}; and their sums
-    // (the same for all warps: they lie in shared memory, 16 bytes of every lane together)
-    uint4* qb = reinterpret_cast<uint4*>(dsmem + QT::QUERIES) + lane;
-    uint32_t qm[NH][3];  // the sums as operands against (step, mid) pairs, in three terms: lane t has group t's
+    // queries as operands: products j = 0, 1 of group G pair element 8 t + 2 j + {0, 1} with 8 t + 4 + 2 j + {0, 1}. The same for all
+    // warps: they lie in shared memory, 16 bytes of every lane together, and the first warps make a group each
+    uint4* queries = reinterpret_cast<uint4*>(dsmem + QT::QUERIES) + lane;
+    float* scales = reinterpret_cast<float*>(dsmem + QT::QUERIES + NH * NG * TERMS * 512);
+    float* sums = scales + 8 * NH;
+    if (warp < NG) {
 #pragma unroll
-    for (int n = 0; n < NH; ++n) {
-      float own_sum = 0.f;
-#pragma unroll
-      for (int G = 0; G < NG; ++G) {
-        float x[8], sum = 0.f;
+      for (int n = 0; n < NH; ++n) {
+        const int head = 8 * n + gid;
+        float x[8], top = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if (8 * n + gid < p.g) {
-          const T* q = reinterpret_cast<const T*>(p.q) + ((int64_t)bl * p.Hq + h * p.g + 8 * n + gid) * D + 32 * G + 8 * t;
-          load4(q, *reinterpret_cast<float(*)[4]>(x));
-          load4(q + 4, *reinterpret_cast<float(*)[4]>(x + 4));
-        }
+        if (head < p.g) {
+          const T* q = reinterpret_cast<const T*>(p.q) + ((int64_t)bl * p.Hq + h * p.g + head) * D + 8 * t;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += x[e];
+          for (int G = 0; G < NG; ++G) {
+            float v[8];
+            load4(q + 32 * G, *reinterpret_cast<float(*)[4]>(v));
+            load4(q + 32 * G + 4, *reinterpret_cast<float(*)[4]>(v + 4));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              top = fmaxf(top, fabsf(v[e]));
+              if (G == warp) x[e] = v[e];
+            }
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // the head's largest element comes to [2^14, 2^15), where fp16 holds what is 2^-29 of it or more; an infinity makes the head NaN
+        const int k = min(60, 14 - ((int)(__float_as_uint(top) >> 23) - 127));
+        const float up = __uint_as_float((uint32_t)(k + 127) << 23);
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += x[e] *= up;
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (t == G) own_sum = sum;
+        if (t == 0) {
+          sums[head * NG + warp] = sum;
+          if (warp == 0) scales[head] = top < INFINITY ? p.scale2 * __uint_as_float((uint32_t)(127 - k) << 23) : NAN;
+        }
 #pragma unroll
         for (int term = 0; term < TERMS; ++term) {
           uint4 w;
-          w.x = next_term(x[0], x[4]);
-          w.y = next_term(x[1], x[5]);
-          w.z = next_term(x[2], x[6]);
-          w.w = next_term(x[3], x[7]);
-          if (warp == 0) qb[((n * TERMS + term) * NG + G) * 32] = w;
+          w.x = next_halves(x[0], x[4]);
+          w.y = next_halves(x[1], x[5]);
+          w.z = next_halves(x[2], x[6]);
+          w.w = next_halves(x[3], x[7]);
+          queries[((n * TERMS + term) * NG + warp) * 32] = w;
         }
       }
-#pragma unroll
-      float off_sum = kExact ? 0.f : -23.5f * own_sum;
-#pragma unroll
-      for (int term = 0; term < 3; ++term) qm[n][term] = next_term(off_sum, own_sum);
     }
-
     __syncthreads();
+    uint32_t qm[NH][3];  // the sums as operands against (step, mid) words: lane t has group t's
+    float scale[NH][2];  // of heads 2 t and 2 t + 1: what the scaling took, and the softmax's scale
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      float sum = t < NG ? sums[(8 * n + gid) * NG + t] : 0.f, off_sum = -7.5f * sum;
+#pragma unroll
+      for (int term = 0; term < 3; ++term) qm[n][term] = next_term(off_sum, sum);
+      scale[n][0] = scales[8 * n + 2 * t];
+      scale[n][1] = scales[8 * n + 2 * t + 1];
+    }
     float m[NH][2], l[NH][2];
     float o[NH][NG][2][4], ones[NH][NG][4], mids[NH][NG][2];
 #pragma unroll
@@ -294,7 +355,7 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
         }
         const uint32_t ap[4] = {own_par[0], own_par[1], own_par[0], own_par[1]};
 #pragma unroll
-        for (int n = 0; n < NH; ++n) {  // sum over groups of (mid - 23.5 step) sum q
+        for (int n = 0; n < NH; ++n) {  // sum over groups of (mid - 7.5 step) sum q
           mma_first(s[n][half], ap, qm[n][2], 0u);
           mma_bf16_16816(s[n][half], ap, qm[n][0], qm[n][1]);
         }
@@ -303,19 +364,19 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           uint32_t a[2][4];
 #pragma unroll
           for (int e = 0; e < 2; ++e)  // elements 8 t .. + 3 of the group in the low half, + 4 .. + 7 in the high
-            operands<kExact>(__byte_perm(kw[e][G / 2], kw[e][KW / 2 + G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
+            k_operands(__byte_perm(kw[e][G / 2], kw[e][KW / 2 + G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
           const uint32_t a0[4] = {a[0][0], a[1][0], a[0][1], a[1][1]}, a1[4] = {a[0][2], a[1][2], a[0][3], a[1][3]};
 #pragma unroll
           for (int n = 0; n < NH; ++n) {
             float c[4];
 #pragma unroll
             for (int term = TERMS - 1; term >= 0; --term) {
-              const uint4 q = qb[((n * TERMS + term) * NG + G) * 32];
+              const uint4 q = queries[((n * TERMS + term) * NG + G) * 32];
               if (term == TERMS - 1)
-                mma_first(c, a0, q.x, q.y);
+                mma_codes_first(c, a0, q.x, q.y);
               else
-                mma_bf16_16816(c, a0, q.x, q.y);
-              mma_bf16_16816(c, a1, q.z, q.w);
+                mma_codes(c, a0, q.x, q.y);
+              mma_codes(c, a1, q.z, q.w);
             }
             fma_pair(s[n][half][0], s[n][half][1], bf16_lo(kp[0][G]), c[0], c[1]);
             fma_pair(s[n][half][2], s[n][half][3], bf16_lo(kp[1][G]), c[2], c[3]);
@@ -331,8 +392,8 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
             if (r + 16 * half + 8 * e + slot_row(gid) < row_end) {
 #pragma unroll
               for (int n = 0; n < NH; ++n) {
-                if (8 * n + 2 * t < p.g) dst[8 * n] = s[n][half][2 * e] * p.scale2;
-                if (8 * n + 2 * t + 1 < p.g) dst[8 * n + 1] = s[n][half][2 * e + 1] * p.scale2;
+                if (8 * n + 2 * t < p.g) dst[8 * n] = s[n][half][2 * e] * scale[n][0];
+                if (8 * n + 2 * t + 1 < p.g) dst[8 * n + 1] = s[n][half][2 * e + 1] * scale[n][1];
               }
             }
       }
@@ -356,14 +417,14 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          const float mn = fmaxf(m[n][e], mx), base = mn == -INFINITY ? 0.f : mn * p.scale2;
-          f[e] = fast_ex2(fmaf(m[n][e], p.scale2, -base));
+          const float mn = fmaxf(m[n][e], mx), base = mn == -INFINITY ? 0.f : mn * scale[n][e];
+          f[e] = fast_ex2(fmaf(m[n][e], scale[n][e], -base));
           m[n][e] = mn;
           float sum = 0.f;
 #pragma unroll
           for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) sum += s[n][half][2 * j + e] = fast_ex2(fmaf(s[n][half][2 * j + e], p.scale2, -base));
+            for (int j = 0; j < 2; ++j) sum += s[n][half][2 * j + e] = fast_ex2(fmaf(s[n][half][2 * j + e], scale[n][e], -base));
           l[n][e] = l[n][e] * f[e] + sum;
         }
         if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
@@ -399,7 +460,7 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           uint32_t a[2][4];
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            operands<kExact, !kExact>(__byte_perm(vw[2 * e][G / 2], vw[2 * e + 1][G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
+            v_operands<kExact>(__byte_perm(vw[2 * e][G / 2], vw[2 * e + 1][G / 2], G % 2 ? 0x7632 : 0x5410), a[e]);
           const uint32_t a0[4] = {a[0][0], a[0][1], a[1][0], a[1][1]}, a1[4] = {a[0][2], a[0][3], a[1][2], a[1][3]};
           const uint32_t one[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
           const float step[2] = {bf16_lo(vp[0][G]), bf16_lo(vp[1][G])}, mid[2] = {bf16_hi(vp[0][G]), bf16_hi(vp[1][G])};
@@ -410,12 +471,31 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
             mul_pair(w[2], w[3], step[1], s[n][half][2], s[n][half][3]);
             fma_pair(mids[n][G][0], mids[n][G][1], mid[0], s[n][half][0], s[n][half][1]);
             fma_pair(mids[n][G][0], mids[n][G][1], mid[1], s[n][half][2], s[n][half][3]);
+            float part[2][4];
 #pragma unroll
             for (int term = 0; term < TERMS; ++term) {
               const uint32_t b0 = transposed(next_term(w[0], w[1])), b1 = transposed(next_term(w[2], w[3]));
-              mma_bf16_16816(o[n][G][0], a0, b0, b1);
-              mma_bf16_16816(o[n][G][1], a1, b0, b1);
-              if (!kExact) mma_bf16_16816(ones[n][G], one, b0, b1);
+              if constexpr (kExact) {
+                // (sums of 16 rows of their own: the products' adder cuts bits off that a running sum of many rows would miss)
+                if (term == 0) {
+                  mma_first(part[0], a0, b0, b1);
+                  mma_first(part[1], a1, b0, b1);
+                } else {
+                  mma_bf16_16816(part[0], a0, b0, b1);
+                  mma_bf16_16816(part[1], a1, b0, b1);
+                }
+              } else {
+                mma_bf16_16816(o[n][G][0], a0, b0, b1);
+                mma_bf16_16816(o[n][G][1], a1, b0, b1);
+                mma_bf16_16816(ones[n][G], one, b0, b1);
+              }
+            }
+            if constexpr (kExact) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                o[n][G][0][j] += part[0][j];
+                o[n][G][1][j] += part[1][j];
+              }
             }
           }
         }
@@ -434,7 +514,7 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
 #pragma unroll
         for (int sh = 4; sh <= 16; sh *= 2) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], sh);
         if (gid == 0) {
-          sm[head] = m[n][e] * p.scale2;
+          sm[head] = m[n][e] * scale[n][e];
           sm[8 * NH + head] = l[n][e];
         }
 #pragma unroll
@@ -442,10 +522,9 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           float add = mids[n][G][e];
 #pragma unroll
           for (int sh = 4; sh <= 16; sh *= 2) add += __shfl_xor_sync(0xffffffffu, add, sh);
-          const float first = kExact ? add : fmaf(-135.5f, ones[n][G][e], add);
           if (!kExact) add = fmaf(-23.5f, ones[n][G][e], add);
           *reinterpret_cast<float4*>(so + head * OPITCH + 32 * G + 4 * gid) = make_float4(
-              o[n][G][0][e] + first, o[n][G][0][e + 2] + add, o[n][G][1][e] + add, o[n][G][1][e + 2] + add);
+              o[n][G][0][e] + add, o[n][G][0][e + 2] + add, o[n][G][1][e] + add, o[n][G][1][e + 2] + add);
         }
       }
     __syncthreads();
@@ -507,7 +586,7 @@ int run(DecodeParams p, const madakv_config& c, int splits, cudaStream_t st) {
   auto go = [&](auto groups, auto warps, auto track) {
     constexpr int W = decltype(warps)::value;
     auto kernel = decode_quant_kernel<T, D, decltype(groups)::value, W, decltype(track)::value>;
-    constexpr int bytes = QuantTile<D, W>::QUERIES + QuantTile<D, W>::query_bytes(sizeof(T) == 4 ? 3 : decltype(groups)::value);
+    constexpr int bytes = QuantTile<D, W>::QUERIES + QuantTile<D, W>::query_bytes(decltype(groups)::value, sizeof(T) == 4 ? 3 : 1);
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return (int)MADAKV_ECUDA;
     launch_pdl(kernel, dim3((unsigned)p.n_sel * p.slots), dim3(32 * W), bytes, st, p);
     return launch_status();
