@@ -10,6 +10,7 @@
 //            to dtype once. (A second kernel for it cost a launch on the host, 2.2 us, and 3-9 us on the GPU per call; a
 //            thread-block cluster per segment that merges through distributed shared memory left too few blocks
 //            resident: 248 us instead of 148 on 1024 segments of 1638 rows.)
+//   track    a call with tracking runs the same kernels with kTrack: they also store their logits, for accumulate_kernel behind them
 #include <mutex>
 #include <type_traits>
 

@@ -14,6 +14,8 @@
 // fp32: queries as three fp16 terms and weights as three bf16 terms, whose products are exact and whose sum is fp32 again; V's
 // operands are code - 7.5 then, so that no sum loses bits to the 23.5.
 // A warp has tiles of 32 rows of its own, read ahead into a ring in shared memory by asynchronous copies.
+// 1024 segments of 1638 rows, g = 1: 84 us, 0.50 of the copy bandwidth; 8 of 131071, g = 4: 51 us, 0.51. What binds is the pipe of
+// shifts, permutations and conversions, two clocks each (60 % busy), and with it the issue slots.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -34,7 +36,7 @@ struct QuantTile {
                        V_PAR = V_CODE + kTile * R::CODE_BYTES, STAGE = V_PAR + kTile * R::PAR_BYTES;
   static constexpr int WARP = kAhead * STAGE;
   static constexpr int FRESH = kWarps * WARP;  // the appended row: codes and parameters of K, then of V
-  static constexpr int QUERIES = FRESH + 2 * (R::CODE_BYTES + R::PAR_BYTES);  // operands of up to 16 heads in bf16 or 8 in fp32
+  static constexpr int QUERIES = FRESH + 2 * (R::CODE_BYTES + R::PAR_BYTES);
   static_assert(QUERIES % 16 == 0, "read in 16-byte pieces");
   // the queries of 8 NH heads: operands of every term, then [8 NH] scales and [8 NH][NG] sums
   static constexpr int query_bytes(int NH, int terms) { return NH * (R::NG * terms * 512 + 32 + 32 * R::NG); }
@@ -577,6 +579,9 @@ int run(DecodeParams p, const madakv_config& c, int splits, cudaStream_t st) {
   // 32 blocks of four warps for each of them 75)
   const bool big = p.n_sel <= 20 && p.n_sel * rows >= 148 * 768;
   const int blocks = big ? 148 : resident;
+  // otherwise as many blocks of four warps as are resident at once. Calls of more segments than that give each one block: finishing a
+  // segment that blocks share takes longer than the more even end saves (1024 segments of 1638 rows, g = 1: 84.8 us with one block,
+  // 91-94 where the longer ones have two, 101 at shares of 1024; 896 of 2512, g = 7 and tracking: 159, 154-158, 164)
   const int64_t want = 3 * rows / 256 + 1, most = blocks / p.n_sel < 1 ? 1 : blocks / p.n_sel < kDecodeSlots ? blocks / p.n_sel : kDecodeSlots;
   p.slots = (int)(want < most ? want : most);
   if (p.slots > splits) p.slots = splits;

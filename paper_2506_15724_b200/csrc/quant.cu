@@ -8,9 +8,12 @@
 //   - a code is one fused multiply-add: (x - mid) / step + 8 in units of 2^-16, rounded to a whole number by the constant it is added
 //     to. It is off by less than 0.6 units, so the bits above the 16th are the code unless the lower 16 are all zero: then x is on
 //     a border, and the bits are right, or just below one. bf16 numbers that are no smaller than step / 256 cannot be that near to a
-//     border without being on it (x, mid and step are multiples of step 2^-15), which spares most of them a closer look (every other
-//     warp has an element on a border); the others, and fp32, are decided by the exact products of step. Groups with elements outside the sixteen cells (a mid that is large
-//     beside step and was rounded), with extreme steps or without one go the exact way altogether.
+//     border without being on it (x, mid and step are multiples of 2^-15 of step's power of two), which spares most of them a closer
+//     look (every other warp has an element on a border); the others, and fp32, are decided by the exact products of step.
+//   - groups with elements outside the sixteen cells (a mid that is large beside step and was rounded), with extreme steps or without
+//     one go the exact way altogether
+// 1024 units of 1638 rows (d = 128, bf16) take 293 us, 0.6 of the copy bandwidth, bound by the instructions issued (282 without the
+// second look, 980 with a division in fp64 for every code); one layer of 4 units of 2048 rows 5.3 us.
 #include <type_traits>
 
 #include "quant.cuh"
@@ -254,7 +257,9 @@ __global__ void __launch_bounds__(NT, 4) compact_quant_kernel(const __grid_const
   }
 }
 
-constexpr int kExpandRows = 2;  // of K and of V that a thread has on their way
+// Rows of K and of V that a thread has on their way. Reading back writes most of its bytes: 1.7 M rows, d = 128, bf16, in 210 us, 0.83 of
+// the copy bandwidth (253 with one row and a block for every 16 rows).
+constexpr int kExpandRows = 2;
 
 struct ExpandParams {
   const int64_t* rows;
