@@ -288,7 +288,7 @@ int madakv_decode_attn_quant(const madakv_config* cfg, int32_t layer, const void
  *   scratch  [capacity, g] fp32, 16-byte aligned, overwritten (the step's logits); calls in flight at once need one each
  *   kept_idx [capacity] int32, position [B] int32: both null if positions are not kept up (eviction then may protect
  *            no recent rows); otherwise position[b] is the new token's position in sequence b
- *   decay    in [0, 1]; 1 sums all steps alike                                                                */
+ *   decay    in [0, 1]; 1 sums all steps alike, 0 keeps this step's weights alone, whatever acc held before                                                                */
 int madakv_decode_attn_track(const madakv_config* cfg, int32_t layer, const void* q, const void* k_new, const void* v_new,
                              void* k_c, void* v_c, const int64_t* seg_off, int32_t* kept_len, int64_t capacity, void* out,
                              float* lse_out, float* acc, float* scratch, int32_t* kept_idx, const int32_t* position,

@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(NT) accumulate_kernel(const __grid_constant__ 
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) {
       const int r = r0 + j * NT;
-      old[j] = r < len ? p.acc[off + r] : 0.f;
+      old[j] = r < len && p.decay > 0.f ? p.acc[off + r] : 0.f;  // (decay 0 forgets whatever was there)
 #pragma unroll
       for (int i = 0; i < G; ++i) s[j][i] = r < len && i < p.g ? p.scores[(off + r) * p.g + i] : 0.f;
     }

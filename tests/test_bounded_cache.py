@@ -286,6 +286,32 @@ def test_compact_quant_equals_the_formula(dtype, d, shape, lens):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_compact_quant_skips_what_selection_refused(d):
+    """A segment that would end behind the cache with its headroom, or whose positions lie outside the prompt, is not written."""
+    lens = [20, 30, 40]
+    cfg = config("bf16", 1, 3, 1, 1, d, 64, new=4)
+    cache = Cache(cfg, lens, quant=False)
+    k, v = (torch.randn((1, 3, 1, 64, d)).bfloat16().cuda() for _ in range(2))
+    cap = int(cache.off[-1]) - 1  # the last segment's headroom lacks a row
+    arrays = [torch.full((cap, d // 2), 77, dtype=torch.uint8, device="cuda"), torch.full((cap, d // 32, 2), 5.0, dtype=torch.bfloat16, device="cuda")]
+    arrays = [a.clone() for a in arrays * 2]
+    cache.kept_idx[3], cache.kept_idx[4] = 64, -1
+    mk.madakv_compact_quant(cfg, k, v, cache.kept_idx, cache.seg_off, cache.kept_len, *arrays, cache.ws)
+    idx = cache.kept_idx.cpu().numpy()
+    for u in range(2):
+        a = int(cache.off[u])
+        rows = np.array([i for i in range(a, a + lens[u]) if 0 <= idx[i] < 64])
+        for src, code, par in ((k, *arrays[:2]), (v, *arrays[2:])):
+            want, want_par = quantise(src[0, u, 0].double().cpu().numpy()[idx[rows]])
+            assert np.array_equal(nibbles(code.cpu().numpy()[rows], d), want)
+            assert np.array_equal(par.double().cpu().numpy()[rows], want_par)
+    for code, par in (arrays[:2], arrays[2:]):
+        for rows in (slice(3, 5), slice(20, 24), slice(int(cache.off[2]) - 4, cap)):
+            assert (code[rows] == 77).all() and (par[rows] == 5.0).all()
+
+
+@pytest.mark.gpu
 def test_quantised_values_are_within_half_a_step():
     cfg = config("f32", n=2000, Hq=1, Hkv=1)
     cache = Cache(cfg, [2000])
@@ -376,13 +402,10 @@ def check_step(cache, dtype, step, layer, before, out, lse, kn, vn, q, track, de
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("quant", [True, False])
-@pytest.mark.parametrize("track", [False, True])
+@pytest.mark.parametrize("quant,track", [(True, False), (True, True), (False, True)])
 @pytest.mark.parametrize("dtype,d,g,units,lens", ATTEND)
-def test_decode_steps_equal_the_formula(dtype, d, g, units, lens, track, quant):
+def test_decode_steps_equal_the_formula(dtype, d, g, units, lens, quant, track):
     """Two appending steps and one without, on one workspace; then one layer alone."""
-    if not (quant or track):
-        pytest.skip("the call that was there before has its own tests")
     B, L = (1, units) if units % 2 else (2, units // 2)
     cfg = config(dtype, B, L, g, 1, d, max(lens) + 1, new=3)
     cache = Cache(cfg, lens, seed=g, quant=quant, extra=5)
@@ -391,8 +414,6 @@ def test_decode_steps_equal_the_formula(dtype, d, g, units, lens, track, quant):
     for step, (append, layer, decay) in enumerate([(True, -1, 1.0), (True, -1, 0.75), (False, -1, 0.0), (True, L - 1, 0.5)]):
         q, kn, vn = cache.step(step, append)
         before = (cache.kept_len.cpu().numpy(), cache.acc.cpu().numpy(), cache.kept_idx.cpu().numpy(), [a.clone() for a in cache.arrays])
-        if not track:
-            before = (before[0], before[1], before[2], before[3])
         out, lse = cache.decode(q, kn, vn, layer, cache.tracking(pos, decay) if track else ())
         assert mk.madakv_poll_status(cache.ws) == 0
         check_step(cache, dtype, step, layer, before, out, lse, kn, vn, q, track, decay, position)
@@ -412,6 +433,51 @@ def test_decode_on_few_long_and_on_very_many_segments(dtype, d, g, units, lens, 
     out, lse = cache.decode(q, kn, vn, -1, cache.tracking(pos, 0.25) if track else ())
     assert mk.madakv_poll_status(cache.ws) == 0
     check_step(cache, dtype, 7, -1, before, out, lse, kn, vn, q, track, 0.25, [123456])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [True, False])
+def test_without_decay_old_sums_do_not_matter(quant):
+    lens = [700, 0, 33]
+    cfg = config("bf16", 1, 3, 2, 1, 128, 1024)
+    a, b = Cache(cfg, lens, quant=quant), Cache(cfg, lens, quant=quant)
+    b.acc.fill_(float("nan"))
+    for c in (a, b):
+        c.decode(*c.step(0), track=(c.acc, c.scratch, None, None, 0.0))
+    for at, n in zip(a.off, lens):
+        assert torch.equal(a.acc[at:at + n + 1], b.acc[at:at + n + 1]) and not a.acc[at:at + n + 1].isnan().any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [True, False])
+def test_calls_on_two_streams_at_once(quant):
+    """Two caches with workspaces and scratch of their own, steps and evictions in flight together: the results of each alone."""
+    cfg = config("bf16", 1, 16, 4, 1, 128, 4096, new=8)
+    rng = np.random.RandomState(3)
+    lens = [rng.randint(1, 4000, size=16), rng.randint(1, 300, size=16)]
+    limit = [torch.from_numpy((n // 2).astype(np.int32)).cuda() for n in lens]
+    call = mk.madakv_evict_quant if quant else mk.madakv_evict
+    pos = torch.tensor([5000], dtype=torch.int32, device="cuda")
+    results = []
+    for together in (False, True):
+        caches = [Cache(cfg, n, seed=i, quant=quant) for i, n in enumerate(lens)]
+        steps = [[tuple(t.cuda() for t in c.step(s)) for s in range(6)] for c in caches]
+        outs = [[torch.zeros(c.shape, dtype=torch.bfloat16, device="cuda") for _ in range(6)] for c in caches]
+        lses = [[torch.zeros(c.shape[:3], device="cuda") for _ in range(6)] for c in caches]
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()] if together else [torch.cuda.current_stream()] * 2
+        torch.cuda.synchronize()
+        for s in range(6):
+            for i, c in enumerate(caches):
+                with torch.cuda.stream(streams[i]):
+                    c.decode(*steps[i][s], track=c.tracking(pos, 0.9), out=outs[i][s], lse=lses[i][s])
+                    if s % 3 == 2:
+                        call(cfg, -1, limit[i], 2, c.acc, c.kept_idx, c.seg_off, c.kept_len, *c.arrays, c.ws)
+        torch.cuda.synchronize()
+        for c in caches:
+            assert mk.madakv_poll_status(c.ws) == 0
+        results.append([t for i, c in enumerate(caches) for t in (*outs[i], *lses[i], c.kept_len, c.kept_idx, c.acc, *c.arrays)])
+    for x, y in zip(*results):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
 @pytest.mark.gpu
