@@ -12,8 +12,9 @@
 //     look (every other warp has an element on a border); the others, and fp32, are decided by the exact products of step.
 //   - groups with elements outside the sixteen cells (a mid that is large beside step and was rounded), with extreme steps or without
 //     one go the exact way altogether
-// 1024 units of 1638 rows (d = 128, bf16) take 293 us, 0.6 of the copy bandwidth, bound by the instructions issued (282 without the
-// second look, 980 with a division in fp64 for every code); one layer of 4 units of 2048 rows 5.3 us.
+// 1024 units of 1638 rows (d = 128, bf16) take 273 us, 0.64 of the copy bandwidth, bound by the instructions issued (980 with a division
+// in fp64 for every code; 238 without looking for elements near borders; 294 with their magnitudes compared as pairs of 16 bits); one
+// layer of 4 units of 2048 rows 4.9 us.
 #include <type_traits>
 
 #include "quant.cuh"
@@ -38,12 +39,6 @@ struct CompactQuantParams {
   int L, Hkv, n_max, headroom, blocks;             // blocks per unit
 };
 
-__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
 template <typename T>
 struct Lane16;
 template <>
@@ -67,7 +62,7 @@ struct Lane16<float> {
   __device__ static float low(Extremes e) { return e.x; }
   __device__ static float high(Extremes e) { return e.y; }
   __device__ static uint32_t par(float lo, float hi) { return group_par(lo, hi); }
-  __device__ static bool may_touch(const uint4&, uint32_t) { return true; }
+  __device__ static bool may_touch(const float (&)[4], float, float) { return true; }
 };
 template <>
 struct Lane16<__nv_bfloat16> {
@@ -102,11 +97,12 @@ struct Lane16<__nv_bfloat16> {
     const uint32_t w = *reinterpret_cast<const uint32_t*>(&r);
     return isfinite(bf16_lo(w)) && isfinite(bf16_hi(w)) ? w : 0x7fc07fc0u;
   }
-  // Whether an element (or mid, unless it is 0) is smaller than step / 256. (Magnitudes compare as their bits.)
-  __device__ static bool may_touch(const uint4& v, uint32_t par) {
-    const uint32_t m = min_u16x2(min_u16x2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), min_u16x2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-    const uint32_t below = (par & 0xffffu) - 0x400u, mid = (par >> 16) & 0x7fffu;
-    return min(m & 0xffffu, m >> 16) < below || (mid < below && mid != 0u);
+  // Whether an element (or mid, unless it is 0) is smaller than step / 256.
+  __device__ static bool may_touch(const float (&x)[8], float step, float mid) {
+    float m = mid == 0.f ? step : fabsf(mid);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fminf(m, fabsf(x[e]));
+    return m < step * (1.f / 256.f);
   }
 };
 
@@ -126,14 +122,14 @@ __device__ __forceinline__ float units_per(uint32_t par, float lo, float hi) {
 template <typename T>
 __device__ __forceinline__ uint32_t codes_of(const uint4& raw, uint32_t par, float units, bool& unsure) {
   constexpr int N = Lane16<T>::N;
-  const float mid = bf16_hi(par);
+  const float step = bf16_lo(par), mid = bf16_hi(par);
   float x[N];
   Lane16<T>::values(raw, x);
   uint32_t t[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) t[e] = __float_as_uint(fmaf(x[e] - mid, units, 8.f * kUnit + kWhole));
   unsure = !(units == units);
-  if (Lane16<T>::may_touch(raw, par)) {
+  if (Lane16<T>::may_touch(x, step, mid)) {
     uint32_t least = t[0] & 0xffffu;
 #pragma unroll
     for (int e = 1; e < N; ++e) least = min(least, t[e] & 0xffffu);
@@ -369,7 +365,7 @@ int launch_compact_quant(const madakv_config& c, const void* k, const void* v, m
   p.n_max = c.max_seq_len;
   p.headroom = c.max_new_tokens;
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, rows = capacity / units + 1;
-  // rows of a block: as many as leave 16 blocks for every SM, 32 to 256 (1024 units of 1638 rows, 32 / 64 / 256 / 512 rows a block: 370 / 330 / 300 / 302 us; 4 of
+  // rows of a block: as many as leave 16 blocks for every SM, 32 to 256 (1024 units of 1638 rows, 32 / 64 / 256 / 512 rows a block, in an earlier state: 370 / 330 / 300 / 302 us; 4 of
   // 2048 rows: 5.9 / 7.0 / 14.4 with 32 / 64 / 256)
   const int64_t share = capacity / (148 * 16) / 32 * 32, per_block = share < 32 ? 32 : share > 256 ? 256 : share;
   const int64_t want = (rows + per_block - 1) / per_block, most = ((1 << 20) + units - 1) / units;
