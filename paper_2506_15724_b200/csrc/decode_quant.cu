@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
       cp_async_wait<kAhead - 1>();
       __syncwarp();
       unsigned char* st = ring + it % kAhead * QT::STAGE;
-      if (view.new_row >= r && view.new_row < r + kTile) {
+      if (owner && view.new_row >= r && view.new_row < r + kTile) {  // (a tile of the block before may reach behind its share, as far as this row)
         const int row = view.new_row - r;
         const uint32_t* fresh = reinterpret_cast<const uint32_t*>(dsmem + QT::FRESH);
         constexpr int CW = R::CODE_BYTES / 4;
