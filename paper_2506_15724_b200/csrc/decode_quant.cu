@@ -419,8 +419,10 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          const float mn = fmaxf(m[n][e], mx), base = mn == -INFINITY ? 0.f : mn * scale[n][e];
-          f[e] = fast_ex2(fmaf(m[n][e], scale[n][e], -base));
+          // m is the largest logit as the weights' exponents see it, scaled and rounded: while it stays, the factor of the sums is exactly 1
+          // (against the product before its rounding it would be off by up to half a step of m in every tile, always the same way)
+          const float mn = fmaxf(m[n][e], mx * scale[n][e]), base = mn == -INFINITY ? 0.f : mn;
+          f[e] = fast_ex2(m[n][e] - base);
           m[n][e] = mn;
           float sum = 0.f;
 #pragma unroll
@@ -516,7 +518,7 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
 #pragma unroll
         for (int sh = 4; sh <= 16; sh *= 2) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], sh);
         if (gid == 0) {
-          sm[head] = m[n][e] * scale[n][e];
+          sm[head] = m[n][e];
           sm[8 * NH + head] = l[n][e];
         }
 #pragma unroll

@@ -38,6 +38,62 @@ def check_attention(dtype, q, k, v, spread, scale, out, lse, least=0.0):
     return w
 
 
+# ------------------------------------------------------------------------------------------------- sums over many tiles
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,g,units", [("f32", 1, 450), ("bf16", 1, 450), ("bf16", 9, 300)])
+def test_sums_do_not_drift_while_the_maximum_stays(dtype, g, units):
+    """One block per segment, 47 tiles for each of its warps, logits of 38 to 96 that differ by little: the sums of a tile count the same however
+    many tiles come after it. All logits are exact (queries of 1, few bits in K), so what is off is what the softmax rounds.
+
+    In units of 2^-24, the half step of fp32, relative unless said otherwise; Z is the largest logit in the log2 domain:
+      a sum l of weights: 4 additions in each of 47 tiles at most, the factors of a new maximum, 3 exchanges, 4 warps: 210; ex2.approx is
+        right to 2^-22: 4 for the weight and 4 for each of up to 16 new maxima; its argument, up to 8, is rounded once: 8 ln 2
+      lse = (base + log2 l) ln 2, absolute: log2f (up to 13) 32, the sum, the product and ln 2 itself 3 Z ln 2; the scale in the log2 domain (log2 e,
+        its product with the softmax scale) 2 Z ln 2
+      acc = exp2(logit - lse2): both rounded, 2 Z ln 2; exp2f 4; the scale's error on differences of up to 5: 10
+      out: numerator and denominator, and in fp32 the products' sums of 16 rows, cut and not rounded, in three terms: 32; in bf16 the weights' and
+        the result's rounding"""
+    d, rows, scale = 64, 6000, 0.3
+    gen = torch.Generator(device="cuda").manual_seed(units)
+    cfg = mk.make_config(DT[dtype], 1, units, g, 1, d, rows, 8, softmax_scale=scale)
+    mid = (2 + 3 * torch.arange(units, device="cuda") / units).bfloat16()
+    code = torch.randint(0, 16, (units, rows, d), generator=gen, device="cuda", dtype=torch.uint8)
+    code[:, 0] = 15  # the largest logit, in the first tile
+    k_code = packed(code.view(-1, d))
+    k_par = torch.empty((units, rows, 2, 2), dtype=torch.bfloat16, device="cuda")
+    k_par[..., 0], k_par[..., 1] = 2.0 ** -6, mid.view(-1, 1, 1)
+    v_code = torch.full((units, rows, d // 2), 0xff, dtype=torch.uint8, device="cuda")
+    v_code[:, rows // 2:] = 0  # 1.875 in the first half of the rows, -1.875 in the second
+    v_par = torch.zeros((units, rows, 2, 2), dtype=torch.bfloat16, device="cuda")
+    v_par[..., 0] = 0.25
+    cache = [k_code, k_par.view(-1, 2, 2), v_code.view(-1, d // 2), v_par.view(-1, 2, 2)]
+    seg_off = torch.arange(units + 1, device="cuda") * rows
+    kept_len = torch.full((units,), rows, dtype=torch.int32, device="cuda")
+    q = torch.ones((1, units, g, d), dtype=DT[dtype], device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((1, units, g), device="cuda")
+    acc, scratch = torch.zeros(units * rows, device="cuda"), torch.empty((units * rows, g), device="cuda")
+    ws = mk.new_workspace(cfg)
+    mk.madakv_decode_attn_quant(cfg, -1, q, None, None, *cache, seg_off, kept_len, out, lse, ws, acc, scratch)
+    assert mk.madakv_poll_status(ws) == 0
+
+    logit = np.float64(np.float32(scale)) * (d * mid.double().view(-1, 1) + 2.0 ** -6 * (code.sum(2, dtype=torch.int64).double() - 7.5 * d))
+    want_lse = torch.logsumexp(logit, 1, keepdim=True)
+    w = torch.exp(logit - want_lse)
+    half, ln2 = 2.0 ** -24, math.log(2)
+    z = logit.amax(1, keepdim=True) / ln2
+    l_off = (210 + 4 + 64 + 8 * ln2) * half
+    off = (lse.view(units, g).double() - want_lse).abs() / (l_off + (32 + 5 * z * ln2) * half)
+    assert float(off.max()) <= 1, float(off.max())
+    off = (acc.view(units, rows).double() - g * w).abs() / (g * w * (l_off + (2 * z * ln2 + 32 + 14 + g) * half))
+    assert float(off.max()) <= 1, float(off.max())
+    want = 1.875 * (w[:, :rows // 2].sum(1) - w[:, rows // 2:].sum(1)).view(units, 1, 1)
+    most = 1.875 * (2 * l_off + 42 * half)
+    if dtype == "bf16":
+        most = most + HALF[dtype] * (1.875 + want.abs())
+    off = (out.view(units, g, d).double() - want).abs() / most
+    assert float(off.max()) <= 1, float(off.max())
+
+
 # ------------------------------------------------------------------------------------------------- ends of blocks
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
