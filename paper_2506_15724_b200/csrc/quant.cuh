@@ -40,10 +40,16 @@ __device__ __forceinline__ uint32_t group_par(float lo, float hi) {
   return isfinite(bf16_lo(w)) && isfinite(bf16_hi(w)) ? w : 0x7fc07fc0u;
 }
 
+// floor((x - mid) / step) + 8 to the last bit. The quotient in 64 bits is never below a whole number that the true one reaches, but may have been
+// rounded up to one, and so may the difference. The multiple of step that it claims is exact (a few bits times eight), and so is d + rest = x - mid:
+// neither d nor the multiple lies within `rest`, half a last bit of d, of the other one without being equal to it.
 __device__ __forceinline__ uint32_t code_of(float x, float step, float mid) {
   if (!(step > 0.f)) return 8u;
-  const double t = floor(((double)x - (double)mid) / (double)step) + 8.0;
-  return (uint32_t)fmin(fmax(t, 0.0), 15.0);
+  const double d = __dsub_rn(x, mid), y = __dsub_rn(d, x), rest = __dadd_rn(__dsub_rn(x, __dsub_rn(d, y)), __dsub_rn(-(double)mid, y));
+  double t = floor(d / (double)step);
+  const double border = t * (double)step;
+  if (d < border || (d == border && rest < 0.0)) t -= 1.0;
+  return (uint32_t)fmin(fmax(t + 8.0, 0.0), 15.0);
 }
 
 // The codes of a lane's four elements and its group's (step, mid); all lanes of the row take part.

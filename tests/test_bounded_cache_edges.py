@@ -127,3 +127,59 @@ def test_appended_row_just_behind_a_share(dtype, d, units, longest, lens):
         for a, row in zip(cache.arrays, before):
             a[first + n] = row
     assert mk.madakv_poll_status(cache.ws) == 0 and not bad, bad
+
+
+# ------------------------------------------------------------------------------------------------- borders
+def border_groups(dtype):
+    """Groups [n, 32] whose (step, mid) are a power of two and a multiple of it, with elements on the borders, next to them, and next to 0, which
+    is a border: as near as the type goes."""
+    groups, pars = [], []
+    for e in (-3, 20, 110, -110, -60):
+        step = 2.0 ** e
+        for j in range(-7, 8):
+            x = [(j - 7.5) * step, (j + 7.5) * step]
+            for tiny in (2.0 ** (e - 20), 2.0 ** (e - 34), 2.0 ** (e - 60), 2.0 ** max(e - 100, -126), 2.0 ** -126):
+                x += [tiny, -tiny] if 2.0 ** -126 <= tiny < step else []
+            x += [0.0, -0.0, 2.0 ** -133, -2.0 ** -133]
+            near = torch.tensor([(j + i) * step for i in (-6, -3, -1, 1, 2, 5)]).to(DT[dtype])
+            for way in (math.inf, -math.inf):
+                x += torch.nextafter(near, torch.full_like(near, way)).double().tolist()
+            x = torch.tensor((x + [j * step] * 32)[:32], dtype=torch.float64)
+            groups.append(x.to(DT[dtype]))
+            assert torch.equal(groups[-1].double(), x.to(torch.float32).double())  # nothing of them was rounded
+            pars.append((step, j * step))
+    return torch.stack(groups), pars
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_elements_next_to_a_border_get_the_code_of_the_formula(dtype, d):
+    """floor((x - mid) / step) in rational numbers, for compacted rows and for appended ones."""
+    groups, pars = border_groups(dtype)
+    rows = groups.view(-1, d) if len(groups) * 32 % d == 0 else torch.cat((groups, groups[:1].expand(-len(groups) % (d // 32), 32))).view(-1, d)
+    pars += pars[:1] * (rows.numel() // 32 - len(pars))
+    want = np.array([[min(15, max(0, math.floor((Fraction(x) - Fraction(m)) / Fraction(s)) + 8)) for x in g]
+                     for g, (s, m) in zip(rows.view(-1, 32).double().tolist(), pars)]).reshape(rows.shape)
+    n = len(rows)
+    par = np.array(pars).reshape(n, d // 32, 2)
+    k, v = rows, rows.flip(0)
+    # compacted
+    cfg = config(dtype, 1, 1, 1, 1, d, n, new=1)
+    cache = Cache(cfg, [n])
+    cache.kept_idx[:n] = torch.arange(n, dtype=torch.int32, device="cuda")
+    for a in cache.arrays:
+        a.zero_()
+    mk.madakv_compact_quant(cfg, k.view(1, 1, 1, n, d).cuda(), v.contiguous().view(1, 1, 1, n, d).cuda(), cache.kept_idx, cache.seg_off,
+                            cache.kept_len, *cache.arrays, cache.ws)
+    # appended, one to each of n segments
+    cfg = config(dtype, 1, n, 1, 1, d, 4, new=1)
+    grown = Cache(cfg, [2] * n)
+    grown.decode(grown.step(0)[0], k.reshape(1, n, 1, d), v.reshape(1, n, 1, d))
+    at = torch.arange(n, device="cuda") * 3 + 2
+    for c, where in ((cache, torch.arange(n, device="cuda")), (grown, at)):
+        assert mk.madakv_poll_status(c.ws) == 0
+        for i, (code, p) in ((0, (want, par)), (2, (want[::-1], par[::-1]))):
+            assert np.array_equal(c.arrays[i + 1][where].double().cpu().numpy(), p)
+            got = nibbles(c.arrays[i][where].cpu().numpy(), d)
+            assert np.array_equal(got, code), np.argwhere(got != code)[:5]
