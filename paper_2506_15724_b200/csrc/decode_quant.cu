@@ -270,8 +270,11 @@ __global__ void __launch_bounds__(32 * kWarps, kWarps > 4 ? 1 : NH == 1 ? 3 : 2)
         }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // the head's largest element comes to [2^14, 2^15), where fp16 holds what is 2^-29 of it or more; an infinity makes the head NaN
-        const int k = min(60, 14 - ((int)(__float_as_uint(top) >> 23) - 127));
+        // the head's largest element comes to [2^14, 2^15), where fp16 holds what is 2^-29 of it or more, unless that would take the scale that
+        // undoes it below fp32's normal numbers (queries below 2^-108 at the usual scale; a scale of 0 would make NaN of the rows behind
+        // a share); an infinity makes the head NaN
+        const int room = min(126, max(1, (int)(__float_as_uint(p.scale2) >> 23)) - 1);
+        const int k = min(room, 14 - ((int)(__float_as_uint(top) >> 23) - 127));
         const float up = __uint_as_float((uint32_t)(k + 127) << 23);
         float sum = 0.f;
 #pragma unroll

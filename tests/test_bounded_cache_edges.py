@@ -183,3 +183,53 @@ def test_elements_next_to_a_border_get_the_code_of_the_formula(dtype, d):
             assert np.array_equal(c.arrays[i + 1][where].double().cpu().numpy(), p)
             got = nibbles(c.arrays[i][where].cpu().numpy(), d)
             assert np.array_equal(got, code), np.argwhere(got != code)[:5]
+
+
+# ------------------------------------------------------------------------------------------------- queries and scales
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q_exp,k_exp,v_exp", [(0, 0, 0), (-60, 60, 0), (-80, 78, 0), (-96, 97, 97), (60, -60, -60), (90, -90, 97), (3, -3, -120)])
+def test_queries_keys_and_values_far_from_one(dtype, d, q_exp, k_exp, v_exp):
+    """The same numbers times powers of two: as right as without, up to 2^100 in the cache."""
+    lens = [40, 1, 700, 129]
+    cfg = config(dtype, 1, 2, 6, 2, d, 1024)
+    cache = Cache(cfg, lens)
+    for i, e in ((1, k_exp), (3, v_exp)):
+        cache.arrays[i].mul_(2.0 ** e)
+    q, _, _ = cache.step(0, False)
+    q = q * 2.0 ** q_exp
+    out, lse = cache.decode(q, None, None, track=(cache.acc, cache.scratch))
+    k, v, spread = cache.contents()
+    assert np.abs(k).max() < 2.0 ** 100 and np.abs(v).max() < 2.0 ** 100
+    qs, out, lse = (t.double().cpu().numpy().reshape(4, 3, -1) for t in (q, out, lse))
+    for u, n in enumerate(lens):
+        a = int(cache.off[u])
+        # weights times step are made of bf16 numbers, whose least is 2^-133: the last one is off by up to 2^-134, under 7.5 at most
+        check_attention(dtype, qs[u], k[a:a + n], v[a:a + n], spread[a:a + n], d ** -0.5, out[u], lse[u, :, 0], least=n * 2.0 ** -131)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [0.02, 1.0, 3.5, 1e-30, 1e-37, 1e-42])
+def test_softmax_scale(dtype, d, scale):
+    """Scales other than 1 / sqrt(d), several KV heads, appended rows and tracking; the smallest make all weights alike."""
+    lens = [40, 0, 700, 129, 33, 2000]
+    cfg = config(dtype, 1, 2, 15, 3, d, 2048, softmax_scale=scale)
+    cache = Cache(cfg, lens)
+    q, kn, vn = cache.step(0)
+    acc = cache.acc.double().cpu().numpy()
+    out, lse = cache.decode(q, kn, vn, track=(cache.acc, cache.scratch))
+    assert mk.madakv_poll_status(cache.ws) == 0
+    k, v, spread = cache.contents()
+    qs, out, lse = (t.double().cpu().numpy().reshape(6, 5, -1) for t in (q, out, lse))
+    scale = float(np.float32(scale))
+    for u, n in enumerate(lens):
+        a, n = int(cache.off[u]), n + 1
+        w = check_attention(dtype, qs[u], k[a:a + n], v[a:a + n], spread[a:a + n], scale, out[u], lse[u, :, 0])
+        old = acc[a:a + n].copy()
+        old[-1] = 0.0
+        want = old + w.sum(0)
+        logit = 2 * ((d + 8) * 2.0 ** -24 * (np.abs(qs[u]) @ np.abs(k[a:a + n]).T).max() * scale + 2.0 ** -20)
+        assert np.all(np.abs(cache.acc[a:a + n].double().cpu().numpy() - want) <= logit * w.sum(0) + 7 * 2.0 ** -24 * want + 1e-38)  # (weights below 2^-126 are 0)
