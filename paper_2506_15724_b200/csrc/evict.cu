@@ -280,7 +280,8 @@ int launch_evict(const madakv_config& c, int layer, const int32_t* limit, int re
   bool wide = true;
   for (const RowArray& r : rows) wide = wide && r.bytes % 16 == 0;
   auto go = [&](auto kernel, int threads) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return (int)MADAKV_ECUDA;
+    // (the kernel's bound belongs to the process, and calls of other configs may come from other threads: the same for all)
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRows / 8) != cudaSuccess) return (int)MADAKV_ECUDA;
     launch_pdl(kernel, dim3((unsigned)n_sel), dim3(threads), smem, st, p);
     return launch_status();
   };

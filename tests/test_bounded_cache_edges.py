@@ -233,3 +233,36 @@ def test_softmax_scale(dtype, d, scale):
         want = old + w.sum(0)
         logit = 2 * ((d + 8) * 2.0 ** -24 * (np.abs(qs[u]) @ np.abs(k[a:a + n]).T).max() * scale + 2.0 ** -20)
         assert np.all(np.abs(cache.acc[a:a + n].double().cpu().numpy() - want) <= logit * w.sum(0) + 7 * 2.0 ** -24 * want + 1e-38)  # (weights below 2^-126 are 0)
+
+
+# ------------------------------------------------------------------------------------------------- host side
+@pytest.mark.gpu
+def test_evictions_of_two_configs_from_two_threads():
+    """A call on a long config needs more shared memory than one on a short one; neither may take away what the other has asked for."""
+    work = []
+    for n in (5000, 1 << 20):
+        cfg = mk.make_config(torch.bfloat16, 1, 1, 1, 1, 64, n, 8, max_new_tokens=8)
+        t = dict(dtype=torch.bfloat16, device="cuda")
+        cap = n + 8
+        work.append((cfg, torch.tensor([n], dtype=torch.int32, device="cuda"), torch.zeros(cap, device="cuda"),
+                     torch.zeros(cap, dtype=torch.int32, device="cuda"), torch.tensor([0, cap], device="cuda"),
+                     torch.tensor([100], dtype=torch.int32, device="cuda"), torch.zeros((cap, 64), **t), torch.zeros((cap, 64), **t),
+                     mk.new_workspace(cfg)))
+    torch.cuda.synchronize()
+    errors = []
+
+    def calls(cfg, limit, acc, idx, seg_off, kept_len, k, v, ws):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20000):
+                try:
+                    mk.madakv_evict(cfg, -1, limit, 0, acc, idx, seg_off, kept_len, k, v, ws)
+                except mk.MadakvError as e:
+                    errors.append(e.code)
+
+    threads = [threading.Thread(target=calls, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, (len(errors), set(errors))
