@@ -58,6 +58,7 @@ struct Args {
   int32_t integer() {
     const long v = PyLong_AsLong(next());
     if (v == -1 && PyErr_Occurred()) throw python_error();
+    if (v != (int32_t)v) fail(PyExc_OverflowError, "expected an integer of 32 bits");
     return (int32_t)v;
   }
 };

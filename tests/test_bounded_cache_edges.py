@@ -266,3 +266,14 @@ def test_evictions_of_two_configs_from_two_threads():
         t.join()
     torch.cuda.synchronize()
     assert not errors, (len(errors), set(errors))
+
+
+@pytest.mark.gpu
+def test_integers_beyond_32_bits_are_refused():
+    cfg = config("bf16", 1, 1, 1, 1, 64, 64)
+    cache = Cache(cfg, [40])
+    limit = torch.tensor([10], dtype=torch.int32, device="cuda")
+    for layer, recent in ((-1, 1 << 32), (-1, (1 << 31)), (1 << 32, 0), (-1 - (1 << 32), 0)):
+        with pytest.raises(OverflowError):
+            mk.madakv_evict_quant(cfg, layer, limit, recent, cache.acc, cache.kept_idx, cache.seg_off, cache.kept_len, *cache.arrays, cache.ws)
+    assert cache.kept_len.tolist() == [40]
