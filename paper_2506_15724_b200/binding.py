@@ -317,5 +317,7 @@ class EvictionBuffers:
 
     def run_trim(self, limit, recent=0, layer=-1):
         """Segments longer than limit [B, L, H_kv] int32 lose their rows of the smallest accumulated weight; needs track."""
+        if not self.track:
+            raise ValueError("run_trim: buffers without track=True accumulate no weights")
         call = madakv_evict_quant if self.quant else madakv_evict
         call(self.cfg, layer, limit, recent, self.acc, self.kept_idx, self.seg_off, self.kept_len, *self.cache, self.ws)

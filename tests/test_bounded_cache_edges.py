@@ -277,3 +277,11 @@ def test_integers_beyond_32_bits_are_refused():
         with pytest.raises(OverflowError):
             mk.madakv_evict_quant(cfg, layer, limit, recent, cache.acc, cache.kept_idx, cache.seg_off, cache.kept_len, *cache.arrays, cache.ws)
     assert cache.kept_len.tolist() == [40]
+
+
+def test_trim_without_tracking_is_refused():
+    cfg = config("bf16", 1, 1, 1, 1, 64, 64)
+    for quant in (False, True):
+        buf = mk.EvictionBuffers(cfg, 80, device="cpu", quant=quant)
+        with pytest.raises(ValueError):
+            buf.run_trim(torch.tensor([10], dtype=torch.int32))
