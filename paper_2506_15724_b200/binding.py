@@ -268,6 +268,9 @@ class EvictionBuffers:
         dt = torch.float32 if cfg.dtype == MADAKV_F32 else torch.bfloat16
         z = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
         self.cfg, self.quant, self.track = cfg, quant, track
+        # kept_idx holds the position of every row of the segments. (To be set by who fills it in other ways than run_eviction, a replayed
+        # graph of it included, after steps without positions.)
+        self.placed = True
         self.ws = new_workspace(cfg, device)
         self.psi = z((B, L, Hkv, n), torch.float32)
         self.lse = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
@@ -302,11 +305,13 @@ class EvictionBuffers:
         madakv_select(c, self.psi, mask, seq_len, self.budgets, self.kept_len, self.seg_off, self.kept_idx, self.ws)
         compact = madakv_compact_quant if self.quant else madakv_compact
         compact(c, k, v, self.kept_idx, self.seg_off, self.kept_len, *self.cache, self.ws)
+        self.placed = True
         if self.track:
             self.acc.zero_()
 
     def run_decode(self, q, k_new=None, v_new=None, layer=-1, position=None, decay=1.0):
-        """One decode step. With tracking, position [B] int32 says where the new tokens stand (None: kept_idx is not kept up)."""
+        """One decode step. With tracking, position [B] int32 says where the new tokens stand. None: kept_idx is not kept up, and run_trim
+        can protect no recent rows until the next run_eviction. Without tracking position and decay are not used."""
         head = (self.cfg, layer, q, k_new, v_new, *self.cache, self.seg_off, self.kept_len, self.out, self.lse_dec, self.ws)
         if not (self.quant or self.track):
             return madakv_decode_attn(*head)
@@ -314,10 +319,16 @@ class EvictionBuffers:
         if self.track:
             tracked = (self.acc, self.scratch, self.kept_idx if position is not None else None, position, decay)
         (madakv_decode_attn_quant if self.quant else madakv_decode_attn_track)(*head, *tracked)
+        if k_new is not None and position is None:
+            self.placed = False
 
     def run_trim(self, limit, recent=0, layer=-1):
-        """Segments longer than limit [B, L, H_kv] int32 lose their rows of the smallest accumulated weight; needs track."""
+        """Segments longer than limit [B, L, H_kv] int32 lose their rows of the smallest accumulated weight; needs track. With recent > 0 the
+        rows of the newest `recent` positions stay whatever the limit is: a segment keeps up to max(limit, recent) rows, so its headroom
+        has to hold max(0, recent - limit) rows and those of the steps until the next trim."""
         if not self.track:
             raise ValueError("run_trim: buffers without track=True accumulate no weights")
+        if recent and not self.placed:
+            raise ValueError("run_trim: recent rows cannot be told where run_decode was given no position")
         call = madakv_evict_quant if self.quant else madakv_evict
         call(self.cfg, layer, limit, recent, self.acc, self.kept_idx, self.seg_off, self.kept_len, *self.cache, self.ws)

@@ -285,3 +285,30 @@ def test_trim_without_tracking_is_refused():
         buf = mk.EvictionBuffers(cfg, 80, device="cpu", quant=quant)
         with pytest.raises(ValueError):
             buf.run_trim(torch.tensor([10], dtype=torch.int32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+def test_trim_protects_no_rows_whose_positions_were_not_given(quant):
+    cfg = config("bf16", 1, 1, 2, 2, 64, 200, new=6)
+    buf = mk.EvictionBuffers(cfg, 2 * 206, quant=quant, track=True)
+    given = prompt(cfg, 2)
+    buf.run_eviction(*given)
+    limit = buf.kept_len.clone()
+    gen = torch.Generator().manual_seed(0)
+    q, kn, vn = (torch.randn((1, 1, 2, 64), generator=gen).bfloat16().cuda() for _ in range(3))
+    position = torch.tensor([200], dtype=torch.int32, device="cuda")
+    buf.run_decode(q, kn, vn, position=position)
+    buf.run_decode(q)  # (appends nothing)
+    buf.run_trim(limit, recent=1)
+    assert torch.equal(buf.kept_len, limit)
+    buf.run_decode(q, kn, vn)
+    with pytest.raises(ValueError):
+        buf.run_trim(limit, recent=1)
+    assert torch.equal(buf.kept_len, limit + 1)
+    buf.run_trim(limit)
+    assert torch.equal(buf.kept_len, limit)
+    buf.run_eviction(*given)  # positions are known again
+    buf.run_decode(q, kn, vn, position=position)
+    buf.run_trim(limit, recent=1)
+    assert torch.equal(buf.kept_len, limit) and mk.madakv_poll_status(buf.ws) == 0
