@@ -298,6 +298,8 @@ int madakv_decode_attn_track(const madakv_config* cfg, int32_t layer, const void
  * kept_len[u] > limit[u] the call keeps c = max(limit[u], protected rows) rows (nothing happens if that is all of them):
  *   the protected rows, whose position kept_idx is above newest - recent, newest the largest position of the segment;
  *   then the rows with the largest acc (one that is not > 0, NaN included, counts as 0; equal ones: the lower row first).
+ * (Protected rows may be more than limit[u]: a slot needs room for max(limit[u], recent) rows and those that are appended until the
+ * next call, or the appends behind them are refused with MADAKV_ECAPACITY.)
  * Rows at and behind c that stay move into the rows below c that go, the first into the first and so on, with their acc
  * and kept_idx; kept_len[u] = c. No other row is written, those at and behind c keep their contents. (So the rows of
  * a segment are no longer in the order of their positions; attention does not depend on that order, and kept_idx says it.)

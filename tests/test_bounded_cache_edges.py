@@ -279,6 +279,34 @@ def test_integers_beyond_32_bits_are_refused():
     assert cache.kept_len.tolist() == [40]
 
 
+def readme_generation():
+    text = open(os.path.join(ROOT, "README.md")).read()
+    block = text.split("A generation on a cache in 4 bits", 1)[1].split("```", 2)[1]
+    assert "run_decode" in block and "run_trim" in block
+    return block
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [33, 48, 64])
+def test_the_generation_in_the_readme(new):
+    """It runs as printed, for hundreds of steps, with heads that keep fewer rows than the trims protect: no new token is refused."""
+    cfg = config("bf16", 2, 2, 4, 2, 64, 400, new=new)
+    q_win, k, v, mask, seq_len, budget = prompt(cfg, 1)
+    budget.fill_(5)  # every head keeps few rows
+    gen = torch.Generator().manual_seed(0)
+    shape = lambda h: torch.randn((2, 2, h, 64), generator=gen).bfloat16().cuda()  # noqa: E731
+    names = dict(binding=mk, cfg=cfg, capacity_rows=8 * (400 + new), q_win=q_win, k=k, v=v, mask=mask, seq_len=seq_len, budget=budget, steps=300,
+                 q=shape(4), k_new=shape(2), v_new=shape(2), position=seq_len)
+    exec(readme_generation(), names)
+    buf = names["buf"]
+    assert mk.madakv_poll_status(buf.ws) == 0
+    off, lens = buf.seg_off.tolist(), buf.kept_len.tolist()
+    assert min(names["limit"].view(-1).tolist()) < 32
+    for u in range(8):  # the newest tokens are there
+        newest = int(seq_len[u // 4]) + 299
+        assert set(range(newest - 31, newest + 1)) <= set(buf.kept_idx[off[u]:off[u] + lens[u]].tolist())
+
+
 def test_trim_without_tracking_is_refused():
     cfg = config("bf16", 1, 1, 1, 1, 64, 64)
     for quant in (False, True):
