@@ -265,8 +265,14 @@ int madakv_expand_quant(const madakv_config* cfg, const int64_t* rows, int64_t n
                         void* v_out, void* stream);
 
 /* Stage 5 on the cache in 4 bits: madakv_decode_attn with the values of the codes in the place of k_c and v_c. An appended row
- * (k_new, v_new in dtype) is quantised first, and attention sees its quantised values. Accumulation is fp32, out is
- * rounded to dtype once. A NaN among the values or queries gives NaN in out and lse. g <= 8 for fp32, g <= 16 for bf16.
+ * (k_new, v_new in dtype) is quantised first, and attention sees its quantised values. g <= 8 for fp32, g <= 16 for bf16.
+ * Rounding: sums, log-sum-exps and accumulated weights are fp32, out is rounded to dtype once. With bf16, for any g (in
+ *   madakv_decode_attn only from g = 3 on), softmax weights times a group's step enter the product with V's codes rounded to bf16;
+ *   the denominator stays fp32. A head's query elements are taken to 2^-38 of its largest one.
+ * Range: cache values up to 2^100 in magnitude (beyond, sums may overflow and give NaN for finite values); V below about 2^-90 is right
+ *   to n 2^-131 on n rows, not to a fraction of its size.
+ * NaN: a key that is NaN gives NaN in out and lse of its segment, a query element that is NaN or infinite in those of its head, a value
+ *   that is NaN in out's 32 columns of its group (lse is as without it).
  * acc, scratch, kept_idx, position, decay: as for madakv_decode_attn_track; acc null (with the other three) for a call without
  * tracking.                                                                                                   */
 int madakv_decode_attn_quant(const madakv_config* cfg, int32_t layer, const void* q, const void* k_new, const void* v_new,

@@ -235,6 +235,33 @@ def test_softmax_scale(dtype, d, scale):
         assert np.all(np.abs(cache.acc[a:a + n].double().cpu().numpy() - want) <= logit * w.sum(0) + 7 * 2.0 ** -24 * want + 1e-38)  # (weights below 2^-126 are 0)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,g", [("bf16", 3), ("bf16", 12), ("f32", 3)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[40, 700], [9000, 1]])
+def test_queries_that_are_not_numbers(dtype, g, d, lens):
+    """A head with an infinite or missing query element gets NaN in out and lse and adds no weight; the heads beside it stay as they are."""
+    cfg = config(dtype, 1, 2, g, 1, d, 9100)
+    cache = Cache(cfg, lens)
+    q, _, _ = cache.step(0, False)
+    for i, odd in enumerate((float("nan"), float("inf"), float("-inf"))):
+        results = []
+        for head in (None, i):
+            x = q.clone()
+            if head is not None:
+                x[0, :, head, 5 * i + 1] = odd
+            acc = torch.zeros_like(cache.acc)
+            results.append((*cache.decode(x, None, None, track=(acc, cache.scratch)), acc))
+        (a, la, wa), (b, lb, wb) = results
+        others = [h for h in range(g) if h != i]
+        assert b[0, :, i].isnan().all() and lb[0, :, i].isnan().all()
+        assert torch.equal(a[0, :, others], b[0, :, others]) and torch.equal(la[0, :, others], lb[0, :, others])
+        for u, n in enumerate(lens):
+            at = int(cache.off[u])
+            assert abs(float(wb[at:at + n].double().sum()) - (g - 1)) <= 1e-3 and not wb[at:at + n].isnan().any()
+    assert mk.madakv_poll_status(cache.ws) == 0
+
+
 # ------------------------------------------------------------------------------------------------- host side
 @pytest.mark.gpu
 def test_evictions_of_two_configs_from_two_threads():
