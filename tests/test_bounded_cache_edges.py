@@ -1,5 +1,6 @@
 """The cache in 4 bits and the bounded cache where they went wrong before: long runs of tiles under a maximum that stays, block ends beside
 the appended row, elements next to a border, queries and scales far from one, calls from two threads, heads that keep fewer rows than are protected."""
+import ctypes
 import math
 import os
 import threading
@@ -293,6 +294,32 @@ def test_evictions_of_two_configs_from_two_threads():
         t.join()
     torch.cuda.synchronize()
     assert not errors, (len(errors), set(errors))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,layers,Hq,Hkv,n,w", [("bf16", 16, 4, 4, 2000, 32), ("bf16", 2, 28, 4, 5000, 32), ("f32", 1, 4, 4, 2000, 32)])
+def test_first_call_of_a_thread_scores_as_any_other(dtype, layers, Hq, Hkv, n, w):
+    """A host thread whose first CUDA call it is gets the same kernels, and the same bits."""
+    cfg = mk.make_config(DT[dtype], 1, layers, Hq, Hkv, 128, n, w)
+    gen = torch.Generator(device="cuda").manual_seed(layers)
+    q = torch.randn((1, layers, Hq, w, 128), generator=gen, device="cuda").to(DT[dtype])
+    k = torch.randn((1, layers, Hkv, n, 128), generator=gen, device="cuda").to(DT[dtype])
+    seq_len, ws = torch.tensor([n], dtype=torch.int32, device="cuda"), mk.new_workspace(cfg)
+    psi = [torch.empty((1, layers, Hkv, n), device="cuda") for _ in range(2)]
+    mk.madakv_score(cfg, q, k, seq_len, None, psi[0], ws)
+    torch.cuda.synchronize()
+    rc = []
+    ptrs = [ctypes.c_void_p(t.data_ptr()) for t in (q, k, seq_len, psi[1], ws)]
+    strides = [mk.MadakvStrides(*t.stride()[:4]) for t in (q, k)]
+
+    def call():
+        rc.append(mk.lib().madakv_score(ctypes.byref(cfg), ptrs[0], strides[0], ptrs[1], strides[1], ptrs[2], None, ptrs[3], ptrs[4], ws.numel(), None))
+
+    t = threading.Thread(target=call)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert rc == [mk.OK] and torch.equal(psi[0], psi[1])
 
 
 @pytest.mark.gpu
