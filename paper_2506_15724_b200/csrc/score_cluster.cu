@@ -628,7 +628,8 @@ int run_cluster(const CUtensorMap& mk, const CUtensorMap& mq, const ClParams& p,
   using SL = ClSmem<D, NPAD>;
   const int smem = SL::alloc_bytes(p.C);
   auto kern = score_cluster_kernel<D, NPAD, kLong>;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+  // (the kernel's bound belongs to the process, and calls with other cluster sizes may come from other threads: the same for all)
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SL::alloc_bytes(kMaxCluster)) != cudaSuccess) {
     cudaGetLastError();
     return MADAKV_EUNSUPPORTED;
   }

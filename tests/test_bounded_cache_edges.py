@@ -323,6 +323,40 @@ def test_first_call_of_a_thread_scores_as_any_other(dtype, layers, Hq, Hkv, n, w
 
 
 @pytest.mark.gpu
+def test_scores_of_two_configs_from_two_threads():
+    """Clusters of 8 blocks and of 2 of one kernel, with shared memory for the exchange among as many: every call as if it were alone."""
+    work = []
+    for layers in (1, 16):
+        cfg = mk.make_config(torch.bfloat16, 1, layers, 4, 4, 128, 2000, 32)
+        gen = torch.Generator(device="cuda").manual_seed(layers)
+        q, k = (torch.randn((1, layers, 4, n, 128), generator=gen, device="cuda").bfloat16() for n in (32, 2000))
+        psi = torch.empty((1, layers, 4, 2000), device="cuda")
+        work.append((cfg, q, k, torch.tensor([2000], dtype=torch.int32, device="cuda"), None, psi, mk.new_workspace(cfg)))
+        mk.madakv_score(*work[-1])
+    torch.cuda.synchronize()
+    alone = [w[5].clone() for w in work]
+    errors, differ = [], []
+
+    def calls(want, cfg, q, k, seq_len, lse, psi, ws):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(3000):
+                try:
+                    mk.madakv_score(cfg, q, k, seq_len, lse, psi, ws)
+                    differ.append((psi != want).any())
+                except mk.MadakvError as e:
+                    errors.append(e.code)
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=calls, args=(a, *w)) for a, w in zip(alone, work)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, (len(errors), set(errors))
+    assert not torch.stack(differ).any(), int(torch.stack(differ).sum())
+
+
+@pytest.mark.gpu
 def test_integers_beyond_32_bits_are_refused():
     cfg = config("bf16", 1, 1, 1, 1, 64, 64)
     cache = Cache(cfg, [40])
