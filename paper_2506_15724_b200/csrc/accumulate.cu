@@ -1,7 +1,7 @@
 // Accumulated attention weight (Eq. 7's sum, over the decode steps instead of the proxy tokens):
 //   acc[row] = decay * acc[row] + sum over the group's heads of exp2(logit - lse)
 // with the logits and log2-sum-exps that the decode kernel before it has left. Bound by the logits, 4 g bytes a row that are written and
-// read (896 segments of 2512 rows, 7 heads: 29 us beside 126 of attention on 4 bits), and on one layer by being a second, dependent
+// read (896 segments of 2512 rows, 7 heads: 29 us beside 122 of attention on 4 bits), and on one layer by being a second, dependent
 // launch (8 segments of 2952 rows: 2.7 us).
 #include "common.cuh"
 

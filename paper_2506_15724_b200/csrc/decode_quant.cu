@@ -14,8 +14,9 @@
 // fp32: queries as three fp16 terms and weights as three bf16 terms, whose products are exact and whose sum is fp32 again; V's
 // operands are code - 7.5 then, so that no sum loses bits to the 23.5.
 // A warp has tiles of 32 rows of its own, read ahead into a ring in shared memory by asynchronous copies.
-// 1024 segments of 1638 rows, g = 1: 84 us, 0.50 of the copy bandwidth; 8 of 131071, g = 4: 51 us, 0.51. What binds is the pipe of
-// shifts, permutations and conversions, two clocks each (60 % busy), and with it the issue slots.
+// 1024 segments of 1638 rows, g = 1: 83 us, 0.50 of the copy bandwidth; 8 of 131071, g = 4: 50 us, 0.52. No unit is full (shifts, permutations
+// and conversions, two clocks each, 59 % of their pipe; issue 57 %, tensor cores 23 %, DRAM 38 %): three warps a partition go through
+// a serial chain per tile.
 #include <cuda_fp16.h>
 
 #include <type_traits>
