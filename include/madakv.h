@@ -8,9 +8,12 @@
  *   stage 4  madakv_select       per-head, per-modality eviction: keep the budgeted top-psi tokens     (Section 3.3, text after Eq. 8)
  *            madakv_compact      gather the kept K/V rows into a ragged per-head cache
  *   stage 5  madakv_decode_attn  cache append and decode attention over the ragged cache                (Eq. 4, Eq. 5)
- * and two things that a long generation needs beside it and the paper does not have:
+ * two things that a long generation needs beside it and the paper does not have:
  *   a ragged cache in 4 bits      madakv_compact_quant, madakv_decode_attn_quant, madakv_expand_quant
  *   a cache that stays bounded    madakv_decode_attn_track, madakv_evict, madakv_evict_quant
+ * and the attention on either side of it, which the paper takes as given:
+ *   before it, of the prompt      madakv_prefill_attn (its log-sum-exps are what madakv_score_lse reads)
+ *   after it, of drafted tokens   madakv_tree_attn, madakv_tree_commit
  *
  * General rules for every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller (the only host pointers are `cfg` and the
@@ -322,6 +325,64 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
                        int32_t* kept_idx, const int64_t* seg_off, int32_t* kept_len, int64_t capacity, uint8_t* k_code,
                        void* k_par, uint8_t* v_code, void* v_par, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Attention of a prompt ---------------------------------------------------------------------------------------
+ * Eq. 5 over the prompt of one layer, of whole sequences or of their newest queries (a chunk of a long prompt over the keys that are
+ * there already). Sequence b has n = keys(b) keys and m = queries(b) queries; query i stands at position n - m + i and with cfg->causal
+ * sees keys 0 .. n - m + i, else all n:
+ *   out[b][hq][i] = sum_j p_j v_j / sum_j p_j,  p_j = exp( scale * q_i . k_j - max ),  lse = max + log(sum_j p_j)
+ * over the keys that it sees; a query that sees none (n = 0, or a negative position where m > n) gets out = 0 and lse = -inf.
+ *   q, out  [B, L, H_q, q_rows, d] dtype, strides sq and so; layer `layer` of them is read and written
+ *   k, v    [B, L, H_kv, k_rows, d] dtype, strides sk and sv
+ *   With q_off (or k_off) non-null the sequences stand packed behind one another: q and out (k and v) are [L, H, rows, d], their
+ *   strides' `batch` is not used, and
+ *     q_off, k_off [B + 1] int64: sequence b has rows off[b] .. off[b + 1] - 1. A stretch that ends before it begins or beyond the last
+ *           row counts as empty. The lengths follow from it, at most n_max.
+ *   Otherwise
+ *     seq_len [B] int32: keys(b), brought into [0, min(n_max, k_rows)]. Exactly one of seq_len and k_off is given
+ *     q_len   [B] int32: queries(b), brought into [0, min(n_max, q_rows)]; null: as many as keys. Not with q_off
+ *   lse_out [B, L, H_q, q_rows] fp32 (packed: [L, H_q, q_rows]), contiguous, or null
+ * Rows of out and lse_out that belong to no query are left as they were. Two results that the eviction pass goes on from, each may be null
+ * and is written in full for the layer:
+ *   q_win   [B, L, H_q, w, d] dtype, contiguous: the queries of the proxy tokens (window row r is query m - w + r; a row that is
+ *           none of the call's queries is 0)
+ *   lse_win [B, L, H_q, w] fp32, contiguous: their log-sum-exps (-inf for those rows), as madakv_score_lse takes them
+ * H_q / H_kv is at most 64. bf16: products of bf16 with fp32 sums; the weights, at most 2^8 against the running maximum that they are
+ * taken to, are rounded to bf16 before the product with v (their sum is not), out is rounded once. fp32: fp32 throughout.
+ * Every query of a sequence reads whole tiles of up to 128 keys: a row of v that is not finite makes NaN of results of the same sequence
+ * whose query stands up to 127 positions before it too. What stands behind a sequence's last key is never used.
+ * Deterministic. Few queries share out their keys over blocks, with the partial results in the workspace.           */
+int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
+                        const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
+                        madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
+                        madakv_strides so, float* lse_out, void* q_win, float* lse_win, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Drafted tokens ----------------------------------------------------------------------------------------------
+ * A speculative step: T = nodes (1 .. 64) drafted tokens of every sequence, a tree, are attended to in one call, and the path of them that
+ * is accepted is appended to the ragged cache.
+ *   mask    [B, T] uint64: bit j of mask[b][i] says that node i sees node j (its ancestors and itself)
+ *   n_nodes [B] int32 or null: the nodes of sequence b are 0 .. n_nodes[b] - 1 (brought into [0, T]; null: all T); others are neither
+ *           seen nor computed
+ *   q, out  [B, L, H_q, T, d], k_tree, v_tree [B, L, H_kv, T, d] dtype, with strides
+ *   k_c, v_c, seg_off, kept_len, capacity: the ragged cache, as in madakv_decode_attn; layer -1 means all layers
+ * madakv_tree_attn: node i attends to all rows of every segment and to the nodes that it sees. A node that sees nothing (an empty segment, no
+ * bit set) gets out = 0 and lse = -inf; a segment that selection refused counts as empty. The cache is only read.
+ *   lse_out [B, L, H_q, T] fp32, contiguous, or null
+ * Rows of out and lse_out of nodes that are not there are left as they were. Roundings as in madakv_prefill_attn; H_q / H_kv at most 64. */
+int madakv_tree_attn(const madakv_config* cfg, int32_t layer, int32_t nodes, const void* q, madakv_strides sq, const void* k_tree,
+                     madakv_strides sk, const void* v_tree, madakv_strides sv, const uint64_t* mask, const int32_t* n_nodes,
+                     const void* k_c, const void* v_c, const int64_t* seg_off, const int32_t* kept_len, int64_t capacity,
+                     void* out, madakv_strides so, float* lse_out, void* ws, size_t ws_bytes, void* stream);
+
+/* Appends to every segment of sequence b the rows of k_tree and v_tree of the nodes that mask[b][node[b]] names, in ascending order, and
+ * makes kept_len longer by them. node [B] int32: the last accepted node, negative: none. A segment without room for all of them is left
+ * as it is and MADAKV_ECAPACITY is recorded; a node that is not there (node[b] >= n_nodes[b]) appends nothing and records MADAKV_ESHAPE.
+ *   acc      [capacity] fp32 or null: an appended row starts with weight 0
+ *   kept_idx [capacity] int32 and position [B] int32, both or neither: row i of the path gets position[b] + i                    */
+int madakv_tree_commit(const madakv_config* cfg, int32_t layer, int32_t nodes, const uint64_t* mask, const int32_t* n_nodes,
+                       const int32_t* node, const void* k_tree, madakv_strides sk, const void* v_tree, madakv_strides sv, void* k_c,
+                       void* v_c, const int64_t* seg_off, int32_t* kept_len, int64_t capacity, float* acc, int32_t* kept_idx,
+                       const int32_t* position, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronises `stream`, copies the device status word (a madakv_status) to *status_out and clears it. */
 int madakv_poll_status(void* ws, void* stream, int32_t* status_out);
 
@@ -331,7 +392,7 @@ const char* madakv_status_string(int status);
  * (nothing that version 1 had was changed). 3: madakv_config grew by keep_window and pool_kernel (struct_size is
  * checked: a caller built against version 2 gets MADAKV_EINVAL, not a misread struct). 4: madakv_demand_layer
  * added, madakv_allocate_layer accepts psi = NULL (nothing that version 3 had was changed). Calls that were added since (the
- * cache in 4 bits, tracking and eviction) changed nothing that version 4 had and left the number as it is: a program that
+ * cache in 4 bits, tracking and eviction, attention of prompts and drafted trees) changed nothing that version 4 had and left the number as it is: a program that
  * may meet an older library of version 4 looks their symbols up. */
 int madakv_abi_version(void);
 

@@ -25,7 +25,7 @@ EXPORTS = [
     "madakv_allocate", "madakv_allocate_layer", "madakv_demand_layer",
     "madakv_select", "madakv_compact", "madakv_decode_attn", "madakv_decode_attn_static", "madakv_poll_status",
     "madakv_compact_quant", "madakv_expand_quant", "madakv_decode_attn_quant", "madakv_decode_attn_track", "madakv_evict",
-    "madakv_evict_quant",
+    "madakv_evict_quant", "madakv_prefill_attn", "madakv_tree_attn", "madakv_tree_commit",
 ]
 
 
@@ -84,6 +84,10 @@ def lib():
         L.madakv_decode_attn_track.argtypes = [cfgp, i32] + [vp] * 7 + [i64] + [vp] * 6 + [f32, vp, sz, vp]
         L.madakv_evict.argtypes = [cfgp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
         L.madakv_evict_quant.argtypes = [cfgp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+        S = MadakvStrides
+        L.madakv_prefill_attn.argtypes = [cfgp, i32, vp, S, i64, vp, vp, vp, S, vp, S, i64, vp, vp, vp, S, vp, vp, vp, vp, sz, vp]
+        L.madakv_tree_attn.argtypes = [cfgp, i32, i32, vp, S, vp, S, vp, S] + [vp] * 6 + [i64, vp, S, vp, vp, sz, vp]
+        L.madakv_tree_commit.argtypes = [cfgp, i32, i32, vp, vp, vp, vp, S, vp, S] + [vp] * 4 + [i64] + [vp] * 4 + [sz, vp]
         L.madakv_poll_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         for f in EXPORTS:
             if f not in ("madakv_status_string",):
@@ -245,6 +249,29 @@ def madakv_evict_quant(cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_l
         raise MadakvError("madakv_evict_quant", rc)
 
 
+def madakv_prefill_attn(cfg, layer, q, k, v, out, ws, lse_out=None, q_win=None, lse_win=None, q_off=None, k_off=None, seq_len=None,
+                        q_len=None):
+    """Attention of a prompt's layer. q and out [B, L, H_q, rows, d], k and v [B, L, H_kv, rows, d], strided; with q_off (k_off) packed:
+    [L, H, rows, d]. Exactly one of k_off and seq_len is given; without q_off and q_len there are as many queries as keys."""
+    rc = _native.prefill_attn(cfg, int(layer), q, k, v, out, ws, lse_out, q_win, lse_win, q_off, k_off, seq_len, q_len)
+    if rc:
+        raise MadakvError("madakv_prefill_attn", rc)
+
+
+def madakv_tree_attn(cfg, layer, q, k_tree, v_tree, mask, k_c, v_c, seg_off, kept_len, out, lse_out, ws, n_nodes=None):
+    """mask [B, T] int64: the bits of the nodes that a node sees."""
+    rc = _native.tree_attn(cfg, int(layer), q, k_tree, v_tree, mask, k_c, v_c, seg_off, kept_len, out, lse_out, ws, n_nodes)
+    if rc:
+        raise MadakvError("madakv_tree_attn", rc)
+
+
+def madakv_tree_commit(cfg, layer, mask, node, k_tree, v_tree, k_c, v_c, seg_off, kept_len, ws, n_nodes=None, acc=None, kept_idx=None,
+                       position=None):
+    rc = _native.tree_commit(cfg, int(layer), mask, node, k_tree, v_tree, k_c, v_c, seg_off, kept_len, ws, n_nodes, acc, kept_idx, position)
+    if rc:
+        raise MadakvError("madakv_tree_commit", rc)
+
+
 def madakv_poll_status(ws):
     out = ctypes.c_int32(0)
     _check("madakv_poll_status", lib().madakv_poll_status(_ptr(ws), _stream(), ctypes.byref(out)))
@@ -274,6 +301,7 @@ class EvictionBuffers:
         self.ws = new_workspace(cfg, device)
         self.psi = z((B, L, Hkv, n), torch.float32)
         self.lse = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
+        self.q_win = None
         self.mass = z((B, L, Hkv, 2), torch.float64)
         self.pref = z((B, L, Hkv, 2), torch.float64)
         self.demand = z((B, L, Hkv, 2), torch.int32)
@@ -296,10 +324,26 @@ class EvictionBuffers:
         self.out = z((B, L, Hq, d), dt)
         self.lse_dec = z((B, L, Hq), torch.float32)
 
+    def run_prefill(self, layer, q, k, v, out, **lengths):
+        """Attention of a layer's prompt (lengths: q_off, k_off, seq_len, q_len, lse_out of madakv_prefill_attn). The proxy tokens' queries and
+        log-sum-exps are kept for run_eviction; needs want_lse."""
+        if self.lse is None:
+            raise ValueError("run_prefill: buffers without want_lse=True keep no log-sum-exps")
+        if self.q_win is None:
+            c = self.cfg
+            self.q_win = torch.zeros((c.batch, c.n_layers, c.n_q_heads, c.window, c.head_dim), dtype=self.out.dtype, device=self.out.device)
+        madakv_prefill_attn(self.cfg, layer, q, k, v, out, self.ws, q_win=self.q_win, lse_win=self.lse, **lengths)
+
     def run_eviction(self, q_win, k, v, mask, seq_len, budget):
-        """Stages 1-4, enqueued on the current stream."""
+        """Stages 1-4, enqueued on the current stream. q_win None: the queries and log-sum-exps that run_prefill has kept of every layer, with
+        which K is read once."""
         c = self.cfg
-        madakv_score(c, q_win, k, seq_len, self.lse, self.psi, self.ws)
+        if q_win is None:
+            if self.q_win is None:
+                raise ValueError("run_eviction: no q_win, and no run_prefill that has kept it")
+            madakv_score_lse(c, self.q_win, k, seq_len, self.lse, self.psi, self.ws)
+        else:
+            madakv_score(c, q_win, k, seq_len, self.lse, self.psi, self.ws)
         madakv_allocate(c, self.psi, mask, seq_len, budget, self.mass, self.pref, self.demand, self.phi, self.budgets,
                         self.ws)
         madakv_select(c, self.psi, mask, seq_len, self.budgets, self.kept_len, self.seg_off, self.kept_idx, self.ws)
@@ -320,6 +364,23 @@ class EvictionBuffers:
             tracked = (self.acc, self.scratch, self.kept_idx if position is not None else None, position, decay)
         (madakv_decode_attn_quant if self.quant else madakv_decode_attn_track)(*head, *tracked)
         if k_new is not None and position is None:
+            self.placed = False
+
+    def run_tree(self, q, k_tree, v_tree, mask, out, lse_out=None, layer=-1, n_nodes=None):
+        """Attention of drafted tokens over the segments and their tree (madakv_tree_attn); the cache is left as it is."""
+        if self.quant:
+            raise ValueError("run_tree: not on a cache in 4 bits")
+        madakv_tree_attn(self.cfg, layer, q, k_tree, v_tree, mask, *self.cache, self.seg_off, self.kept_len, out, lse_out, self.ws, n_nodes)
+
+    def run_commit(self, mask, node, k_tree, v_tree, layer=-1, n_nodes=None, position=None):
+        """The path up to node [B] int32 is appended (madakv_tree_commit). position [B] int32 is that of its first node; None: kept_idx is not kept
+        up, and run_trim can protect no recent rows until the next run_eviction. With tracking appended rows start without weight: that of
+        drafted tokens' attention is not accumulated."""
+        if self.quant:
+            raise ValueError("run_commit: not on a cache in 4 bits")
+        madakv_tree_commit(self.cfg, layer, mask, node, k_tree, v_tree, *self.cache, self.seg_off, self.kept_len, self.ws, n_nodes,
+                           self.acc if self.track else None, self.kept_idx if position is not None else None, position)
+        if position is None:
             self.placed = False
 
     def run_trim(self, limit, recent=0, layer=-1):

@@ -1,5 +1,7 @@
 // C-ABI entry points: argument checks, then stage launchers. No entry point allocates or synchronises, except
 // madakv_poll_status, which synchronises the stream to read the device status word.
+#include <initializer_list>
+
 #include "common.cuh"
 
 using namespace madakv;
@@ -267,6 +269,73 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
   const int code = cfg->head_dim / 2, par = cfg->head_dim / 8;
   return evict(cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_len, capacity,
                {{k_code, code}, {k_par, par}, {v_code, code}, {v_par, par}}, ws, ws_bytes, stream);
+}
+
+static bool all_strides_ok(const madakv_config& c, std::initializer_list<madakv_strides> all) {
+  for (const madakv_strides& s : all)
+    if (!strides_ok(c, s)) return false;
+  return true;
+}
+
+int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
+                        const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
+                        madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
+                        madakv_strides so, float* lse_out, void* q_win, float* lse_win, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  if (!q || !k || !v || !out) return MADAKV_EINVAL;
+  if ((k_off != nullptr) == (seq_len != nullptr) || (q_off && q_len)) return MADAKV_EINVAL;
+  if (layer < 0 || layer >= cfg->n_layers || q_rows <= 0 || k_rows <= 0) return MADAKV_ESHAPE;
+  if (q_rows > 0x7fffffffll || k_rows > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(q_win) || ((uintptr_t)q_off & 7) ||
+      ((uintptr_t)k_off & 7) || ((uintptr_t)q_len & 3) || ((uintptr_t)seq_len & 3) || ((uintptr_t)lse_out & 3) ||
+      ((uintptr_t)lse_win & 3))
+    return MADAKV_EALIGN;
+  if (!all_strides_ok(*cfg, {sq, sk, sv, so})) return MADAKV_EALIGN;
+  if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
+  return launch_prefill_attn(*cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win},
+                             ws, (cudaStream_t)stream);
+}
+
+// What the two calls on drafted trees share.
+static int check_tree(const madakv_config* cfg, int32_t layer, const TreeCall& a, const void* k_c, const void* v_c,
+                      const int32_t* kept_len) {
+  if (!a.k_tree || !a.v_tree || !a.mask || !k_c || !v_c || !a.seg_off || !kept_len) return MADAKV_EINVAL;
+  if (layer < -1 || layer >= cfg->n_layers || a.nodes <= 0) return MADAKV_ESHAPE;
+  if (a.nodes > 64) return MADAKV_EUNSUPPORTED;
+  if (a.capacity <= 0) return MADAKV_ECAPACITY;
+  if (!aligned16(a.k_tree) || !aligned16(a.v_tree) || !aligned16(k_c) || !aligned16(v_c) || ((uintptr_t)a.mask & 7) ||
+      ((uintptr_t)a.n_nodes & 3) || ((uintptr_t)a.seg_off & 7) || ((uintptr_t)kept_len & 3))
+    return MADAKV_EALIGN;
+  return all_strides_ok(*cfg, {a.sk, a.sv}) ? MADAKV_OK : MADAKV_EALIGN;
+}
+
+int madakv_tree_attn(const madakv_config* cfg, int32_t layer, int32_t nodes, const void* q, madakv_strides sq, const void* k_tree,
+                     madakv_strides sk, const void* v_tree, madakv_strides sv, const uint64_t* mask, const int32_t* n_nodes,
+                     const void* k_c, const void* v_c, const int64_t* seg_off, const int32_t* kept_len, int64_t capacity,
+                     void* out, madakv_strides so, float* lse_out, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  const TreeCall a{nodes, q, sq, k_tree, sk, v_tree, sv, mask, n_nodes, seg_off, capacity};
+  if (!q || !out) return MADAKV_EINVAL;
+  if ((rc = check_tree(cfg, layer, a, k_c, v_c, kept_len))) return rc;
+  if (!aligned16(q) || !aligned16(out) || ((uintptr_t)lse_out & 3) || !all_strides_ok(*cfg, {sq, so})) return MADAKV_EALIGN;
+  if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
+  return launch_tree_attn(*cfg, layer, a, k_c, v_c, kept_len, out, so, lse_out, ws, (cudaStream_t)stream);
+}
+
+int madakv_tree_commit(const madakv_config* cfg, int32_t layer, int32_t nodes, const uint64_t* mask, const int32_t* n_nodes,
+                       const int32_t* node, const void* k_tree, madakv_strides sk, const void* v_tree, madakv_strides sv, void* k_c,
+                       void* v_c, const int64_t* seg_off, int32_t* kept_len, int64_t capacity, float* acc, int32_t* kept_idx,
+                       const int32_t* position, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  const TreeCall a{nodes, nullptr, sk, k_tree, sk, v_tree, sv, mask, n_nodes, seg_off, capacity};
+  if (!node || (kept_idx == nullptr) != (position == nullptr)) return MADAKV_EINVAL;
+  if ((rc = check_tree(cfg, layer, a, k_c, v_c, kept_len))) return rc;
+  if (((uintptr_t)node & 3) || ((uintptr_t)acc & 3) || ((uintptr_t)kept_idx & 3) || ((uintptr_t)position & 3)) return MADAKV_EALIGN;
+  if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
+  return launch_tree_commit(*cfg, layer, a, node, k_c, v_c, kept_len, acc, kept_idx, position, ws, (cudaStream_t)stream);
 }
 
 int madakv_poll_status(void* ws, void* stream, int32_t* status_out) {

@@ -22,7 +22,8 @@ namespace madakv {
 //   [.., .. + score)         stage 1 scratch: finished-item counters [units * rows] int32, log2-domain row
 //                            log-sum-exp [units * rows] fp32 (rows = g * w padded to a multiple of 32), per-chunk
 //                            partial (max, sum) pairs, the bf16 terms of small fp32 calls (see ws_layout)
-//   [.., .. + decode)        stage 5 scratch: split partials [B * L * H_q * splits * (d + 2)] fp32
+//   [.., .. + decode)        stage 5 scratch: split partials [B * L * H_q * splits * (d + 2)] fp32; attention of prompts and of
+//                            drafted trees has its partials in the same place [kAttnPartRows * (d + 2)]
 // Stages 2-3 keep their scratch in shared memory.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr size_t kHeaderBytes = 256;
@@ -30,6 +31,7 @@ constexpr int kScoreChunk = 1024;   // keys per (max, sum) partial of the generi
 constexpr int kScoreTcChunk = 512;  // keys per work item (and per partial) of the tensor-core scoring path
 constexpr int kCounters = 16384;
 constexpr int kDecodeChunk = 256;   // cache rows per split of decode attention
+constexpr int kAttnPartRows = 148 * 256;  // rows of partial results of prompt and tree attention: a tile of 256 for every SM
 
 struct WsHeader {
   int32_t status;        // madakv_status set by device code
@@ -119,8 +121,9 @@ inline WsLayout ws_layout(const madakv_config& c) {
   w.score_split_off = off;
   off = align_up(off + split_area_bytes(c), 256);
   w.decode_off = off;
-  off = align_up(off + (size_t)c.batch * c.n_layers * c.n_q_heads * (size_t)w.decode_splits * (c.head_dim + 2) *
-                           sizeof(float), 256);
+  size_t rows_of_partials = (size_t)c.batch * c.n_layers * c.n_q_heads * (size_t)w.decode_splits;
+  if (rows_of_partials < kAttnPartRows) rows_of_partials = kAttnPartRows;
+  off = align_up(off + rows_of_partials * (c.head_dim + 2) * sizeof(float), 256);
   w.total = off;
   return w;
 }
@@ -318,5 +321,44 @@ struct RowArray {
 };
 int launch_evict(const madakv_config& c, int layer, const int32_t* limit, int recent, float* acc, int32_t* kept_idx,
                  const int64_t* seg_off, int32_t* kept_len, int64_t capacity, const RowArray (&rows)[4], cudaStream_t st);
+
+// Attention of a prompt, of drafted trees, and the commit of a tree's accepted path (argument names as in madakv.h).
+struct PromptCall {
+  const void* q;
+  madakv_strides sq;
+  int64_t q_rows;
+  const int64_t* q_off;
+  const int32_t* q_len;
+  const void* k;
+  madakv_strides sk;
+  const void* v;
+  madakv_strides sv;
+  int64_t k_rows;
+  const int64_t* k_off;
+  const int32_t* seq_len;
+  void* out;
+  madakv_strides so;
+  float* lse_out;
+  void* q_win;
+  float* lse_win;
+};
+struct TreeCall {
+  int nodes;
+  const void* q;
+  madakv_strides sq;
+  const void* k_tree;
+  madakv_strides sk;
+  const void* v_tree;
+  madakv_strides sv;
+  const uint64_t* mask;
+  const int32_t* n_nodes;
+  const int64_t* seg_off;
+  int64_t capacity;
+};
+int launch_prefill_attn(const madakv_config& c, int layer, const PromptCall& a, void* ws, cudaStream_t st);
+int launch_tree_attn(const madakv_config& c, int layer, const TreeCall& a, const void* k_c, const void* v_c, const int32_t* kept_len,
+                     void* out, madakv_strides so, float* lse_out, void* ws, cudaStream_t st);
+int launch_tree_commit(const madakv_config& c, int layer, const TreeCall& a, const int32_t* node, void* k_c, void* v_c,
+                       int32_t* kept_len, float* acc, int32_t* kept_idx, const int32_t* position, void* ws, cudaStream_t st);
 
 }  // namespace madakv

@@ -422,6 +422,110 @@ PyObject* evict(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- attention of prompts and of drafted trees
+// [B, L, heads, rows, d], or [L, heads, rows, d] of packed sequences
+struct Rows {
+  void* data;
+  madakv_strides st;
+  int64_t rows;
+  Rows(Checked& a, const char* name, int64_t heads, bool packed) {
+    const at::Tensor& t = a.on_device(a.next(), name, a.dtype());
+    const int x = packed ? 0 : 1;
+    if (t.dim() != 4 + x) Checked::wrong(name, packed ? "expected [L, H, rows, d]" : "expected [B, L, H, rows, d]");
+    if ((!packed && t.size(0) != a.cfg->batch) || t.size(x) != a.cfg->n_layers || t.size(x + 1) != heads ||
+        t.size(x + 3) != a.cfg->head_dim)
+      Checked::wrong(name, "wrong size for this config");
+    if (t.stride(x + 3) != 1) Checked::wrong(name, "expected contiguous rows");
+    rows = t.size(x + 2);
+    // (a dimension of one element is never walked: whatever stride it has)
+    auto stride = [&](int i) { return t.size(i) > 1 ? t.stride(i) : 0; };
+    st = {packed ? 0 : stride(0), stride(x), stride(x + 1), rows > 1 ? t.stride(x + 2) : a.cfg->head_dim};
+    data = t.data_ptr();
+  }
+};
+
+PyObject* prefill_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Checked a(args, n, 14);
+  if (a.bad_config) return PyLong_FromLong(a.bad_config);
+  const int32_t layer = a.integer();
+  const bool q_packed = args[10] != Py_None, k_packed = args[11] != Py_None;
+  const int64_t B = a.cfg->batch, Hq = a.cfg->n_q_heads, w = a.cfg->window, d = a.cfg->head_dim;
+  const Rows q(a, "q", Hq, q_packed), k(a, "k", a.cfg->n_kv_heads, k_packed), v(a, "v", a.cfg->n_kv_heads, k_packed),
+      out(a, "out", Hq, q_packed);
+  if (k.rows != v.rows) Checked::wrong("v", "expected as many rows as k has");
+  if (q.rows != out.rows) Checked::wrong("out", "expected as many rows as q has");
+  size_t bytes;
+  void *ws = a.workspace(bytes), *st = stream();
+  float* lse = a.array<float>("lse_out", at::kFloat, (q_packed ? 1 : B) * a.cfg->n_layers * Hq * q.rows, true, true);
+  void* q_win = a.array("q_win", a.dtype(), a.heads * w * d, true, true);
+  float* lse_win = a.array<float>("lse_win", at::kFloat, a.heads * w, true, true);
+  const int64_t *q_off = a.array<int64_t>("q_off", at::kLong, B + 1, true, true), *k_off = a.array<int64_t>("k_off", at::kLong, B + 1, true, true);
+  const int32_t *seq_len = a.array<int32_t>("seq_len", at::kInt, B, true), *q_len = a.array<int32_t>("q_len", at::kInt, B, true);
+  return without_lock([&] {
+    return madakv_prefill_attn(a.cfg, layer, q.data, q.st, q.rows, q_off, q_len, k.data, k.st, v.data, v.st, k.rows, k_off, seq_len,
+                               out.data, out.st, lse, q_win, lse_win, ws, bytes, st);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* tree_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Checked a(args, n, 14);
+  if (a.bad_config) return PyLong_FromLong(a.bad_config);
+  const int32_t layer = a.integer();
+  const int64_t Hq = a.cfg->n_q_heads, Hkv = a.cfg->n_kv_heads, d = a.cfg->head_dim;
+  const Rows q(a, "q", Hq, false), k(a, "k_tree", Hkv, false), v(a, "v_tree", Hkv, false);
+  if (k.rows != q.rows || v.rows != q.rows) Checked::wrong("k_tree, v_tree", "expected as many rows as q has");
+  if (q.rows > 64) return PyLong_FromLong(MADAKV_EUNSUPPORTED);
+  const int64_t* mask = a.array<int64_t>("mask", at::kLong, a.cfg->batch * q.rows, false, true);
+  int64_t capacity = -1;
+  const void *k_c = a.cache("k_c", a.dtype(), d, capacity), *v_c = a.cache("v_c", a.dtype(), d, capacity);
+  const int64_t* seg_off = a.array<int64_t>("seg_off", at::kLong, a.units + 1);
+  const int32_t* kept_len = a.array<int32_t>("kept_len", at::kInt, a.units);
+  const Rows out(a, "out", Hq, false);
+  if (out.rows != q.rows) Checked::wrong("out", "expected as many rows as q has");
+  float* lse = a.array<float>("lse_out", at::kFloat, a.heads * q.rows, true, true);
+  size_t bytes;
+  void *ws = a.workspace(bytes), *st = stream();
+  const int32_t* n_nodes = a.array<int32_t>("n_nodes", at::kInt, a.cfg->batch, true);
+  return without_lock([&] {
+    return madakv_tree_attn(a.cfg, layer, (int32_t)q.rows, q.data, q.st, k.data, k.st, v.data, v.st, (const uint64_t*)mask, n_nodes, k_c,
+                            v_c, seg_off, kept_len, capacity, out.data, out.st, lse, ws, bytes, st);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* tree_commit(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Checked a(args, n, 15);
+  if (a.bad_config) return PyLong_FromLong(a.bad_config);
+  const int32_t layer = a.integer();
+  const int64_t B = a.cfg->batch, Hkv = a.cfg->n_kv_heads, d = a.cfg->head_dim;
+  const int64_t* mask = a.array<int64_t>("mask", at::kLong, B);
+  const int64_t listed = a.tensor(args[2]).numel();
+  const int32_t* node = a.array<int32_t>("node", at::kInt, B);
+  const Rows k(a, "k_tree", Hkv, false), v(a, "v_tree", Hkv, false);
+  if (k.rows != v.rows) Checked::wrong("v_tree", "expected as many rows as k_tree has");
+  if (k.rows > 64) return PyLong_FromLong(MADAKV_EUNSUPPORTED);
+  if (listed != B * k.rows) Checked::wrong("mask", "expected [B, nodes]");
+  int64_t capacity = -1;
+  void *k_c = a.cache("k_c", a.dtype(), d, capacity), *v_c = a.cache("v_c", a.dtype(), d, capacity);
+  const int64_t* seg_off = a.array<int64_t>("seg_off", at::kLong, a.units + 1);
+  int32_t* kept_len = a.array<int32_t>("kept_len", at::kInt, a.units);
+  size_t bytes;
+  void *ws = a.workspace(bytes), *st = stream();
+  const int32_t* n_nodes = a.array<int32_t>("n_nodes", at::kInt, B, true);
+  float* acc = a.array<float>("acc", at::kFloat, capacity, true);
+  int32_t* kept_idx = a.array<int32_t>("kept_idx", at::kInt, capacity, true);
+  const int32_t* position = a.array<int32_t>("position", at::kInt, B, true);
+  return without_lock([&] {
+    return madakv_tree_commit(a.cfg, layer, (int32_t)k.rows, (const uint64_t*)mask, n_nodes, node, k.data, k.st, v.data, v.st, k_c, v_c,
+                              seg_off, kept_len, capacity, acc, kept_idx, position, ws, bytes, st);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 PyCFunction as_method(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -441,6 +545,9 @@ PyMethodDef methods[] = {
     {"decode_attn_track", as_method(decode_more<false>), METH_FASTCALL, nullptr},
     {"evict", as_method(evict<false>), METH_FASTCALL, nullptr},
     {"evict_quant", as_method(evict<true>), METH_FASTCALL, nullptr},
+    {"prefill_attn", as_method(prefill_attn), METH_FASTCALL, nullptr},
+    {"tree_attn", as_method(tree_attn), METH_FASTCALL, nullptr},
+    {"tree_commit", as_method(tree_commit), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
