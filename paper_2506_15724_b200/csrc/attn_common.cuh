@@ -48,6 +48,8 @@ struct AttnParams {
   int64_t n_items;     // items (without slots) at most
   int q_tiles;         // tree: tiles of a unit's rows
   void* ws;
+  int hold_copies;        // test of waits that run out: no tile of keys is copied
+  long long wait_clocks;  // bound of a wait
 };
 
 // One work item. Row r of its tile is query q0 + r / g, head r % g of the group.
@@ -135,17 +137,17 @@ __device__ __forceinline__ bool prompt_item(const AttnParams& p, int64_t i, Attn
   return true;
 }
 
-// The proxy tokens' rows that are none of the call's queries: log-sum-exp -inf, query 0. All threads of the grid.
+// The proxy tokens' rows that are none of the call's queries: log-sum-exp -inf, query 0. `threads` threads of every block.
 template <int ROW_BYTES>
-__device__ __forceinline__ void fill_window(const AttnParams& p) {
+__device__ __forceinline__ void fill_window(const AttnParams& p, int thread, int threads) {
   if (!p.lse_win && !p.q_win) return;
   for (int x = blockIdx.x; x < p.B * p.Hq; x += gridDim.x) {
     const int b = x / p.Hq, none = max(0, p.w - prompt_queries(p, b, p.q_off || p.q_len ? 0 : prompt_keys(p, b)));
     const int64_t row = (((int64_t)b * p.L + p.layer) * p.Hq + x % p.Hq) * p.w;
     if (p.lse_win)
-      for (int r = threadIdx.x; r < none; r += blockDim.x) p.lse_win[row + r] = -INFINITY;
+      for (int r = thread; r < none; r += threads) p.lse_win[row + r] = -INFINITY;
     if (p.q_win)
-      for (int r = threadIdx.x; r < none * (ROW_BYTES / 16); r += blockDim.x)
+      for (int r = thread; r < none * (ROW_BYTES / 16); r += threads)
         reinterpret_cast<uint4*>((char*)p.q_win + row * ROW_BYTES)[r] = make_uint4(0, 0, 0, 0);
   }
 }
@@ -237,5 +239,6 @@ inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int til
 }
 
 int launch_attn_plain(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);
+int launch_attn_tc(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);  // -1: its copies cannot take these strides
 
 }  // namespace madakv

@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
   pdl_go();
   const int64_t y = blockIdx.x / p.slots;
   const int slot = blockIdx.x % p.slots;
-  if constexpr (!kTree) fill_window<D * (int)sizeof(T)>(p);
+  if constexpr (!kTree) fill_window<D * (int)sizeof(T)>(p, threadIdx.x, NT);
   if (threadIdx.x < 32) {
     AttnItem it;
     const bool there = kTree ? tree_item(p, y, it) : prompt_item(p, y, it);

@@ -1,0 +1,685 @@
+// Attention of a prompt and of drafted trees on the tensor cores (bf16):
+//   S = Q K^T,  P = exp2(scale * log2(e) * S - m),  O = sum over the tiles of keys of P V,  out = O / sum P
+// A block is resident on every SM and goes through work items; an item is two tiles of 128 rows (query, head of the group) of one KV
+// head and the 128-key tiles that they see. Everything stays on the SM: S and O in tensor memory (4 x 128 columns), P over the S that it
+// was made of, as the product's left operand, K and V in a ring of stages that both tiles read.
+//   warps 0-3, 4-7   a row per thread: weights of the first and the second tile, results
+//   warps 8-11       queries (plain copies: any strides, any group)
+//   warp 12, 13      matrix products; copies of keys and values, a thread each
+//   warp 14          the items one after the other, ahead of the others
+//   warp 15          rows of V behind the last key become zeros before the products see them (weights of 0 do not keep a NaN out, and
+//                    other sequences' rows or none at all stand there; in K they only make logits that are masked)
+// The products of one tile run under the exponentials of the other: S0 S1 | O0 S0' O1 S1' | ...
+// An item whose rows fill one tile only takes the keys in turn: even tiles of keys go to the first accumulator, odd ones to the
+// second, and the two are joined at the end.
+// The maximum m that weights are taken against follows the running maximum only when that is 2^8 above it (in the weights), so O is
+// seldom corrected; the weights stay below 2^8, and numerator and denominator share the factor.
+#include "attn_common.cuh"
+#include "tc_common.cuh"
+
+namespace madakv {
+namespace {
+
+constexpr int kRows = 128, kKeys = 128, kThreads = 512, kRing = 4;
+constexpr float kSlack = 8.f;  // log2 of how far a row's maximum may run ahead of its reference
+
+template <int D>
+struct Geo {
+  static constexpr int kTile = 128 * D * 2;  // bytes of 128 rows: D / 64 blocks of 128 rows of 128 bytes, swizzled
+  static constexpr int kStages = D == 128 ? 5 : 10;
+};
+
+struct Work {
+  AttnItem it;
+  int64_t y;
+  int slot, nb;          // share of the keys, shares that take part
+  int begin, end, end0;  // tiles of keys; where the first tile of rows stops
+  int main_tiles;        // tiles of keys before the tree's own
+  int dual, tok0, tok1;  // one tile of rows only; queries of the tiles
+  int valid;
+};
+
+struct Barriers {
+  uint64_t full[10], empty[10], s_full[2], p_full[2], o_done[2], q_full, q_empty, item_full[kRing], item_empty[kRing], pair, landed[2], mended[2], drain;
+  Work ring[kRing];
+  float2 stats[2][kRows];
+  uint32_t tmem;
+  int abort;
+  unsigned last;
+  int mend_stage[2];  // where the copies that landed[] counts go
+};
+template <int D>
+constexpr int smem_bytes() {
+  return 2 * Geo<D>::kTile + Geo<D>::kStages * Geo<D>::kTile + (int)sizeof(Barriers);
+}
+static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
+
+// What a role waits with: bounded; once a wait has run out, here or in another role, everything that follows returns at once. A
+// single thread calls it; warps call all(), which all lanes leave together and with the same answer (instructions that take a whole
+// warp follow).
+struct Waiter {
+  volatile int* abort;
+  int32_t* status;
+  long long limit;
+  bool dead = false;
+  __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity, int site) {
+    if (dead) return false;
+    if (mbar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    int spins = 0;
+    while (!mbar_try(bar, parity)) {
+      if ((++spins & 15) == 0) {
+        if (*abort) return dead = true, false;
+        if (clock64() - t0 > limit) {
+          give_up(abort, status, site);
+          return dead = true, false;
+        }
+      }
+    }
+    return true;
+  }
+  __device__ __forceinline__ bool all(uint64_t* bar, uint32_t parity, int site) {
+    if (!__all_sync(0xffffffffu, (*this)(bar, parity, site))) dead = true;
+    return !dead;
+  }
+};
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+      "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_5d_plain(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3, int c4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+      "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// A from tensor memory, B from shared memory.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_desc_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 db;\nsetp.ne.b32 p, %4, 0;\nmov.b64 db, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_desc_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      : "memory");
+}
+// Descriptor of V as the operand whose rows are the contraction: 64 columns (128 bytes) by 8 keys are 1024 bytes, swizzled; the next
+// 8 keys follow 1024 bytes on (the stride offset, as for the other operands), the next 64 columns a block of 128 keys on.
+__device__ __forceinline__ uint32_t v_desc_lo(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((uint32_t)(kKeys * 128 >> 4) << 16); }
+__host__ __device__ constexpr uint32_t instr_desc_pv(int n) { return instr_desc_bf16(n) | (1u << 16); }
+
+#define R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
+#define T8(r, o) "+r"(r[o]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7])
+#define I8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+// 32 columns of a warp's lanes; valid behind tmem_wait and tie.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24)
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::I8(r, 0),
+      I8(r, 8), I8(r, 16), I8(r, 24), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tie32(uint32_t* r) { asm volatile("" : T8(r, 0), T8(r, 8), T8(r, 16), T8(r, 24) : : "memory"); }
+#undef R8
+#undef T8
+#undef I8
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// The tile that copy number i of an item brings, and whether it is V: as the products ask for them. K0 V0 K1 V1 ... where both tiles of
+// rows read every tile of keys; K0 K1 V0 K2 V1 ... where they take them in turn.
+__device__ __forceinline__ void copy_of(bool dual, int tiles, int i, int& tile, bool& is_v) {
+  if (!dual || tiles == 1) {
+    tile = i / 2;
+    is_v = i & 1;
+  } else if (i == 0) {
+    tile = 0;
+    is_v = false;
+  } else if (i == 2 * tiles - 1) {
+    tile = tiles - 1;
+    is_v = true;
+  } else {  // 1: K1, 2: V0, 3: K2, 4: V1, ...
+    tile = i & 1 ? (i + 1) / 2 : i / 2 - 1;
+    is_v = !(i & 1);
+  }
+}
+__device__ __forceinline__ int copy_of_k(bool dual, int tiles, int t) { return !dual || tiles == 1 ? 2 * t : t == 0 ? 0 : 2 * t - 1; }
+__device__ __forceinline__ int copy_of_v(bool dual, int tiles, int t) { return !dual || tiles == 1 ? 2 * t + 1 : t == tiles - 1 ? 2 * tiles - 1 : 2 * t + 2; }
+
+// Keys of the sequence, or nodes, in a tile of 128.
+__device__ __forceinline__ int keys_there(const Work& w, int tile, bool own) { return own ? w.it.nodes : w.it.n_keys - tile * kKeys; }
+
+template <int D, bool kTree>
+__global__ void __launch_bounds__(kThreads, 1)
+    attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_tk,
+                   const __grid_constant__ CUtensorMap map_tv, const __grid_constant__ AttnParams p) {
+  extern __shared__ __align__(1024) unsigned char base[];
+  constexpr int TILE = Geo<D>::kTile, NST = Geo<D>::kStages, BLOCK = kRows * 128;
+  const uint32_t q_smem = smem_u32(base), ring_smem = q_smem + 2 * TILE;
+  Barriers& sb = *reinterpret_cast<Barriers*>(base + 2 * TILE + NST * TILE);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (q_smem & 1023) {  // (the swizzle pattern is one of addresses; the driver places dynamic shared memory so)
+    if (threadIdx.x == 0) set_status(p.ws, MADAKV_ECUDA);
+    return;
+  }
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NST; ++i) mbar_init(&sb.full[i], 1), mbar_init(&sb.empty[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&sb.s_full[i], 1), mbar_init(&sb.p_full[i], 4), mbar_init(&sb.o_done[i], 1);
+    mbar_init(&sb.q_full, 128);
+    mbar_init(&sb.q_empty, 1);
+    for (int i = 0; i < kRing; ++i) mbar_init(&sb.item_full[i], 1), mbar_init(&sb.item_empty[i], 1 + 1 + 4 + 8 + 1);
+    mbar_init(&sb.pair, 8);
+    for (int i = 0; i < 2; ++i) mbar_init(&sb.landed[i], 1), mbar_init(&sb.mended[i], 1);
+    mbar_init(&sb.drain, 1);
+    sb.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sb.tmem)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sb.tmem;
+  pdl_wait();
+  pdl_go();
+  Waiter wait{&sb.abort, reinterpret_cast<int32_t*>(p.ws), p.wait_clocks};
+  const int tok_m = p.tile_q / 2;  // queries of a tile of rows
+
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    // ---- weights and results -------------------------------------------------------------------------------------------
+    const int s = warp / 4, r = (warp % 4) * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)((warp % 4) * 32) << 16), s_tm = lanes + s * 128, o_tm = lanes + 256 + s * D;
+    const int r_q = r / p.g, r_head = r % p.g;
+    const uint64_t scale2x = pack2(p.scale2, p.scale2);
+    uint32_t n_s = 0, n_o = 0, n_pair = 0;  // waits done on s_full, products issued for O, meetings of the eight warps
+    auto meet = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sb.pair);
+      wait.all(&sb.pair, n_pair++ & 1, kSiteTile);
+    };
+    for (uint32_t round = 0;; ++round) {
+      const Work& w = sb.ring[round % kRing];
+      if (!wait.all(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
+      const AttnItem& it = w.it;
+      const bool dual = w.dual;
+      const int tiles = w.end - w.begin, mt = dual ? 0 : s;
+      const int mine = dual ? (tiles + 1 - s) / 2 : s ? tiles : max(0, w.end0 - w.begin);
+      const int t = it.q0 + mt * tok_m + r_q;
+      const bool valid = r_q < (mt ? w.tok1 : w.tok0);
+      const bool active = __any_sync(0xffffffffu, valid);
+      const int visible = !valid ? 0x7fffffff : kTree || !p.causal ? it.n_keys : min(it.n_keys, t + it.shift + 1);
+      const int visible_all = __reduce_min_sync(0xffffffffu, visible);
+      uint64_t nodes = 0;
+      if constexpr (kTree) nodes = valid ? node_mask(p, it, t) : 0;
+      float m = -INFINITY, l = 0.f;
+      for (int x = 0; x < mine; ++x) {
+        if (!wait.all(&sb.s_full[s], n_s & 1, kSiteFull)) break;
+        ++n_s;
+        tc_fence_after();
+        if (active) {
+          uint32_t z[128];
+#pragma unroll
+          for (int c = 0; c < 128; c += 32) tmem_ld32(s_tm + c, z + c);
+          tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < 128; c += 32) tie32(z + c);
+          const int tile = w.begin + (dual ? 2 * x + s : x);
+          if (kTree && tile == w.main_tiles) {
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c >= 64 || !(nodes >> c & 1)) z[c] = 0xff800000u;
+          } else if ((tile + 1) * kKeys > visible_all) {
+            const int left = visible - tile * kKeys;
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c >= left) z[c] = 0xff800000u;
+          }
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < 128; c += 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top[i] = max3f(top[i], __uint_as_float(z[c + 2 * i]), __uint_as_float(z[c + 2 * i + 1]));
+          const float now = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
+          if (__any_sync(0xffffffffu, now > m && !((now - m) * p.scale2 <= kSlack))) {
+            const float next = fmaxf(m, now);
+            const float f = m == -INFINITY ? 0.f : ex2((m - next) * p.scale2);
+            l *= f;
+            m = next;
+            if (x > 0) {
+              // (S of this step has arrived, so the product before it, which was issued before, is done)
+#pragma unroll
+              for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(o_tm + c, o);
+                tmem_wait_ld();
+                tie32(o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st32(o_tm + c, o);
+              }
+            }
+          }
+          const float off = m == -INFINITY ? 0.f : -m * p.scale2;
+          const uint64_t off2 = pack2(off, off);
+          uint64_t sum[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t w2[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              float lo, hi;
+              unpack2(fma2(pack2u(z[64 * h + 2 * i], z[64 * h + 2 * i + 1]), scale2x, off2), lo, hi);
+              lo = ex2(lo);
+              hi = ex2(hi);
+              sum[i & 3] = add2(sum[i & 3], pack2(lo, hi));
+              w2[i] = pack_bf16x2(lo, hi);
+            }
+            tmem_st32(s_tm + 32 * h, w2);
+          }
+          float lo, hi;
+          unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), lo, hi);
+          l += lo + hi;
+          tmem_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sb.p_full[s]);
+        ++n_o;
+      }
+      // ---- results ----
+      if (mine > 0) wait.all(&sb.o_done[s], (n_o - 1) & 1, kSiteDrain);
+      tc_fence_after();
+      float f0 = 1.f, f1 = 0.f;  // factors of this thread's row in the accumulators that it reads
+      if (dual) {
+        // the second accumulator's rows join the first's: each half of the warps takes half of the columns of both
+        sb.stats[s][r] = make_float2(m, mine > 0 ? l : 0.f);
+        meet();
+        const float2 a = sb.stats[0][r], b = sb.stats[1][r];
+        m = fmaxf(a.x, b.x);
+        const float at = m == -INFINITY ? 0.f : m;
+        f0 = a.x == -INFINITY ? 0.f : ex2((a.x - at) * p.scale2);
+        f1 = b.x == -INFINITY ? 0.f : ex2((b.x - at) * p.scale2);
+        l = a.y * f0 + b.y * f1;
+        if (a.y != a.y || b.y != b.y) l = NAN;
+      }
+      const bool has0 = dual ? tiles > 0 : mine > 0, has1 = dual && tiles > 1;
+      const uint32_t o0 = dual ? lanes + 256 : o_tm, o1 = lanes + 256 + D;
+      const int c_begin = dual ? s * (D / 2) : 0, c_end = dual ? c_begin + D / 2 : D;
+      const bool split = w.nb > 1;
+      const float norm = split ? 1.f : row_factor(l);
+      const int64_t row = (w.y * p.slots + w.slot) * (p.tile_q * p.g) + mt * tok_m * p.g + r;
+      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)t * p.so.token + r_head * p.so.head;
+      if (active && !wait.dead) {
+#pragma unroll 1
+        for (int c = c_begin; c < c_end; c += 32) {
+          uint32_t a[32], b[32];
+          __syncwarp();
+          tmem_ld32(o0 + c, a);
+          if (dual) tmem_ld32(o1 + c, b);
+          tmem_wait_ld();
+          tie32(a);
+          if (dual) tie32(b);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float v = has0 ? __uint_as_float(a[i]) * f0 : 0.f;
+            if (has1) v += __uint_as_float(b[i]) * f1;
+            a[i] = __float_as_uint(v * norm);
+          }
+          if (!valid) continue;
+          if (split) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              __stcg(reinterpret_cast<uint4*>(p.part + row * D + c + i), make_uint4(a[i], a[i + 1], a[i + 2], a[i + 3]));
+          } else {
+            const bool none = !(l > 0.f || l != l);
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint4 v;
+              v.x = pack_bf16x2(__uint_as_float(a[i]), __uint_as_float(a[i + 1]));
+              v.y = pack_bf16x2(__uint_as_float(a[i + 2]), __uint_as_float(a[i + 3]));
+              v.z = pack_bf16x2(__uint_as_float(a[i + 4]), __uint_as_float(a[i + 5]));
+              v.w = pack_bf16x2(__uint_as_float(a[i + 6]), __uint_as_float(a[i + 7]));
+              *reinterpret_cast<uint4*>(dst + c + i) = none ? make_uint4(0, 0, 0, 0) : v;
+            }
+          }
+        }
+        if (valid && (!dual || s == 0)) {
+          if (split) __stcg(p.part_ml + row, make_float2(m, l));
+        }
+      }
+      auto finish = [&](int tt, int j, float lse) {
+        int64_t win;
+        if (!store_row_lse(p, it, tt, j, lse, win)) return;
+        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) + it.q_at + tt * p.sq.token + j * p.sq.head);
+        uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.q_win) + win * D);
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) to[i] = src[i];
+      };
+      if (!split && valid && (!dual || s == 0) && !wait.dead) finish(t, r_head, row_lse(m * p.scale2, l));
+      tc_fence_before();
+      if (dual) meet();  // (both accumulators have been read before either is written again)
+      if (split) {
+        meet();
+        if (threadIdx.x == 0 && !wait.dead) sb.last = arrive_inc(p.counter + w.y, (unsigned)w.nb - 1u);  // (wraps to 0: ready for the next call)
+        meet();
+        if (!wait.dead && sb.last == (unsigned)w.nb - 1u) {
+          constexpr int C4 = D / 4;
+          const int rows = (w.tok0 + w.tok1) * p.g, tile_rows = p.tile_q * p.g;
+          const int64_t first = w.y * p.slots * tile_rows;
+          for (int x = threadIdx.x; x < rows * C4; x += 256) {
+            const int rr = x / C4, c = x % C4 * 4;
+            float top = -INFINITY, sum = 0.f;
+            for (int i = 0; i < w.nb; ++i) top = fmaxf(top, __ldcg(p.part_ml + first + i * tile_rows + rr).x);
+            const float at = top == -INFINITY ? 0.f : top;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = 0; i < w.nb; ++i) {
+              const float2 ml = __ldcg(p.part_ml + first + i * tile_rows + rr);
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + (first + i * tile_rows + rr) * D + c));
+              const float f = ml.x == -INFINITY && ml.y == ml.y ? 0.f : ex2((ml.x - at) * p.scale2);
+              sum += ml.y * f;
+              o.x += v.x * f, o.y += v.y * f, o.z += v.z * f, o.w += v.w * f;
+            }
+            const float z = row_factor(sum);
+            const int tt = it.q0 + rr / p.g, j = rr % p.g;
+            __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)tt * p.so.token + j * p.so.head + c;
+            *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(o.x * z, o.y * z), pack_bf16x2(o.z * z, o.w * z));
+            if (c == 0) finish(tt, j, row_lse(top * p.scale2, sum));
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sb.item_empty[round % kRing]);
+      if (wait.dead) break;
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp < 12) {
+      // ---- queries -------------------------------------------------------------------------------------------------------
+      const int tid = threadIdx.x - 256;
+      constexpr int CPR = D / 8;  // 16-byte pieces of a row
+      const int c = tid % CPR, row_first = tid / CPR;
+      constexpr int STEP = 128 / CPR;
+      const uint32_t col = (c / 8) * BLOCK;
+      uint32_t n_q = 0;
+      for (uint32_t round = 0;; ++round) {
+        const Work& w = sb.ring[round % kRing];
+        if (!wait.all(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
+        const AttnItem& it = w.it;
+        const int tiles = w.end - w.begin;
+        if (tiles > 0) {
+          if (!wait.all(&sb.q_empty, (n_q++ & 1) ^ 1, kSiteQEmpty)) break;
+          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q) + it.q_at + c * 8;
+          for (int mt = 0; mt < (w.dual ? 1 : 2); ++mt)
+            for (int r = row_first; r < kRows; r += STEP) {
+              const int tq = r / p.g, j = r - tq * p.g;
+              const bool there = tq < (mt ? w.tok1 : w.tok0);
+              const int64_t at = (int64_t)(it.q0 + mt * tok_m + tq) * p.sq.token + j * p.sq.head;
+              cp_async16(q_smem + mt * TILE + col + r * 128 + ((c % 8) ^ (r & 7)) * 16, q + (there ? at : 0), there);
+            }
+          cp_async_all();
+          fence_async();
+          mbar_arrive(&sb.q_full);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sb.item_empty[round % kRing]);
+      }
+    } else if (warp == 12) {
+      // ---- matrix products: one thread ----------------------------------------------------------------------------------
+      if (elect_one()) {
+        constexpr uint32_t kQk = instr_desc_bf16(kKeys), kPv = instr_desc_pv(D);
+        uint32_t seq = 0, n_p[2] = {0, 0}, n_q = 0;
+        for (uint32_t round = 0;; ++round) {
+          const Work& w = sb.ring[round % kRing];
+          if (!wait(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
+          const bool dual = w.dual;
+          const int tiles = w.end - w.begin, n0 = dual ? tiles : w.end0 - w.begin;
+          const int steps = dual ? tiles : 2 * tiles;
+          mbar_arrive(&sb.item_empty[round % kRing]);
+          if (tiles == 0) continue;
+          if (!wait(&sb.q_full, n_q++ & 1, kSiteQFull)) break;
+          for (int x = 0; x <= steps; ++x) {
+            if (x < steps) {  // S of step x
+              const int s = x & 1, t = dual ? x : x / 2;
+              const uint32_t n = seq + copy_of_k(dual, tiles, t), st = n % NST;
+              if (dual || s || t < n0) {
+                if (!wait(&sb.full[st], n / NST & 1, kSiteFull)) break;
+                tc_fence_after();
+                const uint32_t a = smem_desc_lo(q_smem + (dual ? 0 : s) * TILE), b = smem_desc_lo(ring_smem + st * TILE);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                  const uint32_t at = (k / 4) * (BLOCK >> 4) + (k % 4) * 2;
+                  umma_bf16(tmem + s * 128, a + at, b + at, kQk, k > 0);
+                }
+                umma_commit(&sb.s_full[s]);
+              }
+              if (dual || s) umma_commit(&sb.empty[st]);
+              if (x == steps - 1) umma_commit(&sb.q_empty);
+            }
+            if (x > 0) {  // O of step x - 1
+              const int y = x - 1, s = y & 1, t = dual ? y : y / 2;
+              const uint32_t n = seq + copy_of_v(dual, tiles, t), st = n % NST;
+              if (dual || s || t < n0) {
+                if (!wait(&sb.full[st], n / NST & 1, kSiteFull) || !wait(&sb.p_full[s], n_p[s] & 1, kSiteTEmpty)) break;
+                ++n_p[s];
+                tc_fence_after();
+                const uint32_t b = v_desc_lo(ring_smem + st * TILE);
+                const bool first = dual ? y < 2 : t == 0;
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k)
+                  umma_bf16_ts(tmem + 256 + s * D, tmem + s * 128 + k * 8, b + k * (16 * 128 >> 4), kPv, !first || k > 0);
+                umma_commit(&sb.o_done[s]);
+              }
+              if (dual || s) umma_commit(&sb.empty[st]);
+            }
+          }
+          if (wait.dead) break;
+          seq += 2 * tiles;
+        }
+        if (wait.dead) {  // products in flight end before the block does
+          umma_commit(&sb.drain);
+          const long long t0 = clock64();
+          while (!mbar_try(&sb.drain, 0) && clock64() - t0 < kWaitCycles) {}
+        }
+      }
+    } else if (warp == 13) {
+      // ---- copies: one thread, which alone waits for stages to become free (a barrier's phases have two names only) -----------
+      if (elect_one()) {
+        uint32_t seq = 0, n_mend = 0;
+        for (uint32_t round = 0;; ++round) {
+          const Work& w = sb.ring[round % kRing];
+          if (!wait(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
+          const int tiles = w.end - w.begin, h = kTree ? 0 : w.it.h, b = kTree || p.k_off ? 0 : w.it.b;
+          for (int i = 0; i < 2 * tiles; ++i) {
+            int tile;
+            bool is_v;
+            copy_of(w.dual, tiles, i, tile, is_v);
+            tile += w.begin;
+            const bool own = kTree && tile == w.main_tiles;
+            const uint32_t n = seq + i, st = n % NST;
+            if (!wait(&sb.empty[st], (n / NST & 1) ^ 1, kSiteStage)) break;
+            uint64_t* bar = &sb.full[st];
+            if (is_v && keys_there(w, tile, own) < kKeys) {
+              const uint32_t e = n_mend & 1;
+              if (!wait(&sb.mended[e], (n_mend / 2 & 1) ^ 1, kSiteTile)) break;
+              sb.mend_stage[e] = (int)st;
+              bar = &sb.landed[e];
+              ++n_mend;
+            }
+            if (p.hold_copies) continue;
+            mbar_expect_tx(bar, TILE);
+            const uint32_t dst = ring_smem + st * TILE;
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x) {
+              if (own)
+                tma_load_5d_plain(dst + x * BLOCK, is_v ? &map_tv : &map_tk, bar, x * 64, 0, w.it.h, w.it.unit / p.Hkv % p.L, w.it.b);
+              else
+                tma_load_4d(dst + x * BLOCK, is_v ? &map_v : &map_k, bar, x * 64, (int)(w.it.key_row + tile * kKeys), h, b);
+            }
+          }
+          if (wait.dead) break;
+          mbar_arrive(&sb.item_empty[round % kRing]);
+          seq += 2 * tiles;
+        }
+        if (wait.dead) {  // copies in flight land before the block ends
+          const long long t0 = clock64();
+          while (clock64() - t0 < 2000000ll) {}
+        }
+      }
+    } else if (warp == 14) {
+      // ---- the items: in rounds over the blocks, to and fro, so that every block gets its share of long ones ----------------
+      uint32_t round = 0;
+      for (int64_t pass = 0;; ++pass) {
+        const int64_t g = gridDim.x, at = pass * g + (pass & 1 ? g - 1 - (int64_t)blockIdx.x : (int64_t)blockIdx.x);
+        Work w;
+        w.y = at / p.slots;
+        w.slot = (int)(at % p.slots);
+        w.valid = kTree ? tree_item(p, w.y, w.it) : prompt_item(p, w.y, w.it);
+        if (w.valid) {
+          const AttnItem& it = w.it;
+          const int toks = min(p.tile_q, it.n_q - it.q0);
+          if (toks <= 0) continue;
+          w.tok0 = min(tok_m, toks);
+          w.tok1 = toks - w.tok0;
+          w.dual = w.tok1 == 0;
+          auto tiles_for = [&](int last) {  // tiles of keys that query `last` sees
+            const int seen = kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, last + it.shift + 1));
+            return (seen + kKeys - 1) / kKeys;
+          };
+          w.main_tiles = tiles_for(it.q0 + toks - 1);
+          const int tiles = w.main_tiles + (kTree ? 1 : 0), tiles0 = tiles_for(it.q0 + w.tok0 - 1) + (kTree ? 1 : 0);
+          w.nb = shares_of(p, tiles);
+          if (w.slot >= w.nb) continue;
+          share_tiles(w.nb, tiles, w.slot, w.begin, w.end);
+          w.end0 = max(w.begin, min(w.end, tiles0));
+        }
+        if (!wait.all(&sb.item_empty[round % kRing], (round / kRing & 1) ^ 1, kSiteFlag)) break;
+        if (lane == 0) {
+          sb.ring[round % kRing] = w;
+          mbar_arrive(&sb.item_full[round % kRing]);
+        }
+        __syncwarp();
+        ++round;
+        if (!w.valid) break;
+      }
+    } else {
+      if constexpr (!kTree) fill_window<D * 2>(p, lane, 32);
+      // ---- rows of V behind the last key ----------------------------------------------------------------------------------
+      uint32_t n_mend = 0;
+      for (uint32_t round = 0;; ++round) {
+        const Work& w = sb.ring[round % kRing];
+        if (!wait.all(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
+        for (int tile = max(w.begin, w.main_tiles - 1); tile < w.end; ++tile) {
+          const int there = keys_there(w, tile, kTree && tile == w.main_tiles);
+          if (there >= kKeys) continue;
+          const uint32_t e = n_mend & 1;
+          if (!wait.all(&sb.landed[e], n_mend / 2 & 1, kSiteTile)) break;
+          ++n_mend;
+          const int st = sb.mend_stage[e];
+          unsigned char* v = base + 2 * TILE + st * TILE;
+          for (int x = there * 8 + lane; x < kKeys * 8; x += 32)
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half) *reinterpret_cast<uint4*>(v + half * BLOCK + x * 16) = make_uint4(0, 0, 0, 0);
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&sb.full[st]);
+            mbar_arrive(&sb.mended[e]);
+          }
+        }
+        if (wait.dead) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sb.item_empty[round % kRing]);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 12)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+// [batch, layers, heads, rows, d] with element strides, boxes of 128 rows by 64 elements; without layers in four dimensions.
+bool make_rows_map(CUtensorMap* map, const void* base, int d, int64_t rows, int heads, int layers, int batch, madakv_strides s) {
+  if ((heads > 1 && s.head <= 0) || (layers > 1 && s.layer <= 0) || (batch > 1 && s.batch <= 0)) return false;
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const int rank = layers ? 5 : 4;
+  const cuuint64_t batches = (cuuint64_t)batch;
+  const cuuint64_t dims[5] = {(cuuint64_t)d, (cuuint64_t)rows, (cuuint64_t)heads, layers ? (cuuint64_t)layers : batches, batches};
+  auto bytes = [&](int64_t v) { return (cuuint64_t)((v > 0 ? v : d) * 2); };  // (a dimension of extent 1 never advances)
+  const cuuint64_t strides[4] = {bytes(s.token), bytes(s.head), bytes(layers ? s.layer : s.batch), bytes(s.batch)};
+  for (const cuuint64_t x : strides)
+    if (x % 16 || x >= ((cuuint64_t)1 << 40)) return false;
+  const cuuint32_t box[5] = {64, kKeys, 1, 1, 1}, one[5] = {1, 1, 1, 1, 1};
+  auto encode = [&] {
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  // (a driver call: in a host thread whose first CUDA call this is it needs the context that the runtime makes)
+  int dev;
+  return encode() || (cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode());
+}
+
+template <int D, bool kTree>
+int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
+  CUtensorMap mk, mv, tk, tv;
+  if constexpr (kTree) {
+    const madakv_strides rows{0, 0, 0, D};
+    if (p.capacity >= 0x7fffffffll || !make_rows_map(&mk, p.k_c, D, p.capacity, 1, 0, 1, rows) || !make_rows_map(&mv, p.v_c, D, p.capacity, 1, 0, 1, rows) ||
+        !make_rows_map(&tk, p.k, D, p.q_rows, p.Hkv, p.L, p.B, p.sk) || !make_rows_map(&tv, p.v, D, p.q_rows, p.Hkv, p.L, p.B, p.sv))
+      return -1;
+  } else {
+    const int batch = p.k_off ? 1 : p.B;
+    if (!make_rows_map(&mk, p.k, D, p.k_rows, p.Hkv, 0, batch, p.sk) || !make_rows_map(&mv, p.v, D, p.k_rows, p.Hkv, 0, batch, p.sv)) return -1;
+    tk = mk;
+    tv = mv;
+  }
+  p.tile_q = kRows / p.g * 2;
+  attn_items(p, kTree);
+  attn_slots(p, c, kTree, kKeys, 148, 2);
+  p.wait_clocks = kWaitCycles;
+  // Failure-path test (no GPU fault involved), as in decode attention: the copies are withheld, waits are bounded to that many clocks.
+  if (const char* e = getenv("MADAKV_TEST_HOLD_COPIES")) {
+    const long long v = atoll(e);
+    if (v >= 100000 && v < kWaitCycles) p.hold_copies = 1, p.wait_clocks = v;
+  }
+  auto kernel = attn_tc_kernel<D, kTree>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()) != cudaSuccess) return MADAKV_ECUDA;
+  const int64_t works = p.n_items * p.slots;
+  launch_pdl(kernel, dim3((unsigned)(works < 1 ? 1 : works < 148 ? works : 148)), dim3(kThreads), smem_bytes<D>(), st, mk, mv, tk, tv, p);
+  return launch_status();
+}
+
+}  // namespace
+
+int launch_attn_tc(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st) {
+  if (c.head_dim == 64) return tree ? run<64, true>(p, c, st) : run<64, false>(p, c, st);
+  return tree ? run<128, true>(p, c, st) : run<128, false>(p, c, st);
+}
+
+}  // namespace madakv
