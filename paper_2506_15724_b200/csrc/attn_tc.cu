@@ -127,13 +127,20 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
       : "r"(taddr)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::I8(r, 0),
-      I8(r, 8), I8(r, 16), I8(r, 24), "r"(taddr)
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : R8(r, 0), R8(r, 8)
+      : "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::I8(r, 0),
+      I8(r, 8), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tie16(uint32_t* r) { asm volatile("" : T8(r, 0), T8(r, 8) : : "memory"); }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tie32(uint32_t* r) { asm volatile("" : T8(r, 0), T8(r, 8), T8(r, 16), T8(r, 24) : : "memory"); }
@@ -272,14 +279,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (x > 0) {
               // (S of this step has arrived, so the product before it, which was issued before, is done)
 #pragma unroll
-              for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                tmem_ld32(o_tm + c, o);
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tmem_ld16(o_tm + c, o);
                 tmem_wait_ld();
-                tie32(o);
+                tie16(o);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                tmem_st32(o_tm + c, o);
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st16(o_tm + c, o);
               }
             }
           }
@@ -287,18 +294,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint64_t off2 = pack2(off, off);
           uint64_t sum[4] = {0, 0, 0, 0};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t w2[32];
+          for (int h = 0; h < 4; ++h) {
+            uint32_t w2[16];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < 16; ++i) {
               float lo, hi;
-              unpack2(fma2(pack2u(z[64 * h + 2 * i], z[64 * h + 2 * i + 1]), scale2x, off2), lo, hi);
+              unpack2(fma2(pack2u(z[32 * h + 2 * i], z[32 * h + 2 * i + 1]), scale2x, off2), lo, hi);
               lo = ex2(lo);
               hi = ex2(hi);
               sum[i & 3] = add2(sum[i & 3], pack2(lo, hi));
               w2[i] = pack_bf16x2(lo, hi);
             }
-            tmem_st32(s_tm + 32 * h, w2);
+            tmem_st16(s_tm + 16 * h, w2);
           }
           float lo, hi;
           unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), lo, hi);
