@@ -1,27 +1,27 @@
 // Attention of a prompt and of drafted trees on the tensor cores (bf16):
 //   S = Q K^T,  P = exp2(scale * log2(e) * S - m),  O = sum over the tiles of keys of P V,  out = O / sum P
 // A block is resident on every SM and goes through work items; an item is two tiles of 128 rows (query, head of the group) of one KV
-// head and the 128-key tiles that they see. Everything stays on the SM: S and O in tensor memory (4 x 128 columns), P over the S that it
-// was made of, as the product's left operand, K and V in a ring of stages that both tiles read.
+// head and the 128-key tiles that they see. Everything stays on the SM: S and O of both tiles of rows in tensor memory (4 x 128 columns), P
+// over the S that it was made of, as the product's left operand, K and V in a ring of stages that both tiles of rows read.
 //   warps 0-3, 4-7   a row per thread: weights of the first and the second tile, results
-//   warps 8-11       queries (plain copies: any strides, any group)
-//   warp 12, 13      matrix products; copies of keys and values, a thread each
-//   warp 14          the items one after the other, ahead of the others
-//   warp 15          rows of V behind the last key become zeros before the products see them (weights of 0 do not keep a NaN out, and
-//                    other sequences' rows or none at all stand there; in K they only make logits that are masked)
-// The products of one tile run under the exponentials of the other: S0 S1 | O0 S0' O1 S1' | ...
+//   warps 8, 9       matrix products; copies of keys and values, a thread each
+//   warp 10          the items one after the other, ahead of the others
+//   warp 11          copies of queries; rows of V behind the last key become zeros before the products see them (weights of 0 do not
+//                    keep a NaN out, and other sequences' rows or none at all stand there; in K they only make logits that are masked)
+// The products of one tile of rows run under the exponentials of the other: S0 S1 | O0 S0' O1 S1' | ...
 // An item whose rows fill one tile only takes the keys in turn: even tiles of keys go to the first accumulator, odd ones to the
 // second, and the two are joined at the end.
-// The maximum m that weights are taken against follows the running maximum only when that is 2^8 above it (in the weights), so O is
-// seldom corrected; the weights stay below 2^8, and numerator and denominator share the factor.
+// The reference m that weights are taken against is the maximum of the row's first tile of keys. It stays, without a look at later
+// maxima, until a tile's weights add up to more than 2^16; only then the tile is done again with its maximum, and O and the sum are scaled down. bf16
+// weights and fp32 sums have the range for it, relative errors are the same, and numerator and denominator share the factor.
 #include "attn_common.cuh"
 #include "tc_common.cuh"
 
 namespace madakv {
 namespace {
 
-constexpr int kRows = 128, kKeys = 128, kThreads = 512, kRing = 4;
-constexpr float kSlack = 8.f;  // log2 of how far a row's maximum may run ahead of its reference
+constexpr int kRows = 128, kKeys = 128, kThreads = 384, kRing = 4;
+constexpr float kMostSum = 65536.f;   // of a tile's weights, against the reference
 
 template <int D>
 struct Geo {
@@ -36,6 +36,7 @@ struct Work {
   int begin, end, end0;  // tiles of keys; where the first tile of rows stops
   int main_tiles;        // tiles of keys before the tree's own
   int dual, tok0, tok1;  // one tile of rows only; queries of the tiles
+  int q_row, q_outer;    // where the copies of queries begin
   int valid;
 };
 
@@ -96,10 +97,6 @@ __device__ __forceinline__ void tma_load_5d_plain(uint32_t dst, const CUtensorMa
       "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
       : "memory");
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // A from tensor memory, B from shared memory.
@@ -179,7 +176,7 @@ __device__ __forceinline__ int keys_there(const Work& w, int tile, bool own) { r
 template <int D, bool kTree>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_tk,
-                   const __grid_constant__ CUtensorMap map_tv, const __grid_constant__ AttnParams p) {
+                   const __grid_constant__ CUtensorMap map_tv, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ AttnParams p) {
   extern __shared__ __align__(1024) unsigned char base[];
   constexpr int TILE = Geo<D>::kTile, NST = Geo<D>::kStages, BLOCK = kRows * 128;
   const uint32_t q_smem = smem_u32(base), ring_smem = q_smem + 2 * TILE;
@@ -192,17 +189,21 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < NST; ++i) mbar_init(&sb.full[i], 1), mbar_init(&sb.empty[i], 1);
-    for (int i = 0; i < 2; ++i) mbar_init(&sb.s_full[i], 1), mbar_init(&sb.p_full[i], 4), mbar_init(&sb.o_done[i], 1);
-    mbar_init(&sb.q_full, 128);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sb.s_full[i], 1);
+      mbar_init(&sb.p_full[i], 4);
+      mbar_init(&sb.o_done[i], 1);
+    }
+    mbar_init(&sb.q_full, 1);
     mbar_init(&sb.q_empty, 1);
-    for (int i = 0; i < kRing; ++i) mbar_init(&sb.item_full[i], 1), mbar_init(&sb.item_empty[i], 1 + 1 + 4 + 8 + 1);
+    for (int i = 0; i < kRing; ++i) mbar_init(&sb.item_full[i], 1), mbar_init(&sb.item_empty[i], 1 + 1 + 1 + 8);
     mbar_init(&sb.pair, 8);
     for (int i = 0; i < 2; ++i) mbar_init(&sb.landed[i], 1), mbar_init(&sb.mended[i], 1);
     mbar_init(&sb.drain, 1);
     sb.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sb.tmem)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -216,13 +217,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tok_m = p.tile_q / 2;  // queries of a tile of rows
 
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---- weights and results -------------------------------------------------------------------------------------------
     const int s = warp / 4, r = (warp % 4) * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)((warp % 4) * 32) << 16), s_tm = lanes + s * 128, o_tm = lanes + 256 + s * D;
     const int r_q = r / p.g, r_head = r % p.g;
     const uint64_t scale2x = pack2(p.scale2, p.scale2);
-    uint32_t n_s = 0, n_o = 0, n_pair = 0;  // waits done on s_full, products issued for O, meetings of the eight warps
+    uint32_t n_s = 0, n_pair = 0;  // tiles of keys done, meetings of the eight warps
     auto meet = [&] {
       __syncwarp();
       if (lane == 0) mbar_arrive(&sb.pair);
@@ -233,8 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!wait.all(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
       const AttnItem& it = w.it;
       const bool dual = w.dual;
-      const int tiles = w.end - w.begin, mt = dual ? 0 : s;
-      const int mine = dual ? (tiles + 1 - s) / 2 : s ? tiles : max(0, w.end0 - w.begin);
+      const int mt = dual ? 0 : s;
       const int t = it.q0 + mt * tok_m + r_q;
       const bool valid = r_q < (mt ? w.tok1 : w.tok0);
       const bool active = __any_sync(0xffffffffu, valid);
@@ -243,87 +243,95 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint64_t nodes = 0;
       if constexpr (kTree) nodes = valid ? node_mask(p, it, t) : 0;
       float m = -INFINITY, l = 0.f;
-      for (int x = 0; x < mine; ++x) {
+      const int stride = dual ? 2 : 1, tile_end = dual || s ? w.end : w.end0;
+      int tile = w.begin + (dual ? s : 0);
+      const bool some = tile < tile_end;
+      bool look = true;  // rows without a reference
+      for (bool first = true; tile < tile_end; tile += stride, first = false) {
         if (!wait.all(&sb.s_full[s], n_s & 1, kSiteFull)) break;
-        ++n_s;
         tc_fence_after();
         if (active) {
-          uint32_t z[128];
+          uint32_t z[kKeys];
 #pragma unroll
-          for (int c = 0; c < 128; c += 32) tmem_ld32(s_tm + c, z + c);
+          for (int c = 0; c < kKeys; c += 32) tmem_ld32(s_tm + c, z + c);
           tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < 128; c += 32) tie32(z + c);
-          const int tile = w.begin + (dual ? 2 * x + s : x);
+          for (int c = 0; c < kKeys; c += 32) tie32(z + c);
           if (kTree && tile == w.main_tiles) {
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
+            for (int c = 0; c < kKeys; ++c)
               if (c >= 64 || !(nodes >> c & 1)) z[c] = 0xff800000u;
           } else if ((tile + 1) * kKeys > visible_all) {
             const int left = visible - tile * kKeys;
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
+            for (int c = 0; c < kKeys; ++c)
               if (c >= left) z[c] = 0xff800000u;
           }
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (bool again = look;; again = true) {
+            if (again) {
+              float top[2] = {m, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < 128; c += 8)
+              for (int c = 0; c < kKeys; c += 4) {
+                top[0] = max3f(top[0], __uint_as_float(z[c]), __uint_as_float(z[c + 1]));
+                top[1] = max3f(top[1], __uint_as_float(z[c + 2]), __uint_as_float(z[c + 3]));
+              }
+              const float now = fmaxf(top[0], top[1]), f = m == -INFINITY ? 0.f : ex2((m - now) * p.scale2);
+              l *= f;
+              m = now;
+              look = __any_sync(0xffffffffu, m == -INFINITY);
+              // (S of this tile has arrived, so the product before it, which was issued before, is done)
+              if (!first) {
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                  uint32_t o[16];
+                  tmem_ld16(o_tm + c, o);
+                  tmem_wait_ld();
+                  tie16(o);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top[i] = max3f(top[i], __uint_as_float(z[c + 2 * i]), __uint_as_float(z[c + 2 * i + 1]));
-          const float now = fmaxf(max3f(top[0], top[1], top[2]), top[3]);
-          if (__any_sync(0xffffffffu, now > m && !((now - m) * p.scale2 <= kSlack))) {
-            const float next = fmaxf(m, now);
-            const float f = m == -INFINITY ? 0.f : ex2((m - next) * p.scale2);
-            l *= f;
-            m = next;
-            if (x > 0) {
-              // (S of this step has arrived, so the product before it, which was issued before, is done)
-#pragma unroll
-              for (int c = 0; c < D; c += 16) {
-                uint32_t o[16];
-                tmem_ld16(o_tm + c, o);
-                tmem_wait_ld();
-                tie16(o);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                tmem_st16(o_tm + c, o);
+                  for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                  tmem_st16(o_tm + c, o);
+                }
               }
             }
-          }
-          const float off = m == -INFINITY ? 0.f : -m * p.scale2;
-          const uint64_t off2 = pack2(off, off);
-          uint64_t sum[4] = {0, 0, 0, 0};
+            const float off = m == -INFINITY ? 0.f : -m * p.scale2;
+            const uint64_t off2 = pack2(off, off);
+            uint64_t sum[2] = {0, 0};
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            uint32_t w2[16];
+            for (int h = 0; h < 4; ++h) {
+              uint32_t w2[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float lo, hi;
-              unpack2(fma2(pack2u(z[32 * h + 2 * i], z[32 * h + 2 * i + 1]), scale2x, off2), lo, hi);
-              lo = ex2(lo);
-              hi = ex2(hi);
-              sum[i & 3] = add2(sum[i & 3], pack2(lo, hi));
-              w2[i] = pack_bf16x2(lo, hi);
+              for (int i = 0; i < 16; ++i) {
+                float lo, hi;
+                unpack2(fma2(pack2u(z[32 * h + 2 * i], z[32 * h + 2 * i + 1]), scale2x, off2), lo, hi);
+                lo = ex2(lo);
+                hi = ex2(hi);
+                sum[i & 1] = add2(sum[i & 1], pack2(lo, hi));
+                w2[i] = pack_bf16x2(lo, hi);
+              }
+              tmem_st16(s_tm + 16 * h, w2);
             }
-            tmem_st16(s_tm + 16 * h, w2);
+            float lo, hi;
+            unpack2(add2(sum[0], sum[1]), lo, hi);
+            lo += hi;
+            if (again || !__any_sync(0xffffffffu, lo > kMostSum)) {
+              l += lo;
+              break;
+            }
           }
-          float lo, hi;
-          unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), lo, hi);
-          l += lo + hi;
           tmem_wait_st();
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sb.p_full[s]);
-        ++n_o;
+        ++n_s;
       }
       // ---- results ----
-      if (mine > 0) wait.all(&sb.o_done[s], (n_o - 1) & 1, kSiteDrain);
+      if (some) wait.all(&sb.o_done[s], (n_s - 1) & 1, kSiteDrain);
       tc_fence_after();
       float f0 = 1.f, f1 = 0.f;  // factors of this thread's row in the accumulators that it reads
       if (dual) {
         // the second accumulator's rows join the first's: each half of the warps takes half of the columns of both
-        sb.stats[s][r] = make_float2(m, mine > 0 ? l : 0.f);
+        sb.stats[s][r] = make_float2(m, l);
         meet();
         const float2 a = sb.stats[0][r], b = sb.stats[1][r];
         m = fmaxf(a.x, b.x);
@@ -333,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         l = a.y * f0 + b.y * f1;
         if (a.y != a.y || b.y != b.y) l = NAN;
       }
-      const bool has0 = dual ? tiles > 0 : mine > 0, has1 = dual && tiles > 1;
+      const bool has0 = dual ? w.end > w.begin : some, has1 = dual && w.end > w.begin + 1;
       const uint32_t o0 = dual ? lanes + 256 : o_tm, o1 = lanes + 256 + D;
       const int c_begin = dual ? s * (D / 2) : 0, c_end = dual ? c_begin + D / 2 : D;
       const bool split = w.nb > 1;
@@ -424,37 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp < 12) {
-      // ---- queries -------------------------------------------------------------------------------------------------------
-      const int tid = threadIdx.x - 256;
-      constexpr int CPR = D / 8;  // 16-byte pieces of a row
-      const int c = tid % CPR, row_first = tid / CPR;
-      constexpr int STEP = 128 / CPR;
-      const uint32_t col = (c / 8) * BLOCK;
-      uint32_t n_q = 0;
-      for (uint32_t round = 0;; ++round) {
-        const Work& w = sb.ring[round % kRing];
-        if (!wait.all(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
-        const AttnItem& it = w.it;
-        const int tiles = w.end - w.begin;
-        if (tiles > 0) {
-          if (!wait.all(&sb.q_empty, (n_q++ & 1) ^ 1, kSiteQEmpty)) break;
-          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q) + it.q_at + c * 8;
-          for (int mt = 0; mt < (w.dual ? 1 : 2); ++mt)
-            for (int r = row_first; r < kRows; r += STEP) {
-              const int tq = r / p.g, j = r - tq * p.g;
-              const bool there = tq < (mt ? w.tok1 : w.tok0);
-              const int64_t at = (int64_t)(it.q0 + mt * tok_m + tq) * p.sq.token + j * p.sq.head;
-              cp_async16(q_smem + mt * TILE + col + r * 128 + ((c % 8) ^ (r & 7)) * 16, q + (there ? at : 0), there);
-            }
-          cp_async_all();
-          fence_async();
-          mbar_arrive(&sb.q_full);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sb.item_empty[round % kRing]);
-      }
-    } else if (warp == 12) {
+    if (warp == 8) {
       // ---- matrix products: one thread ----------------------------------------------------------------------------------
       if (elect_one()) {
         constexpr uint32_t kQk = instr_desc_bf16(kKeys), kPv = instr_desc_pv(D);
@@ -494,10 +472,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ++n_p[s];
                 tc_fence_after();
                 const uint32_t b = v_desc_lo(ring_smem + st * TILE);
-                const bool first = dual ? y < 2 : t == 0;
+                const bool begun = dual ? y >= 2 : t > 0;
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k)
-                  umma_bf16_ts(tmem + 256 + s * D, tmem + s * 128 + k * 8, b + k * (16 * 128 >> 4), kPv, !first || k > 0);
+                  umma_bf16_ts(tmem + 256 + s * D, tmem + s * 128 + k * 8, b + k * (16 * 128 >> 4), kPv, begun || k > 0);
                 umma_commit(&sb.o_done[s]);
               }
               if (dual || s) umma_commit(&sb.empty[st]);
@@ -512,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           while (!mbar_try(&sb.drain, 0) && clock64() - t0 < kWaitCycles) {}
         }
       }
-    } else if (warp == 13) {
+    } else if (warp == 9) {
       // ---- copies: one thread, which alone waits for stages to become free (a barrier's phases have two names only) -----------
       if (elect_one()) {
         uint32_t seq = 0, n_mend = 0;
@@ -556,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           while (clock64() - t0 < 2000000ll) {}
         }
       }
-    } else if (warp == 14) {
+    } else if (warp == 10) {
       // ---- the items: in rounds over the blocks, to and fro, so that every block gets its share of long ones ----------------
       uint32_t round = 0;
       for (int64_t pass = 0;; ++pass) {
@@ -572,16 +550,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           w.tok0 = min(tok_m, toks);
           w.tok1 = toks - w.tok0;
           w.dual = w.tok1 == 0;
-          auto tiles_for = [&](int last) {  // tiles of keys that query `last` sees
-            const int seen = kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, last + it.shift + 1));
-            return (seen + kKeys - 1) / kKeys;
-          };
-          w.main_tiles = tiles_for(it.q0 + toks - 1);
-          const int tiles = w.main_tiles + (kTree ? 1 : 0), tiles0 = tiles_for(it.q0 + w.tok0 - 1) + (kTree ? 1 : 0);
+          auto seen_by = [&](int last) { return kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, last + it.shift + 1)); };
+          w.main_tiles = (seen_by(it.q0 + toks - 1) + kKeys - 1) / kKeys;
+          const int tiles = w.main_tiles + (kTree ? 1 : 0), tiles0 = (seen_by(it.q0 + w.tok0 - 1) + kKeys - 1) / kKeys + (kTree ? 1 : 0);
           w.nb = shares_of(p, tiles);
           if (w.slot >= w.nb) continue;
           share_tiles(w.nb, tiles, w.slot, w.begin, w.end);
           w.end0 = max(w.begin, min(w.end, tiles0));
+          w.q_row = (int)((!kTree && p.q_off ? p.q_off[it.b] : 0) + it.q0);
+          w.q_outer = kTree && p.layer < 0 ? it.unit / p.Hkv : !kTree && p.q_off ? 0 : it.b;
         }
         if (!wait.all(&sb.item_empty[round % kRing], (round / kRing & 1) ^ 1, kSiteFlag)) break;
         if (lane == 0) {
@@ -594,11 +571,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     } else {
       if constexpr (!kTree) fill_window<D * 2>(p, lane, 32);
-      // ---- rows of V behind the last key ----------------------------------------------------------------------------------
-      uint32_t n_mend = 0;
+      // ---- queries, rows of V behind the last key -----------------------------------------------------------------------------
+      uint32_t n_mend = 0, n_q = 0;
       for (uint32_t round = 0;; ++round) {
         const Work& w = sb.ring[round % kRing];
         if (!wait.all(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
+        if (w.end > w.begin) {
+          if (!wait.all(&sb.q_empty, (n_q++ & 1) ^ 1, kSiteQEmpty)) break;
+          if (elect_one()) {
+            const int tiles_of_rows = w.dual ? 1 : 2;
+            mbar_expect_tx(&sb.q_full, (uint32_t)(tiles_of_rows * tok_m * p.g * D * 2));
+            for (int mt = 0; mt < tiles_of_rows; ++mt)
+#pragma unroll
+              for (int x = 0; x < D / 64; ++x)
+                tma_load_5d_plain(q_smem + mt * TILE + x * BLOCK, &map_q, &sb.q_full, x * 64, 0, w.q_row + mt * tok_m, w.it.h, w.q_outer);
+          }
+          __syncwarp();
+        }
         for (int tile = max(w.begin, w.main_tiles - 1); tile < w.end; ++tile) {
           const int there = keys_there(w, tile, kTree && tile == w.main_tiles);
           if (there >= kKeys) continue;
@@ -626,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 12)
+  if (warp == 8)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
@@ -652,9 +641,25 @@ bool make_rows_map(CUtensorMap* map, const void* base, int d, int64_t rows, int 
   return encode() || (cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode());
 }
 
+// Queries as (d, head of the group, query, KV head, outer), boxes of `queries` queries of a whole group: rows of the tile in their order.
+bool make_query_map(CUtensorMap* map, const void* base, int d, int g, int64_t rows, int heads, int64_t outer, int64_t outer_stride, madakv_strides s,
+                    int queries) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn || (g * heads > 1 && s.head <= 0) || (outer > 1 && outer_stride <= 0)) return false;
+  const cuuint64_t dims[5] = {(cuuint64_t)d, (cuuint64_t)g, (cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)outer};
+  auto bytes = [&](int64_t v) { return (cuuint64_t)((v > 0 ? v : d) * 2); };
+  const cuuint64_t strides[4] = {bytes(s.head), bytes(s.token), bytes(s.head * g), bytes(outer_stride)};
+  for (const cuuint64_t x : strides)
+    if (x % 16 || x >= ((cuuint64_t)1 << 40)) return false;
+  const cuuint32_t box[5] = {64, (cuuint32_t)g, (cuuint32_t)queries, 1, 1}, one[5] = {1, 1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, bool kTree>
 int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
-  CUtensorMap mk, mv, tk, tv;
+  CUtensorMap mk, mv, tk, tv, mq;
+  p.tile_q = kRows / p.g * 2;
   if constexpr (kTree) {
     const madakv_strides rows{0, 0, 0, D};
     if (p.capacity >= 0x7fffffffll || !make_rows_map(&mk, p.k_c, D, p.capacity, 1, 0, 1, rows) || !make_rows_map(&mv, p.v_c, D, p.capacity, 1, 0, 1, rows) ||
@@ -666,7 +671,12 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
     tk = mk;
     tv = mv;
   }
-  p.tile_q = kRows / p.g * 2;
+  // (behind the others: they have seen to it that this thread has a context)
+  const bool all = kTree && p.layer < 0;
+  if (all && p.B > 1 && p.L > 1 && p.sq.batch != p.L * p.sq.layer) return -1;
+  const int64_t outer = all ? (int64_t)p.B * p.L : !kTree && p.q_off ? 1 : p.B;
+  const void* q = kTree && !all ? (const char*)p.q + p.layer * p.sq.layer * 2 : p.q;
+  if (!make_query_map(&mq, q, D, p.g, p.q_rows, p.Hkv, outer, all && p.L > 1 ? p.sq.layer : p.sq.batch, p.sq, p.tile_q / 2)) return -1;
   attn_items(p, kTree);
   attn_slots(p, c, kTree, kKeys, 148, 2);
   p.wait_clocks = kWaitCycles;
@@ -678,7 +688,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   auto kernel = attn_tc_kernel<D, kTree>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()) != cudaSuccess) return MADAKV_ECUDA;
   const int64_t works = p.n_items * p.slots;
-  launch_pdl(kernel, dim3((unsigned)(works < 1 ? 1 : works < 148 ? works : 148)), dim3(kThreads), smem_bytes<D>(), st, mk, mv, tk, tv, p);
+  launch_pdl(kernel, dim3((unsigned)(works < 1 ? 1 : works < 148 ? works : 148)), dim3(kThreads), smem_bytes<D>(), st, mk, mv, tk, tv, mq, p);
   return launch_status();
 }
 
