@@ -167,9 +167,6 @@ __device__ __forceinline__ void copy_of(bool dual, int tiles, int i, int& tile, 
     is_v = !(i & 1);
   }
 }
-__device__ __forceinline__ int copy_of_k(bool dual, int tiles, int t) { return !dual || tiles == 1 ? 2 * t : t == 0 ? 0 : 2 * t - 1; }
-__device__ __forceinline__ int copy_of_v(bool dual, int tiles, int t) { return !dual || tiles == 1 ? 2 * t + 1 : t == tiles - 1 ? 2 * tiles - 1 : 2 * t + 2; }
-
 // Keys of the sequence, or nodes, in a tile of 128.
 __device__ __forceinline__ int keys_there(const Work& w, int tile, bool own) { return own ? w.it.nodes : w.it.n_keys - tile * kKeys; }
 
@@ -223,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = tmem + ((uint32_t)((warp % 4) * 32) << 16), s_tm = lanes + s * 128, o_tm = lanes + 256 + s * D;
     const int r_q = r / p.g, r_head = r % p.g;
     const uint64_t scale2x = pack2(p.scale2, p.scale2);
-    uint32_t n_s = 0, n_pair = 0;  // tiles of keys done, meetings of the eight warps
+    uint32_t n_s = 0, n_o = 0, n_pair = 0;  // tiles of keys done, meetings of the eight warps
     auto meet = [&] {
       __syncwarp();
       if (lane == 0) mbar_arrive(&sb.pair);
@@ -267,32 +264,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int c = 0; c < kKeys; ++c)
               if (c >= left) z[c] = 0xff800000u;
           }
-          for (bool again = look;; again = true) {
-            if (again) {
-              float top[2] = {m, -INFINITY};
-#pragma unroll
-              for (int c = 0; c < kKeys; c += 4) {
-                top[0] = max3f(top[0], __uint_as_float(z[c]), __uint_as_float(z[c + 1]));
-                top[1] = max3f(top[1], __uint_as_float(z[c + 2]), __uint_as_float(z[c + 3]));
-              }
-              const float now = fmaxf(top[0], top[1]), f = m == -INFINITY ? 0.f : ex2((m - now) * p.scale2);
-              l *= f;
-              m = now;
-              look = __any_sync(0xffffffffu, m == -INFINITY);
-              // (S of this tile has arrived, so the product before it, which was issued before, is done)
-              if (!first) {
-#pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                  uint32_t o[16];
-                  tmem_ld16(o_tm + c, o);
-                  tmem_wait_ld();
-                  tie16(o);
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                  tmem_st16(o_tm + c, o);
-                }
-              }
-            }
+          // weights of the tile to where the product reads them; their sum is good where they were taken against a fit reference
+          auto weights = [&](auto) {
             const float off = m == -INFINITY ? 0.f : -m * p.scale2;
             const uint64_t off2 = pack2(off, off);
             uint64_t sum[2] = {0, 0};
@@ -312,12 +285,37 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             float lo, hi;
             unpack2(add2(sum[0], sum[1]), lo, hi);
-            lo += hi;
-            if (again || !__any_sync(0xffffffffu, lo > kMostSum)) {
-              l += lo;
-              break;
+            return lo + hi;
+          };
+          float part = 0.f;
+          if (!look) part = weights(std::false_type());
+          if (look || !__all_sync(0xffffffffu, part <= kMostSum || !valid)) {
+            float top[2] = {m, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < kKeys; c += 4) {
+              top[0] = max3f(top[0], __uint_as_float(z[c]), __uint_as_float(z[c + 1]));
+              top[1] = max3f(top[1], __uint_as_float(z[c + 2]), __uint_as_float(z[c + 3]));
             }
+            const float now = fmaxf(top[0], top[1]), f = m == -INFINITY ? 0.f : ex2((m - now) * p.scale2);
+            l *= f;
+            m = now;
+            look = __any_sync(0xffffffffu, valid && m == -INFINITY);
+            // (S of this tile has arrived, so the product before it, which was issued before, is done)
+            if (!first) {
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tmem_ld16(o_tm + c, o);
+                tmem_wait_ld();
+                tie16(o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st16(o_tm + c, o);
+              }
+            }
+            part = weights(std::true_type());
           }
+          l += part;
           tmem_wait_st();
         }
         tc_fence_before();
@@ -326,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++n_s;
       }
       // ---- results ----
-      if (some) wait.all(&sb.o_done[s], (n_s - 1) & 1, kSiteDrain);
+      if (some) wait.all(&sb.o_done[s], n_o++ & 1, kSiteDrain);
       tc_fence_after();
       float f0 = 1.f, f1 = 0.f;  // factors of this thread's row in the accumulators that it reads
       if (dual) {
@@ -435,54 +433,101 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 8) {
       // ---- matrix products: one thread ----------------------------------------------------------------------------------
       if (elect_one()) {
+        // This thread's chain (weights there -> their product -> the next S) is a row's too: stages are waited for ahead of the weights, and
+        // where they are is counted, not worked out.
         constexpr uint32_t kQk = instr_desc_bf16(kKeys), kPv = instr_desc_pv(D);
-        uint32_t seq = 0, n_p[2] = {0, 0}, n_q = 0;
+        uint32_t cur = 0, cur_phase = 0, n_p0 = 0, n_p1 = 0, n_q = 0;
+        const uint32_t q_desc = smem_desc_lo(q_smem), ring_desc = smem_desc_lo(ring_smem), v_desc = v_desc_lo(ring_smem);
+        struct Stage {
+          uint32_t st, phase;
+        };
+        auto next_stage = [&] {
+          const Stage at{cur, cur_phase};
+          if (++cur == NST) cur = 0, cur_phase ^= 1;
+          return at;
+        };
+        auto landed = [&](Stage g) { return wait(&sb.full[g.st], g.phase, kSiteFull); };
+        auto logits = [&](auto slot, uint32_t q, Stage g) {
+          const uint32_t k = ring_desc + g.st * (TILE >> 4);
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const uint32_t at = (i / 4) * (BLOCK >> 4) + (i % 4) * 2;
+            umma_bf16(tmem + slot.value * 128, q + at, k + at, kQk, i > 0);
+          }
+          umma_commit(&sb.s_full[slot.value]);
+        };
+        auto results = [&](auto slot, uint32_t& n_p, Stage g, bool begun) {
+          const uint32_t v = v_desc + g.st * (TILE >> 4);
+          if (!wait(&sb.p_full[slot.value], n_p & 1, kSiteTEmpty)) return false;
+          ++n_p;
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < kKeys / 16; ++i)
+            umma_bf16_ts(tmem + 256 + slot.value * D, tmem + slot.value * 128 + i * 8, v + i * (16 * 128 >> 4), kPv, begun || i > 0);
+          return true;
+        };
+        using Slot0 = std::integral_constant<int, 0>;
+        using Slot1 = std::integral_constant<int, 1>;
         for (uint32_t round = 0;; ++round) {
           const Work& w = sb.ring[round % kRing];
           if (!wait(&sb.item_full[round % kRing], round / kRing & 1, kSiteQFull) || !w.valid) break;
           const bool dual = w.dual;
-          const int tiles = w.end - w.begin, n0 = dual ? tiles : w.end0 - w.begin;
-          const int steps = dual ? tiles : 2 * tiles;
+          const int tiles = w.end - w.begin, n0 = w.end0 - w.begin;
           mbar_arrive(&sb.item_empty[round % kRing]);
           if (tiles == 0) continue;
           if (!wait(&sb.q_full, n_q++ & 1, kSiteQFull)) break;
-          for (int x = 0; x <= steps; ++x) {
-            if (x < steps) {  // S of step x
-              const int s = x & 1, t = dual ? x : x / 2;
-              const uint32_t n = seq + copy_of_k(dual, tiles, t), st = n % NST;
-              if (dual || s || t < n0) {
-                if (!wait(&sb.full[st], n / NST & 1, kSiteFull)) break;
-                tc_fence_after();
-                const uint32_t a = smem_desc_lo(q_smem + (dual ? 0 : s) * TILE), b = smem_desc_lo(ring_smem + st * TILE);
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                  const uint32_t at = (k / 4) * (BLOCK >> 4) + (k % 4) * 2;
-                  umma_bf16(tmem + s * 128, a + at, b + at, kQk, k > 0);
-                }
-                umma_commit(&sb.s_full[s]);
-              }
-              if (dual || s) umma_commit(&sb.empty[st]);
-              if (x == steps - 1) umma_commit(&sb.q_empty);
+          if (dual) {
+            auto begin = [&](auto slot) {
+              const Stage k = next_stage();
+              if (!landed(k)) return;
+              tc_fence_after();
+              logits(slot, q_desc, k);
+              umma_commit(&sb.empty[k.st]);
+            };
+            begin(Slot0());
+            if (tiles > 1) begin(Slot1());
+            if (tiles <= 2) umma_commit(&sb.q_empty);
+            auto step = [&](auto slot, uint32_t& n_p, int t) {
+              const bool more = t + 2 < tiles;
+              const Stage v = next_stage(), k = more ? next_stage() : v;
+              if (!landed(v) || (more && !landed(k)) || !results(slot, n_p, v, t >= 2)) return false;
+              if (more) logits(slot, q_desc, k);
+              if (!more) umma_commit(&sb.o_done[slot.value]);
+              umma_commit(&sb.empty[v.st]);
+              if (more) umma_commit(&sb.empty[k.st]);
+              if (t + 3 == tiles) umma_commit(&sb.q_empty);
+              return true;
+            };
+            for (int t = 0; t < tiles; t += 2) {
+              if (!step(Slot0(), n_p0, t)) break;
+              if (t + 1 < tiles && !step(Slot1(), n_p1, t + 1)) break;
             }
-            if (x > 0) {  // O of step x - 1
-              const int y = x - 1, s = y & 1, t = dual ? y : y / 2;
-              const uint32_t n = seq + copy_of_v(dual, tiles, t), st = n % NST;
-              if (dual || s || t < n0) {
-                if (!wait(&sb.full[st], n / NST & 1, kSiteFull) || !wait(&sb.p_full[s], n_p[s] & 1, kSiteTEmpty)) break;
-                ++n_p[s];
-                tc_fence_after();
-                const uint32_t b = v_desc_lo(ring_smem + st * TILE);
-                const bool begun = dual ? y >= 2 : t > 0;
-#pragma unroll
-                for (int k = 0; k < kKeys / 16; ++k)
-                  umma_bf16_ts(tmem + 256 + s * D, tmem + s * 128 + k * 8, b + k * (16 * 128 >> 4), kPv, begun || k > 0);
-                umma_commit(&sb.o_done[s]);
-              }
-              if (dual || s) umma_commit(&sb.empty[st]);
+          } else {
+            const uint32_t q1 = q_desc + (TILE >> 4);
+            Stage k = next_stage();
+            if (!landed(k)) break;
+            tc_fence_after();
+            if (n0 > 0) logits(Slot0(), q_desc, k);
+            logits(Slot1(), q1, k);
+            umma_commit(&sb.empty[k.st]);
+            if (tiles == 1) umma_commit(&sb.q_empty);
+            for (int t = 0; t < tiles; ++t) {
+              const bool more = t + 1 < tiles;
+              const Stage v = next_stage();
+              if (more) k = next_stage();
+              if (!landed(v) || (more && !landed(k))) break;
+              if (t < n0 && !results(Slot0(), n_p0, v, t > 0)) break;
+              if (t + 1 < n0) logits(Slot0(), q_desc, k);
+              if (t + 1 == n0) umma_commit(&sb.o_done[0]);
+              if (!results(Slot1(), n_p1, v, t > 0)) break;
+              if (more) logits(Slot1(), q1, k);
+              if (!more) umma_commit(&sb.o_done[1]);
+              umma_commit(&sb.empty[v.st]);
+              if (more) umma_commit(&sb.empty[k.st]);
+              if (t + 2 == tiles) umma_commit(&sb.q_empty);
             }
           }
           if (wait.dead) break;
-          seq += 2 * tiles;
         }
         if (wait.dead) {  // products in flight end before the block does
           umma_commit(&sb.drain);
