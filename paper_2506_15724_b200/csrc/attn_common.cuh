@@ -45,6 +45,7 @@ struct AttnParams {
   unsigned* counter;
   int slots, min_tiles;
   int tile_q;          // queries of an item
+  int tile_rows;       // rows of an item at most
   int64_t n_items;     // items (without slots) at most
   int q_tiles;         // tree: tiles of a unit's rows
   void* ws;
@@ -222,13 +223,15 @@ inline void attn_items(AttnParams& p, bool tree) {
   p.n_items = (p.q_off && packed < tiles ? packed : tiles) * p.Hkv;
 }
 // Shares of the keys: as many as give `blocks` blocks, of at least min_tiles tiles of tile_keys keys by the longest sequence or the mean
-// segment. (blocks * p.tile_q * p.g is at most kAttnPartRows.)
+// segment, and no more than there is room for their results.
 inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int tile_keys, int blocks, int min_tiles) {
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, longest = (int64_t)c.max_seq_len + c.max_new_tokens;
   const int64_t keys = !tree ? (p.k_rows < p.n_max ? p.k_rows : p.n_max) : p.capacity / units < longest ? p.capacity / units : longest;
+  p.tile_rows = (int)(p.tile_q < p.q_rows ? p.tile_q : p.q_rows) * p.g;
   int64_t slots = p.n_items ? blocks / p.n_items : 1;
-  const int64_t by_keys = (keys / tile_keys + min_tiles) / min_tiles;
+  const int64_t by_keys = (keys / tile_keys + min_tiles) / min_tiles, by_room = p.n_items ? kAttnPartRows / (p.n_items * p.tile_rows) : 1;
   if (slots > by_keys) slots = by_keys;
+  if (slots > by_room) slots = by_room;
   if (slots > kAttnSlots) slots = kAttnSlots;
   if (slots < 1 || p.n_items > kCounters) slots = 1;
   p.slots = (int)slots;

@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
     }
     return;
   }
-  auto part_row = [&](int x, int r) { return (y * p.slots + x) * (p.tile_q * p.g) + r; };
+  auto part_row = [&](int x, int r) { return (y * p.slots + x) * p.tile_rows + r; };
   if (slot < nb) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int c_begin = dual ? s * (D / 2) : 0, c_end = dual ? c_begin + D / 2 : D;
       const bool split = w.nb > 1;
       const float norm = split ? 1.f : row_factor(l);
-      const int64_t row = (w.y * p.slots + w.slot) * (p.tile_q * p.g) + mt * tok_m * p.g + r;
+      const int64_t row = (w.y * p.slots + w.slot) * p.tile_rows + mt * tok_m * p.g + r;
       __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)t * p.so.token + r_head * p.so.head;
       if (active && !wait.dead) {
 #pragma unroll 1
@@ -400,27 +400,57 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (threadIdx.x == 0 && !wait.dead) sb.last = arrive_inc(p.counter + w.y, (unsigned)w.nb - 1u);  // (wraps to 0: ready for the next call)
         meet();
         if (!wait.dead && sb.last == (unsigned)w.nb - 1u) {
-          constexpr int C4 = D / 4;
-          const int rows = (w.tok0 + w.tok1) * p.g, tile_rows = p.tile_q * p.g;
-          const int64_t first = w.y * p.slots * tile_rows;
-          for (int x = threadIdx.x; x < rows * C4; x += 256) {
-            const int rr = x / C4, c = x % C4 * 4;
-            float top = -INFINITY, sum = 0.f;
-            for (int i = 0; i < w.nb; ++i) top = fmaxf(top, __ldcg(p.part_ml + first + i * tile_rows + rr).x);
-            const float at = top == -INFINITY ? 0.f : top;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int i = 0; i < w.nb; ++i) {
-              const float2 ml = __ldcg(p.part_ml + first + i * tile_rows + rr);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + (first + i * tile_rows + rr) * D + c));
-              const float f = ml.x == -INFINITY && ml.y == ml.y ? 0.f : ex2((ml.x - at) * p.scale2);
-              sum += ml.y * f;
-              o.x += v.x * f, o.y += v.y * f, o.z += v.z * f, o.w += v.w * f;
+          // A warp joins four rows at a time, a lane has V columns of each. (A thread to a piece of a row, all shares' statistics read by
+          // each: 60 us for 4 items of 112 rows and 9 shares.)
+          constexpr int V = D / 32, R = 4;
+          using Piece = std::conditional_t<V == 4, float4, float2>;
+          const int rows = (w.tok0 + w.tok1) * p.g;
+          const int64_t first = w.y * p.slots * p.tile_rows;
+          for (int r0 = warp * R; r0 < rows; r0 += 8 * R) {
+            float top[R], fac[R], sum[R], acc[R][V];
+            float2 ml[R];
+#pragma unroll
+            for (int q = 0; q < R; ++q)
+              ml[q] = lane < w.nb && r0 + q < rows ? __ldcg(p.part_ml + first + lane * p.tile_rows + r0 + q) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+              top[q] = warp_max(ml[q].x);
+              fac[q] = ex2((ml[q].x - (top[q] == -INFINITY ? 0.f : top[q])) * p.scale2);
+              sum[q] = ml[q].y * fac[q];
+#pragma unroll
+              for (int i = 16; i >= 1; i >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], i);
+#pragma unroll
+              for (int i = 0; i < V; ++i) acc[q][i] = 0.f;
             }
-            const float z = row_factor(sum);
-            const int tt = it.q0 + rr / p.g, j = rr % p.g;
-            __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)tt * p.so.token + j * p.so.head + c;
-            *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(o.x * z, o.y * z), pack_bf16x2(o.z * z, o.w * z));
-            if (c == 0) finish(tt, j, row_lse(top * p.scale2, sum));
+            for (int i0 = 0; i0 < w.nb; i0 += 4) {
+              Piece v[4][R];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < R; ++q)
+                  v[i][q] = i0 + i < w.nb && r0 + q < rows
+                                ? __ldcg(reinterpret_cast<const Piece*>(p.part + (first + (i0 + i) * p.tile_rows + r0 + q) * D) + lane)
+                                : Piece();
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                  const float f = __shfl_sync(0xffffffffu, fac[q], (i0 + i) & 31);
+                  if (i0 + i >= w.nb) continue;
+#pragma unroll
+                  for (int e = 0; e < V; ++e) acc[q][e] += reinterpret_cast<const float*>(&v[i][q])[e] * f;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+              const int tt = it.q0 + (r0 + q) / p.g, j = (r0 + q) % p.g;
+              if (r0 + q >= rows) break;
+              const float z = row_factor(sum[q]);
+              uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)tt * p.so.token + j * p.so.head) + lane * (V / 2);
+#pragma unroll
+              for (int e = 0; e < V; e += 2) to[e / 2] = pack_bf16x2(acc[q][e] * z, acc[q][e + 1] * z);
+              if (lane == q) finish(tt, j, row_lse(top[q] * p.scale2, sum[q]));
+            }
           }
         }
       }
@@ -723,7 +753,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   const void* q = kTree && !all ? (const char*)p.q + p.layer * p.sq.layer * 2 : p.q;
   if (!make_query_map(&mq, q, D, p.g, p.q_rows, p.Hkv, outer, all && p.L > 1 ? p.sq.layer : p.sq.batch, p.sq, p.tile_q / 2)) return -1;
   attn_items(p, kTree);
-  attn_slots(p, c, kTree, kKeys, 148, 2);
+  attn_slots(p, c, kTree, kKeys, 2 * 148, 4);
   p.wait_clocks = kWaitCycles;
   // Failure-path test (no GPU fault involved), as in decode attention: the copies are withheld, waits are bounded to that many clocks.
   if (const char* e = getenv("MADAKV_TEST_HOLD_COPIES")) {
@@ -732,8 +762,10 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   }
   auto kernel = attn_tc_kernel<D, kTree>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()) != cudaSuccess) return MADAKV_ECUDA;
-  const int64_t works = p.n_items * p.slots;
-  launch_pdl(kernel, dim3((unsigned)(works < 1 ? 1 : works < 148 ? works : 148)), dim3(kThreads), smem_bytes<D>(), st, mk, mv, tk, tv, mq, p);
+  // (few works: as many blocks as all get the same number of them)
+  const int64_t works = p.n_items * p.slots, each = p.slots > 1 ? (works + 147) / 148 : 1;
+  const int64_t blocks = (works + each - 1) / each;
+  launch_pdl(kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < 148 ? blocks : 148)), dim3(kThreads), smem_bytes<D>(), st, mk, mv, tk, tv, mq, p);
   return launch_status();
 }
 

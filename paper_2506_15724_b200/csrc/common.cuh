@@ -31,7 +31,7 @@ constexpr int kScoreChunk = 1024;   // keys per (max, sum) partial of the generi
 constexpr int kScoreTcChunk = 512;  // keys per work item (and per partial) of the tensor-core scoring path
 constexpr int kCounters = 16384;
 constexpr int kDecodeChunk = 256;   // cache rows per split of decode attention
-constexpr int kAttnPartRows = 148 * 256;  // rows of partial results of prompt and tree attention: a tile of 256 for every SM
+constexpr int kAttnPartRows = 2 * 148 * 256;  // rows of partial results of prompt and tree attention: two tiles of 256 for every SM
 
 struct WsHeader {
   int32_t status;        // madakv_status set by device code
