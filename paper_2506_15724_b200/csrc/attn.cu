@@ -13,6 +13,7 @@ AttnParams base_params(const madakv_config& c, int layer, void* ws) {
   p.Hq = c.n_q_heads;
   p.Hkv = c.n_kv_heads;
   p.g = c.n_q_heads / c.n_kv_heads;
+  p.g_inverse = (65536 + p.g - 1) / p.g;
   p.layer = layer;
   p.causal = c.causal;
   p.w = c.window;

@@ -46,7 +46,9 @@ struct AttnParams {
   int slots, min_tiles;
   int tile_q;          // queries of an item
   int tile_rows;       // rows of an item at most
-  int64_t n_items;     // items (without slots) at most
+  int g_inverse;       // 2^16 / g, rounded up
+  int wide_q, wide_out;  // rows begin on 32-byte boundaries
+  int64_t n_items;     // items (without slots) at most; items times slots are fewer than 2^31
   int q_tiles;         // tree: tiles of a unit's rows
   void* ws;
   int hold_copies;        // test of waits that run out: no tile of keys is copied
@@ -65,6 +67,9 @@ struct AttnItem {
   int64_t k_at, v_at;       // elements: prompt: key 0 of the head; tree: node 0 of the head
   int64_t key_row;          // first key: prompt: row of the token dimension; tree: row of the cache
 };
+
+// Row r of a tile (fewer than 512) belongs to query r / g: exact, because r times what the inverse is rounded up by stays below 2^16.
+__device__ __forceinline__ int group_of(const AttnParams& p, int r) { return r * p.g_inverse >> 16; }
 
 // ---- prompts -------------------------------------------------------------------------------------------------------------
 // Keys and queries of sequence b. Lengths outside their range are used as the nearest bound; a stretch of rows that is not one (its
@@ -85,25 +90,31 @@ __device__ __forceinline__ int prompt_queries(const AttnParams& p, int b, int ke
 // that the long items are under way when the short ones fill the gaps. All lanes of a warp call this for item i and get the
 // same answer; false: there are no more items. Level t holds the sequences with more than t tiles; at_least(t) counts the tiles of
 // level t and above.
-__device__ __forceinline__ bool find_prompt_tile(const AttnParams& p, int64_t i, int& b_out, int& tile_out) {
+__device__ __forceinline__ bool find_prompt_tile(const AttnParams& p, unsigned i, int& b_out, int& tile_out) {
   const int lane = threadIdx.x & 31;
   auto tiles_of = [&](int b) {
     if (b >= p.B) return 0;
     return (prompt_queries(p, b, p.q_off || p.q_len ? 0 : prompt_keys(p, b)) + p.tile_q - 1) / p.tile_q;
   };
+  if (p.B == 1) {
+    const int n = tiles_of(0);
+    b_out = 0;
+    tile_out = n - 1 - (int)i;
+    return i < (unsigned)n;
+  }
   const int first = tiles_of(lane);
   auto at_least = [&](int t) {
     unsigned n = (unsigned)max(0, first - t);
     for (int b = lane + 32; b < p.B; b += 32) n += (unsigned)max(0, tiles_of(b) - t);
-    return (int64_t)__reduce_add_sync(0xffffffffu, n);
+    return __reduce_add_sync(0xffffffffu, n);
   };
   if (i >= at_least(0)) return false;
-  int lo = 0, hi = (int)((min(p.q_rows, (int64_t)p.n_max) + p.tile_q - 1) / p.tile_q);  // at_least(lo) > i >= at_least(hi) = 0
+  int lo = 0, hi = ((int)min(p.q_rows, (int64_t)p.n_max) + p.tile_q - 1) / p.tile_q;  // at_least(lo) > i >= at_least(hi) = 0
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
     if (at_least(mid) > i) lo = mid; else hi = mid;
   }
-  int64_t r = i - at_least(lo + 1);
+  int r = (int)(i - at_least(lo + 1));
   for (int b0 = 0; b0 < p.B; b0 += 32) {
     const unsigned in = __ballot_sync(0xffffffffu, (b0 ? tiles_of(b0 + lane) : first) > lo);
     if (r < __popc(in)) {
@@ -118,10 +129,10 @@ __device__ __forceinline__ bool find_prompt_tile(const AttnParams& p, int64_t i,
   return false;
 }
 
-__device__ __forceinline__ bool prompt_item(const AttnParams& p, int64_t i, AttnItem& it) {
+__device__ __forceinline__ bool prompt_item(const AttnParams& p, unsigned i, AttnItem& it) {
   int tile;
-  it.h = (int)(i % p.Hkv);
-  if (!find_prompt_tile(p, i / p.Hkv, it.b, tile)) return false;
+  it.h = (int)(i % (unsigned)p.Hkv);
+  if (!find_prompt_tile(p, i / (unsigned)p.Hkv, it.b, tile)) return false;
   const int b = it.b;
   it.n_keys = prompt_keys(p, b);
   it.n_q = prompt_queries(p, b, it.n_keys);
@@ -154,15 +165,15 @@ __device__ __forceinline__ void fill_window(const AttnParams& p, int thread, int
 }
 
 // ---- trees ---------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ bool tree_item(const AttnParams& p, int64_t i, AttnItem& it) {
-  if (i >= p.n_items) return false;
-  const int y = (int)(i / p.q_tiles);
+__device__ __forceinline__ bool tree_item(const AttnParams& p, unsigned i, AttnItem& it) {
+  if (i >= (unsigned)p.n_items) return false;
+  const int y = (int)(i / (unsigned)p.q_tiles);
   const int u = p.layer < 0 ? y : (y / p.Hkv * p.L + p.layer) * p.Hkv + y % p.Hkv;
   const int bl = u / p.Hkv, b = bl / p.L, l = bl % p.L;
   it.unit = u;
   it.b = b;
   it.h = u % p.Hkv;
-  it.q0 = (int)(i % p.q_tiles) * p.tile_q;
+  it.q0 = (int)(i % (unsigned)p.q_tiles) * p.tile_q;
   const int T = (int)p.q_rows;
   it.nodes = it.n_q = p.n_nodes ? max(0, min(p.n_nodes[b], T)) : T;
   // a segment that selection refused, or whose length does not fit its slot, counts as empty, as in decode attention
@@ -191,8 +202,8 @@ __device__ __forceinline__ int shares_of(const AttnParams& p, int tiles) {
   return max(1, min(p.slots, (tiles + p.min_tiles - 1) / p.min_tiles));
 }
 __device__ __forceinline__ void share_tiles(int nb, int tiles, int x, int& begin, int& end) {
-  begin = (int)((int64_t)tiles * x / nb);
-  end = (int)((int64_t)tiles * (x + 1) / nb);
+  begin = tiles * x / nb;  // (at most 2^14 tiles, 2^5 shares)
+  end = tiles * (x + 1) / nb;
 }
 
 // Result of a row: o over its sum of weights l; a row without weight gets 0, one whose sum is not a number NaN.
@@ -233,6 +244,7 @@ inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int til
   if (slots > by_keys) slots = by_keys;
   if (slots > by_room) slots = by_room;
   if (slots > kAttnSlots) slots = kAttnSlots;
+  if (slots > 4) slots = slots / 4 * 4;  // (they are joined four at a time)
   if (slots < 1 || p.n_items > kCounters) slots = 1;
   p.slots = (int)slots;
   p.min_tiles = min_tiles;

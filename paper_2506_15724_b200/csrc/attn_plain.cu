@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
   constexpr int C4 = D / 4, CO = D / 64;  // float4 pieces of a row; float4 columns of a thread's results
   pdl_wait();
   pdl_go();
-  const int64_t y = blockIdx.x / p.slots;
+  const unsigned y = blockIdx.x / p.slots;
   const int slot = blockIdx.x % p.slots;
   if constexpr (!kTree) fill_window<D * (int)sizeof(T)>(p, threadIdx.x, NT);
   if (threadIdx.x < 32) {
@@ -208,9 +208,8 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float z = e == 0 ? w[i].x : e == 1 ? w[i].y : e == 2 ? w[i].z : w[i].w;
-              const float2 lo = halves(fma2(pair(z, z), pair(b.x, b.y), pair(o[i][c].x, o[i][c].y)));
-              const float2 hi = halves(fma2(pair(z, z), pair(b.z, b.w), pair(o[i][c].z, o[i][c].w)));
-              o[i][c] = make_float4(lo.x, lo.y, hi.x, hi.y);
+              o[i][c].x = fmaf(z, b.x, o[i][c].x), o[i][c].y = fmaf(z, b.y, o[i][c].y);
+              o[i][c].z = fmaf(z, b.z, o[i][c].z), o[i][c].w = fmaf(z, b.w, o[i][c].w);
             }
           }
       }
@@ -248,7 +247,7 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
     }
     return;
   }
-  auto part_row = [&](int x, int r) { return (y * p.slots + x) * p.tile_rows + r; };
+  auto part_row = [&](int x, int r) { return ((int64_t)y * p.slots + x) * p.tile_rows + r; };
   if (slot < nb) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -297,7 +296,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   p.tile_q = M / p.g;
   attn_items(p, kTree);
   if (p.n_items == 0) p.n_items = 1;  // (the window's missing rows are still filled)
-  attn_slots(p, c, kTree, N, 2 * 148, 4);
+  attn_slots(p, c, kTree, N, 2 * 148, 2);
   auto kernel = attn_plain_kernel<T, D, kTree>;
   if (p.n_items * p.slots > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>)) != cudaSuccess) return MADAKV_ECUDA;

@@ -31,7 +31,7 @@ struct Geo {
 
 struct Work {
   AttnItem it;
-  int64_t y;
+  unsigned y;
   int slot, nb;          // share of the keys, shares that take part
   int begin, end, end0;  // tiles of keys; where the first tile of rows stops
   int main_tiles;        // tiles of keys before the tree's own
@@ -144,6 +144,29 @@ __device__ __forceinline__ void tie32(uint32_t* r) { asm volatile("" : T8(r, 0),
 #undef R8
 #undef T8
 #undef I8
+// 32 bytes to or from global memory at once, or as two halves. (A thread has a row: what a warp's access takes is its lines, 32 each time,
+// so it goes by the number of accesses.)
+__device__ __forceinline__ void store32(void* to, const uint32_t* r, bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+                 "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+  }
+}
+__device__ __forceinline__ void load32(const void* from, uint32_t* r, bool wide) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "l"(from)
+                 : "memory");
+  } else {
+    const uint4 a = reinterpret_cast<const uint4*>(from)[0], b = reinterpret_cast<const uint4*>(from)[1];
+    r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w, r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
+  }
+}
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -218,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- weights and results -------------------------------------------------------------------------------------------
     const int s = warp / 4, r = (warp % 4) * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)((warp % 4) * 32) << 16), s_tm = lanes + s * 128, o_tm = lanes + 256 + s * D;
-    const int r_q = r / p.g, r_head = r % p.g;
+    const int r_q = group_of(p, r), r_head = r - r_q * p.g;
     const uint64_t scale2x = pack2(p.scale2, p.scale2);
     uint32_t n_s = 0, n_o = 0, n_pair = 0;  // tiles of keys done, meetings of the eight warps
     auto meet = [&] {
@@ -344,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int c_begin = dual ? s * (D / 2) : 0, c_end = dual ? c_begin + D / 2 : D;
       const bool split = w.nb > 1;
       const float norm = split ? 1.f : row_factor(l);
-      const int64_t row = (w.y * p.slots + w.slot) * p.tile_rows + mt * tok_m * p.g + r;
+      const int64_t row = ((int64_t)w.y * p.slots + w.slot) * p.tile_rows + mt * tok_m * p.g + r;
       __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)t * p.so.token + r_head * p.so.head;
       if (active && !wait.dead) {
 #pragma unroll 1
@@ -365,19 +388,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!valid) continue;
           if (split) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              __stcg(reinterpret_cast<uint4*>(p.part + row * D + c + i), make_uint4(a[i], a[i + 1], a[i + 2], a[i + 3]));
+            for (int i = 0; i < 32; i += 8) store32(p.part + row * D + c + i, a + i, true);
           } else {
             const bool none = !(l > 0.f || l != l);
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              uint4 v;
-              v.x = pack_bf16x2(__uint_as_float(a[i]), __uint_as_float(a[i + 1]));
-              v.y = pack_bf16x2(__uint_as_float(a[i + 2]), __uint_as_float(a[i + 3]));
-              v.z = pack_bf16x2(__uint_as_float(a[i + 4]), __uint_as_float(a[i + 5]));
-              v.w = pack_bf16x2(__uint_as_float(a[i + 6]), __uint_as_float(a[i + 7]));
-              *reinterpret_cast<uint4*>(dst + c + i) = none ? make_uint4(0, 0, 0, 0) : v;
-            }
+            for (int i = 0; i < 16; ++i) a[i] = none ? 0u : pack_bf16x2(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1]));
+            store32(dst + c, a, p.wide_out);
+            store32(dst + c + 16, a + 8, p.wide_out);
           }
         }
         if (valid && (!dual || s == 0)) {
@@ -387,10 +404,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto finish = [&](int tt, int j, float lse) {
         int64_t win;
         if (!store_row_lse(p, it, tt, j, lse, win)) return;
-        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) + it.q_at + tt * p.sq.token + j * p.sq.head);
-        uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.q_win) + win * D);
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) to[i] = src[i];
+        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.q) + it.q_at + tt * p.sq.token + j * p.sq.head;
+        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.q_win) + win * D;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 64) {
+          uint32_t x[32];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load32(src + c + 16 * i, x + 8 * i, p.wide_q);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) store32(to + c + 16 * i, x + 8 * i, p.wide_q);
+        }
       };
       if (!split && valid && (!dual || s == 0) && !wait.dead) finish(t, r_head, row_lse(m * p.scale2, l));
       tc_fence_before();
@@ -400,58 +423,71 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (threadIdx.x == 0 && !wait.dead) sb.last = arrive_inc(p.counter + w.y, (unsigned)w.nb - 1u);  // (wraps to 0: ready for the next call)
         meet();
         if (!wait.dead && sb.last == (unsigned)w.nb - 1u) {
-          // A warp joins four rows at a time, a lane has V columns of each. (A thread to a piece of a row, all shares' statistics read by
-          // each: 60 us for 4 items of 112 rows and 9 shares.)
-          constexpr int V = D / 32, R = 4;
+          // A warp joins R rows at a time, a lane has V of a row's columns; lane k keeps the sums of the warp's k-th row. Bound by the
+          // latency of what stands between a row's loads: with one row at a time and divisions 2250 clocks a row.
+          constexpr int V = D / 32, N = 4, R = 4;
           using Piece = std::conditional_t<V == 4, float4, float2>;
-          const int rows = (w.tok0 + w.tok1) * p.g;
-          const int64_t first = w.y * p.slots * p.tile_rows;
-          for (int r0 = warp * R; r0 < rows; r0 += 8 * R) {
-            float top[R], fac[R], sum[R], acc[R][V];
+          const int rows = (w.tok0 + w.tok1) * p.g, nb = w.nb, pitch = p.tile_rows;
+          const float2* ml_at = p.part_ml + (int64_t)w.y * p.slots * pitch + lane * pitch;
+          const Piece* part_at = reinterpret_cast<const Piece*>(p.part + (int64_t)w.y * p.slots * pitch * D) + lane;
+          float my_top = -INFINITY, my_sum = 0.f;
+#pragma unroll 1
+          for (int k = 0; warp + 8 * k < rows; k += R) {
             float2 ml[R];
+            Piece v[R][N];
+            auto ask = [&](int i0) {
 #pragma unroll
-            for (int q = 0; q < R; ++q)
-              ml[q] = lane < w.nb && r0 + q < rows ? __ldcg(p.part_ml + first + lane * p.tile_rows + r0 + q) : make_float2(-INFINITY, 0.f);
+              for (int q = 0; q < R; ++q)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                  const int r = warp + 8 * (k + q);
+                  v[q][i] = i0 + i < nb && r < rows ? __ldcg(part_at + ((i0 + i) * pitch + r) * 32) : Piece();
+                }
+            };
 #pragma unroll
             for (int q = 0; q < R; ++q) {
-              top[q] = warp_max(ml[q].x);
-              fac[q] = ex2((ml[q].x - (top[q] == -INFINITY ? 0.f : top[q])) * p.scale2);
-              sum[q] = ml[q].y * fac[q];
-#pragma unroll
-              for (int i = 16; i >= 1; i >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], i);
-#pragma unroll
-              for (int i = 0; i < V; ++i) acc[q][i] = 0.f;
+              const int r = warp + 8 * (k + q);
+              ml[q] = lane < nb && r < rows ? __ldcg(ml_at + r) : make_float2(-INFINITY, 0.f);
             }
-            for (int i0 = 0; i0 < w.nb; i0 += 4) {
-              Piece v[4][R];
+            ask(0);
+            float fac[R], sum[R], acc[R][V] = {};
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
+            for (int q = 0; q < R; ++q) {
+              const float top = warp_max(ml[q].x);
+              fac[q] = ex2((ml[q].x - (top == -INFINITY ? 0.f : top)) * p.scale2);
+              sum[q] = ml[q].y * fac[q];
+              if (lane == k + q) my_top = top;
+            }
 #pragma unroll
-                for (int q = 0; q < R; ++q)
-                  v[i][q] = i0 + i < w.nb && r0 + q < rows
-                                ? __ldcg(reinterpret_cast<const Piece*>(p.part + (first + (i0 + i) * p.tile_rows + r0 + q) * D) + lane)
-                                : Piece();
+            for (int i = 16; i >= 1; i >>= 1)
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
+              for (int q = 0; q < R; ++q) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], i);
+#pragma unroll 1
+            for (int i0 = 0; i0 < nb; i0 += N) {
+              if (i0) ask(i0);
+#pragma unroll
+              for (int i = 0; i < N; ++i)
 #pragma unroll
                 for (int q = 0; q < R; ++q) {
-                  const float f = __shfl_sync(0xffffffffu, fac[q], (i0 + i) & 31);
-                  if (i0 + i >= w.nb) continue;
+                  const float f = __shfl_sync(0xffffffffu, fac[q], i0 + i);
 #pragma unroll
-                  for (int e = 0; e < V; ++e) acc[q][e] += reinterpret_cast<const float*>(&v[i][q])[e] * f;
+                  for (int e = 0; e < V; ++e) acc[q][e] += reinterpret_cast<const float*>(&v[q][i])[e] * f;  // (0 times 0 beyond the last share)
                 }
             }
 #pragma unroll
             for (int q = 0; q < R; ++q) {
-              const int tt = it.q0 + (r0 + q) / p.g, j = (r0 + q) % p.g;
-              if (r0 + q >= rows) break;
+              const int r = warp + 8 * (k + q), tq = group_of(p, r);
+              if (lane == k + q) my_sum = sum[q];
               const float z = row_factor(sum[q]);
-              uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)tt * p.so.token + j * p.so.head) + lane * (V / 2);
+              uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (it.q0 + tq) * p.so.token + (r - tq * p.g) * p.so.head) + lane * (V / 2);
+              if (r < rows) {
 #pragma unroll
-              for (int e = 0; e < V; e += 2) to[e / 2] = pack_bf16x2(acc[q][e] * z, acc[q][e + 1] * z);
-              if (lane == q) finish(tt, j, row_lse(top[q] * p.scale2, sum[q]));
+                for (int e = 0; e < V; e += 2) to[e / 2] = pack_bf16x2(acc[q][e] * z, acc[q][e + 1] * z);
+              }
             }
           }
+          const int r = warp + 8 * lane, tq = group_of(p, r);
+          if (r < rows) finish(it.q0 + tq, r - tq * p.g, row_lse(my_top * p.scale2, my_sum));
         }
       }
       __syncwarp();
@@ -612,11 +648,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == 10) {
       // ---- the items: in rounds over the blocks, to and fro, so that every block gets its share of long ones ----------------
       uint32_t round = 0;
-      for (int64_t pass = 0;; ++pass) {
-        const int64_t g = gridDim.x, at = pass * g + (pass & 1 ? g - 1 - (int64_t)blockIdx.x : (int64_t)blockIdx.x);
+      for (unsigned pass = 0;; ++pass) {
+        const unsigned at = pass * gridDim.x + (pass & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         Work w;
-        w.y = at / p.slots;
-        w.slot = (int)(at % p.slots);
+        w.y = at / (unsigned)p.slots;
+        w.slot = (int)(at % (unsigned)p.slots);
         w.valid = kTree ? tree_item(p, w.y, w.it) : prompt_item(p, w.y, w.it);
         if (w.valid) {
           const AttnItem& it = w.it;
@@ -760,6 +796,12 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
     const long long v = atoll(e);
     if (v >= 100000 && v < kWaitCycles) p.hold_copies = 1, p.wait_clocks = v;
   }
+  if (p.n_items * p.slots > 0x7ffffff0ll) return MADAKV_EUNSUPPORTED;
+  auto wide = [](const void* x, const madakv_strides& t) {
+    return ((uintptr_t)x % 32 | t.batch * 2 % 32 | t.layer * 2 % 32 | t.head * 2 % 32 | t.token * 2 % 32) == 0;
+  };
+  p.wide_out = wide(p.out, p.so);
+  p.wide_q = wide(p.q, p.sq) && (uintptr_t)p.q_win % 32 == 0;
   auto kernel = attn_tc_kernel<D, kTree>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()) != cudaSuccess) return MADAKV_ECUDA;
   // (few works: as many blocks as all get the same number of them)
