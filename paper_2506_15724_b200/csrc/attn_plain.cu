@@ -64,7 +64,7 @@ struct Smem {
 };
 
 template <typename T, int D, bool kTree>
-__global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(NT, 2) attn_plain_kernel(const __grid_constant__ AttnParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
   using S = Smem<D>;
   S& sm = *reinterpret_cast<S*>(raw);
@@ -109,13 +109,13 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
       const int r = x / C4, c = x % C4 * 4;
       const bool there = r < rows;
       *reinterpret_cast<float4*>(sm.q + r * S::PITCH + c) =
-          load4(q + (there ? (int64_t)(it.q0 + r / p.g) * p.sq.token + (r % p.g) * p.sq.head + c : 0), there);
+          load4(q + (there ? (int64_t)(it.q0 + group_of(p, r)) * p.sq.token + (r - group_of(p, r) * p.g) * p.sq.head + c : 0), there);
     }
     int visible[4];  // keys that the thread's rows see
     uint64_t nodes[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = ty * 4 + i, t = it.q0 + r / p.g;
+      const int r = ty * 4 + i, t = it.q0 + group_of(p, r);
       visible[i] = r >= rows ? 0 : (kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, t + it.shift + 1)));
       nodes[i] = kTree && r < rows ? node_mask(p, it, t) : 0;
     }
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
       for (int x = 8; x >= 1; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
   }
   auto finish_row = [&](int r, float mm, float ll) {  // log-sum-exp and proxy query of a row, by 16 threads
-    const int t = it.q0 + r / p.g, j = r % p.g;
+    const int t = it.q0 + group_of(p, r), j = r - group_of(p, r) * p.g;
     int64_t win = 0;
     bool copy = false;
     if (tx == 0) copy = store_row_lse(p, it, t, j, row_lse(mm, ll), win);
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
       const int r = ty * 4 + i;
       if (r >= rows) continue;
       const float z = row_factor(l[i]);
-      T* dst = out + (int64_t)(it.q0 + r / p.g) * p.so.token + (r % p.g) * p.so.head;
+      T* dst = out + (int64_t)(it.q0 + group_of(p, r)) * p.so.token + (r - group_of(p, r) * p.g) * p.so.head;
 #pragma unroll
       for (int c = 0; c < CO; ++c)
         store4(dst + tx * 4 + 64 * c, make_float4(o[i][c].x * z, o[i][c].y * z, o[i][c].z * z, o[i][c].w * z));
@@ -263,31 +263,58 @@ __global__ void __launch_bounds__(NT) attn_plain_kernel(const __grid_constant__ 
   if (tid == 0) sm.last = arrive_inc(p.counter + y, (unsigned)p.slots - 1u);  // (wraps to 0: ready for the next call)
   __syncthreads();
   if (sm.last != (unsigned)p.slots - 1u) return;
+  // the shares' statistics by the 16 threads of a row, then their results two at a time
+  float fac[4][2], sum[4], top[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty * 4 + i;
+    float2 ml[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      ml[h] = r < rows && tx + 16 * h < nb ? __ldcg(p.part_ml + part_row(tx + 16 * h, r)) : make_float2(-INFINITY, 0.f);
+    top[i] = fmaxf(ml[0].x, ml[1].x);
+#pragma unroll
+    for (int x = 8; x >= 1; x >>= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+    const float base = top[i] == -INFINITY ? 0.f : top[i];
+    fac[i][0] = exp2f(ml[0].x - base);
+    fac[i][1] = exp2f(ml[1].x - base);
+    sum[i] = ml[0].y * fac[i][0] + ml[1].y * fac[i][1];
+#pragma unroll
+    for (int x = 8; x >= 1; x >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], x);
+#pragma unroll
+    for (int c = 0; c < CO; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+#pragma unroll 1
+  for (int x0 = 0; x0 < nb; x0 += 2) {
+    float4 z[2][4][CO];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < CO; ++c)
+          z[x][i][c] = x0 + x < nb && ty * 4 + i < rows
+                           ? __ldcg(reinterpret_cast<const float4*>(p.part + part_row(x0 + x, ty * 4 + i) * D + tx * 4 + 64 * c))
+                           : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float f = __shfl_sync(0xffffffffu, x0 + x < 16 ? fac[i][0] : fac[i][1], (tid & 16) + ((x0 + x) & 15));  // (0 beyond the last share)
+#pragma unroll
+        for (int c = 0; c < CO; ++c) o[i][c].x += z[x][i][c].x * f, o[i][c].y += z[x][i][c].y * f, o[i][c].z += z[x][i][c].z * f, o[i][c].w += z[x][i][c].w * f;
+      }
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = ty * 4 + i;
     if (r >= rows) continue;
-    float top = -INFINITY, sum = 0.f;
-    for (int x = 0; x < nb; ++x) top = fmaxf(top, __ldcg(p.part_ml + part_row(x, r)).x);
-    const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int c = 0; c < CO; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int x = 0; x < nb; ++x) {
-      const float2 ml = __ldcg(p.part_ml + part_row(x, r));
-      const float f = exp2f(ml.x - base);
-      sum += ml.y * f;
-#pragma unroll
-      for (int c = 0; c < CO; ++c) {
-        const float4 z = __ldcg(reinterpret_cast<const float4*>(p.part + part_row(x, r) * D + tx * 4 + 64 * c));
-        o[i][c].x += z.x * f, o[i][c].y += z.y * f, o[i][c].z += z.z * f, o[i][c].w += z.w * f;
-      }
-    }
-    const float z = row_factor(sum);
-    T* dst = out + (int64_t)(it.q0 + r / p.g) * p.so.token + (r % p.g) * p.so.head;
+    const float z = row_factor(sum[i]);
+    T* dst = out + (int64_t)(it.q0 + group_of(p, r)) * p.so.token + (r - group_of(p, r) * p.g) * p.so.head;
 #pragma unroll
     for (int c = 0; c < CO; ++c)
       store4(dst + tx * 4 + 64 * c, make_float4(o[i][c].x * z, o[i][c].y * z, o[i][c].z * z, o[i][c].w * z));
-    finish_row(r, top, sum);
+    finish_row(r, top[i], sum[i]);
   }
 }
 
