@@ -23,11 +23,9 @@ AttnParams base_params(const madakv_config& c, int layer, void* ws) {
   return p;
 }
 int launch(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st) {
-  if (c.dtype == MADAKV_BF16) {
-    const int rc = launch_attn_tc(p, c, tree, st);
-    if (rc >= 0) return rc;
-  }
-  return launch_attn_plain(p, c, tree, st);
+  if (c.dtype == MADAKV_F32) return launch_attn_split(p, c, tree, st);
+  const int rc = launch_attn_tc(p, c, tree, st);
+  return rc >= 0 ? rc : launch_attn_plain(p, c, tree, st);
 }
 
 }  // namespace

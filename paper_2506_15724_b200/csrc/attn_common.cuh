@@ -254,6 +254,7 @@ inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int til
 }
 
 int launch_attn_plain(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);
+int launch_attn_split(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);
 int launch_attn_tc(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);  // -1: its copies cannot take these strides
 
 }  // namespace madakv

@@ -1,4 +1,5 @@
-// Attention of a prompt and of drafted trees in fp32 arithmetic:
+// Attention of a prompt and of drafted trees with scalar fp32 arithmetic on bf16 rows, for strides that tensor copies cannot take (a
+// dimension of stride 0, layers and sequences that do not lie evenly):
 //   out = sum_i p_i v_i / sum_i p_i,  p_i = exp2(scale * log2(e) * q . k_i - m),  lse = (m + log2(sum_i p_i)) ln 2
 // with m the running maximum of the row's logits; sums and maxima are kept in fp32 and corrected when m grows, so one pass over
 // the keys is enough. A block has 64 rows and goes through its keys 64 at a time.
@@ -29,24 +30,15 @@ __device__ __forceinline__ float2 halves(uint64_t v) {
 }
 
 // Four elements of a row as fp32, or zeros.
-template <typename T>
+using T = __nv_bfloat16;
 __device__ __forceinline__ float4 load4(const T* src, bool there) {
   if (!there) return make_float4(0.f, 0.f, 0.f, 0.f);
-  if constexpr (sizeof(T) == 4) {
-    return *reinterpret_cast<const float4*>(src);
-  } else {
-    const uint2 x = *reinterpret_cast<const uint2*>(src);
-    return make_float4(bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y));
-  }
+  const uint2 x = *reinterpret_cast<const uint2*>(src);
+  return make_float4(bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y));
 }
-template <typename T>
 __device__ __forceinline__ void store4(T* dst, float4 v) {
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(dst) = v;
-  } else {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-    *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-  }
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
 template <int D>
@@ -63,7 +55,7 @@ struct Smem {
   unsigned last;
 };
 
-template <typename T, int D, bool kTree>
+template <int D, bool kTree>
 __global__ void __launch_bounds__(NT, 2) attn_plain_kernel(const __grid_constant__ AttnParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
   using S = Smem<D>;
@@ -318,13 +310,13 @@ __global__ void __launch_bounds__(NT, 2) attn_plain_kernel(const __grid_constant
   }
 }
 
-template <typename T, int D, bool kTree>
+template <int D, bool kTree>
 int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   p.tile_q = M / p.g;
   attn_items(p, kTree);
   if (p.n_items == 0) p.n_items = 1;  // (the window's missing rows are still filled)
   attn_slots(p, c, kTree, N, 2 * 148, 2);
-  auto kernel = attn_plain_kernel<T, D, kTree>;
+  auto kernel = attn_plain_kernel<D, kTree>;
   if (p.n_items * p.slots > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>)) != cudaSuccess) return MADAKV_ECUDA;
   launch_pdl(kernel, dim3((unsigned)(p.n_items * p.slots)), dim3(NT), sizeof(Smem<D>), st, p);
@@ -334,12 +326,8 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
 }  // namespace
 
 int launch_attn_plain(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st) {
-  auto go = [&](auto t) {
-    using T = decltype(t);
-    if (c.head_dim == 64) return tree ? run<T, 64, true>(p, c, st) : run<T, 64, false>(p, c, st);
-    return tree ? run<T, 128, true>(p, c, st) : run<T, 128, false>(p, c, st);
-  };
-  return c.dtype == MADAKV_F32 ? go(float()) : go(__nv_bfloat16());
+  if (c.head_dim == 64) return tree ? run<64, true>(p, c, st) : run<64, false>(p, c, st);
+  return tree ? run<128, true>(p, c, st) : run<128, false>(p, c, st);
 }
 
 }  // namespace madakv

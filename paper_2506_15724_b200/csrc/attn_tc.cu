@@ -14,8 +14,7 @@
 // The reference m that weights are taken against is the maximum of the row's first tile of keys. It stays, without a look at later
 // maxima, until a tile's weights add up to more than 2^16; only then the tile is done again with its maximum, and O and the sum are scaled down. bf16
 // weights and fp32 sums have the range for it, relative errors are the same, and numerator and denominator share the factor.
-#include "attn_common.cuh"
-#include "tc_common.cuh"
+#include "attn_tmem.cuh"
 
 namespace madakv {
 namespace {
@@ -55,36 +54,6 @@ constexpr int smem_bytes() {
 }
 static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
 
-// What a role waits with: bounded; once a wait has run out, here or in another role, everything that follows returns at once. A
-// single thread calls it; warps call all(), which all lanes leave together and with the same answer (instructions that take a whole
-// warp follow).
-struct Waiter {
-  volatile int* abort;
-  int32_t* status;
-  long long limit;
-  bool dead = false;
-  __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity, int site) {
-    if (dead) return false;
-    if (mbar_try(bar, parity)) return true;
-    const long long t0 = clock64();
-    int spins = 0;
-    while (!mbar_try(bar, parity)) {
-      if ((++spins & 15) == 0) {
-        if (*abort) return dead = true, false;
-        if (clock64() - t0 > limit) {
-          give_up(abort, status, site);
-          return dead = true, false;
-        }
-      }
-    }
-    return true;
-  }
-  __device__ __forceinline__ bool all(uint64_t* bar, uint32_t parity, int site) {
-    if (!__all_sync(0xffffffffu, (*this)(bar, parity, site))) dead = true;
-    return !dead;
-  }
-};
-
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
@@ -97,81 +66,10 @@ __device__ __forceinline__ void tma_load_5d_plain(uint32_t dst, const CUtensorMa
       "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
       : "memory");
 }
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-// A from tensor memory, B from shared memory.
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_desc_lo, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 db;\nsetp.ne.b32 p, %4, 0;\nmov.b64 db, {%2, %5};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}" ::"r"(d_tmem),
-      "r"(a_tmem), "r"(b_desc_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
-      : "memory");
-}
 // Descriptor of V as the operand whose rows are the contraction: 64 columns (128 bytes) by 8 keys are 1024 bytes, swizzled; the next
 // 8 keys follow 1024 bytes on (the stride offset, as for the other operands), the next 64 columns a block of 128 keys on.
 __device__ __forceinline__ uint32_t v_desc_lo(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((uint32_t)(kKeys * 128 >> 4) << 16); }
 __host__ __device__ constexpr uint32_t instr_desc_pv(int n) { return instr_desc_bf16(n) | (1u << 16); }
-
-#define R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
-#define T8(r, o) "+r"(r[o]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7])
-#define I8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
-// 32 columns of a warp's lanes; valid behind tmem_wait and tie.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
-      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24)
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : R8(r, 0), R8(r, 8)
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::I8(r, 0),
-      I8(r, 8), "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tie16(uint32_t* r) { asm volatile("" : T8(r, 0), T8(r, 8) : : "memory"); }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tie32(uint32_t* r) { asm volatile("" : T8(r, 0), T8(r, 8), T8(r, 16), T8(r, 24) : : "memory"); }
-#undef R8
-#undef T8
-#undef I8
-// 32 bytes to or from global memory at once, or as two halves. (A thread has a row: what a warp's access takes is its lines, 32 each time,
-// so it goes by the number of accesses.)
-__device__ __forceinline__ void store32(void* to, const uint32_t* r, bool wide) {
-  if (wide) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
-                 "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-  } else {
-    reinterpret_cast<uint4*>(to)[0] = make_uint4(r[0], r[1], r[2], r[3]);
-    reinterpret_cast<uint4*>(to)[1] = make_uint4(r[4], r[5], r[6], r[7]);
-  }
-}
-__device__ __forceinline__ void load32(const void* from, uint32_t* r, bool wide) {
-  if (wide) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "l"(from)
-                 : "memory");
-  } else {
-    const uint4 a = reinterpret_cast<const uint4*>(from)[0], b = reinterpret_cast<const uint4*>(from)[1];
-    r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w, r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
-  }
-}
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 
 // The tile that copy number i of an item brings, and whether it is V: as the products ask for them. K0 V0 K1 V1 ... where both tiles of
 // rows read every tile of keys; K0 K1 V0 K2 V1 ... where they take them in turn.
@@ -423,71 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (threadIdx.x == 0 && !wait.dead) sb.last = arrive_inc(p.counter + w.y, (unsigned)w.nb - 1u);  // (wraps to 0: ready for the next call)
         meet();
         if (!wait.dead && sb.last == (unsigned)w.nb - 1u) {
-          // A warp joins R rows at a time, a lane has V of a row's columns; lane k keeps the sums of the warp's k-th row. Bound by the
-          // latency of what stands between a row's loads: with one row at a time and divisions 2250 clocks a row.
-          constexpr int V = D / 32, N = 4, R = 4;
-          using Piece = std::conditional_t<V == 4, float4, float2>;
-          const int rows = (w.tok0 + w.tok1) * p.g, nb = w.nb, pitch = p.tile_rows;
-          const float2* ml_at = p.part_ml + (int64_t)w.y * p.slots * pitch + lane * pitch;
-          const Piece* part_at = reinterpret_cast<const Piece*>(p.part + (int64_t)w.y * p.slots * pitch * D) + lane;
-          float my_top = -INFINITY, my_sum = 0.f;
-#pragma unroll 1
-          for (int k = 0; warp + 8 * k < rows; k += R) {
-            float2 ml[R];
-            Piece v[R][N];
-            auto ask = [&](int i0) {
-#pragma unroll
-              for (int q = 0; q < R; ++q)
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                  const int r = warp + 8 * (k + q);
-                  v[q][i] = i0 + i < nb && r < rows ? __ldcg(part_at + ((i0 + i) * pitch + r) * 32) : Piece();
-                }
-            };
-#pragma unroll
-            for (int q = 0; q < R; ++q) {
-              const int r = warp + 8 * (k + q);
-              ml[q] = lane < nb && r < rows ? __ldcg(ml_at + r) : make_float2(-INFINITY, 0.f);
-            }
-            ask(0);
-            float fac[R], sum[R], acc[R][V] = {};
-#pragma unroll
-            for (int q = 0; q < R; ++q) {
-              const float top = warp_max(ml[q].x);
-              fac[q] = ex2((ml[q].x - (top == -INFINITY ? 0.f : top)) * p.scale2);
-              sum[q] = ml[q].y * fac[q];
-              if (lane == k + q) my_top = top;
-            }
-#pragma unroll
-            for (int i = 16; i >= 1; i >>= 1)
-#pragma unroll
-              for (int q = 0; q < R; ++q) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], i);
-#pragma unroll 1
-            for (int i0 = 0; i0 < nb; i0 += N) {
-              if (i0) ask(i0);
-#pragma unroll
-              for (int i = 0; i < N; ++i)
-#pragma unroll
-                for (int q = 0; q < R; ++q) {
-                  const float f = __shfl_sync(0xffffffffu, fac[q], i0 + i);
-#pragma unroll
-                  for (int e = 0; e < V; ++e) acc[q][e] += reinterpret_cast<const float*>(&v[q][i])[e] * f;  // (0 times 0 beyond the last share)
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < R; ++q) {
-              const int r = warp + 8 * (k + q), tq = group_of(p, r);
-              if (lane == k + q) my_sum = sum[q];
-              const float z = row_factor(sum[q]);
-              uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (it.q0 + tq) * p.so.token + (r - tq * p.g) * p.so.head) + lane * (V / 2);
-              if (r < rows) {
-#pragma unroll
-                for (int e = 0; e < V; e += 2) to[e / 2] = pack_bf16x2(acc[q][e] * z, acc[q][e + 1] * z);
-              }
-            }
-          }
-          const int r = warp + 8 * lane, tq = group_of(p, r);
-          if (r < rows) finish(it.q0 + tq, r - tq * p.g, row_lse(my_top * p.scale2, my_sum));
+          join_shares<__nv_bfloat16, D, 8>(p, it, w.y, w.nb, (w.tok0 + w.tok1) * p.g, p.scale2, warp, lane, finish);
         }
       }
       __syncwarp();
@@ -790,12 +624,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   if (!make_query_map(&mq, q, D, p.g, p.q_rows, p.Hkv, outer, all && p.L > 1 ? p.sq.layer : p.sq.batch, p.sq, p.tile_q / 2)) return -1;
   attn_items(p, kTree);
   attn_slots(p, c, kTree, kKeys, 2 * 148, 4);
-  p.wait_clocks = kWaitCycles;
-  // Failure-path test (no GPU fault involved), as in decode attention: the copies are withheld, waits are bounded to that many clocks.
-  if (const char* e = getenv("MADAKV_TEST_HOLD_COPIES")) {
-    const long long v = atoll(e);
-    if (v >= 100000 && v < kWaitCycles) p.hold_copies = 1, p.wait_clocks = v;
-  }
+  attn_waits(p);
   if (p.n_items * p.slots > 0x7ffffff0ll) return MADAKV_EUNSUPPORTED;
   auto wide = [](const void* x, const madakv_strides& t) {
     return ((uintptr_t)x % 32 | t.batch * 2 % 32 | t.layer * 2 % 32 | t.head * 2 % 32 | t.token * 2 % 32) == 0;

@@ -276,6 +276,42 @@ def test_prefill_bad_offsets_and_lengths(dtype):
     assert torch.equal(a, b) and not a[0].any() and a[1].all(dim=-1).all() and not a[2].any()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefill_one_key_head_for_all(dtype):
+    """Keys and values of one head, expanded over the others: a dimension of stride 0."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    n, d, H = 333, 128, 3
+    cfg = config(dtype, 1, 1, 2 * H, H, d, n)
+    q, k, v = normal(gen, (1, 1, 2 * H, n, d), dtype), normal(gen, (1, 1, 1, n, d), dtype), normal(gen, (1, 1, 1, n, d), dtype)
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 2 * H, n), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k.expand(1, 1, H, n, d), v.expand(1, 1, H, n, d), out, mk.new_workspace(cfg), lse_out=lse,
+                           seq_len=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    see = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+    for h in range(2 * H):
+        check(dtype, q[0, 0, h], k[0, 0, 0], v[0, 0, 0], see, d ** -0.5, out[0, 0, h], lse[0, 0, h])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefill_numbers_that_are_none(dtype):
+    """A NaN in a key is in the results of the queries that see it and of no other's; one in a query in that query's alone."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    n, d = 300, 64
+    cfg = config(dtype, 1, 1, 2, 1, d, n)
+    q, k, v = normal(gen, (1, 1, 2, n, d), dtype), normal(gen, (1, 1, 1, n, d), dtype), normal(gen, (1, 1, 1, n, d), dtype)
+    k[0, 0, 0, 170, 5] = math.nan
+    q[0, 0, 1, 40, 9] = math.nan
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 2, n), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    bad = torch.zeros((2, n), dtype=torch.bool, device="cuda")
+    bad[:, 170:] = True
+    bad[1, 40] = True
+    assert torch.equal(lse[0, 0].isnan(), bad) and torch.equal(out[0, 0].isnan(), bad.unsqueeze(2).expand(2, n, d))
+    see = torch.ones((170, 170), dtype=torch.bool, device="cuda").tril()
+    check(dtype, q[0, 0, 0, :170], k[0, 0, 0, :170], v[0, 0, 0, :170], see, d ** -0.5, out[0, 0, 0, :170], lse[0, 0, 0, :170])
+
+
 # ------------------------------------------------------------------------------------------------- drafted trees
 def tree_masks(rng, B, T, kind):
     """[B, T] masks as Python integers: of random trees, of any bits, or none."""
@@ -377,6 +413,51 @@ def test_tree_masks_and_node_counts(dtype, kind):
 def test_tree_long_segments(dtype, T, Hq, Hkv):
     """Few long segments: their rows are shared out over blocks."""
     tree(dtype, 1, 1, Hq, Hkv, 128, T, [9001, 4000, 17, 700], seed=T, spread=2.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tree_layers_that_do_not_lie_evenly(dtype):
+    """Queries of two of three layers: sequences and layers have strides of their own."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    B, L, H, T, d = 2, 2, 2, 5, 64
+    cfg = config(dtype, B, L, H, H, d, 150)
+    seg = Segments(gen, dtype, [130, 0, 77, 128, 20, 5, 140, 64], d)
+    q, k, v = (normal(gen, (B, L + 1, H, T, d), dtype)[:, 1:] for _ in range(3))
+    out, lse, ws = torch.zeros((B, L + 1, H, T, d), device="cuda").to(DT[dtype])[:, :2], torch.empty((B, L, H, T), device="cuda"), mk.new_workspace(cfg)
+    mk.madakv_tree_attn(cfg, -1, q, k, v, as_int64([[1, 3, 7, 15, 31]] * B), seg.k, seg.v, seg.seg_off, seg.kept_len, out, lse, ws)
+    for u, n in enumerate(seg.lens):
+        b, l, h, a = u // (L * H), u // H % L, u % H, seg.off[u]
+        see = torch.cat((torch.ones((T, n), device="cuda"), torch.ones((T, T), device="cuda").tril()), 1).bool()
+        check(dtype, q[b, l, h], torch.cat((seg.k[a:a + n], k[b, l, h])), torch.cat((seg.v[a:a + n], v[b, l, h])), see, d ** -0.5, out[b, l, h], lse[b, l, h], u)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_copies_that_never_come_end_in_a_status(dtype, monkeypatch):
+    """Copies of keys are withheld: every wait for them ends, the call reports it, and the next call on the workspace is whole."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    cfg = config(dtype, 2, 1, 8, 2, 128, 700, new=8)
+    ws, n = mk.new_workspace(cfg), torch.tensor([700, 300], dtype=torch.int32, device="cuda")
+    q, k, v = normal(gen, (2, 1, 8, 700, 128), dtype), normal(gen, (2, 1, 2, 700, 128), dtype), normal(gen, (2, 1, 2, 700, 128), dtype)
+    seg = Segments(gen, dtype, [500, 31, 700, 129], 128, headroom=8)
+    qt, kt, mask = normal(gen, (2, 1, 8, 5, 128), dtype), normal(gen, (2, 1, 2, 5, 128), dtype), as_int64([[1, 3, 5, 9, 17]] * 2)
+    outs = [torch.zeros_like(q), torch.zeros_like(qt)]
+
+    def calls():
+        mk.madakv_prefill_attn(cfg, 0, q, k, v, outs[0], ws, seq_len=n)
+        first = mk.madakv_poll_status(ws)
+        mk.madakv_tree_attn(cfg, -1, qt, kt, kt, mask, seg.k, seg.v, seg.seg_off, seg.kept_len, outs[1], None, ws)
+        return first, mk.madakv_poll_status(ws)
+
+    assert calls() == (0, 0)
+    want = [x.clone() for x in outs]
+    monkeypatch.setenv("MADAKV_TEST_HOLD_COPIES", "200000")
+    assert calls() == (mk.ETIMEOUT, mk.ETIMEOUT)
+    monkeypatch.delenv("MADAKV_TEST_HOLD_COPIES")
+    ws.zero_()  # (shares that were given up have not arrived at their counters)
+    assert calls() == (0, 0)
+    assert all(torch.equal(x, y) for x, y in zip(outs, want))
 
 
 @pytest.mark.gpu
