@@ -485,10 +485,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (unsigned pass = 0;; ++pass) {
         const unsigned at = pass * gridDim.x + (pass & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         Work w;
-        w.y = at / (unsigned)p.slots;
-        w.slot = (int)(at % (unsigned)p.slots);
-        w.valid = kTree ? tree_item(p, w.y, w.it) : prompt_item(p, w.y, w.it);
+        // (all items of a share before the next share: tiles of rows that read the same keys do so at the same time)
+        w.slot = p.slots == 1 ? 0 : (int)(at / (unsigned)p.n_items);
+        w.y = p.slots == 1 ? at : at % (unsigned)p.n_items;
+        const bool there = kTree ? tree_item(p, w.y, w.it) : prompt_item(p, w.y, w.it);
+        w.valid = p.slots == 1 ? there : w.slot < p.slots;
         if (w.valid) {
+          if (!there) continue;
           const AttnItem& it = w.it;
           const int toks = min(p.tile_q, it.n_q - it.q0);
           if (toks <= 0) continue;
