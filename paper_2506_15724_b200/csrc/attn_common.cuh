@@ -39,11 +39,12 @@ struct AttnParams {
   const uint64_t* mask;
   const int32_t* n_nodes;
   int n_sel;  // (sequence, layer, KV head)s of the call
-  // shares of the keys: partial results [item, slot, row of the tile, D] and their (max, sum) [item, slot, row]
+  // shares of the keys: partial results [item, slot, row of the tile, D] and their (max, in the logarithm to base 2, sum) [item, slot, row]
   float* part;
   float2* part_ml;
-  unsigned* counter;
   int slots, min_tiles;
+  int tile_keys;       // keys of a tile
+  int* order;          // tree, null or: the number of items that have rows, then those items, the longest first
   int tile_q;          // queries of an item
   int tile_rows;       // rows of an item at most
   int g_inverse;       // 2^16 / g, rounded up
@@ -197,6 +198,12 @@ __device__ __forceinline__ uint64_t node_mask(const AttnParams& p, const AttnIte
 }
 
 // ---- shares of the keys --------------------------------------------------------------------------------------------------
+// Tiles of keys that any row of the item sees; a tree's own nodes are one behind the segment's.
+template <bool kTree>
+__device__ __forceinline__ int item_tiles(const AttnParams& p, const AttnItem& it) {
+  const int seen = kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, min(it.q0 + p.tile_q, it.n_q) + it.shift));
+  return (seen + p.tile_keys - 1) / p.tile_keys + (kTree ? 1 : 0);
+}
 // Shares of `tiles` tiles of keys that get work, and the tiles of share x. Share 0 always takes part.
 __device__ __forceinline__ int shares_of(const AttnParams& p, int tiles) {
   return max(1, min(p.slots, (tiles + p.min_tiles - 1) / p.min_tiles));
@@ -244,16 +251,16 @@ inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int til
   if (slots > by_keys) slots = by_keys;
   if (slots > by_room) slots = by_room;
   if (slots > kAttnSlots) slots = kAttnSlots;
-  if (slots > 4) slots = slots / 4 * 4;  // (they are joined four at a time)
-  if (slots < 1 || p.n_items > kCounters) slots = 1;
+  if (slots < 1) slots = 1;
   p.slots = (int)slots;
   p.min_tiles = min_tiles;
+  p.tile_keys = tile_keys;
   p.part = reinterpret_cast<float*>((char*)p.ws + ws_layout(c).decode_off);
   p.part_ml = reinterpret_cast<float2*>(p.part + (int64_t)kAttnPartRows * c.head_dim);
-  p.counter = reinterpret_cast<unsigned*>((char*)p.ws + kHeaderBytes);
 }
 
 int launch_attn_plain(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);
+int launch_attn_join(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);  // behind a call with shares
 int launch_attn_split(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);
 int launch_attn_tc(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);  // -1: its copies cannot take these strides
 

@@ -52,7 +52,6 @@ struct Smem {
   float v[N * PITCH];
   AttnItem item;
   int there;
-  unsigned last;
 };
 
 template <int D, bool kTree>
@@ -80,10 +79,8 @@ __global__ void __launch_bounds__(NT, 2) attn_plain_kernel(const __grid_constant
   const int rows = min(p.tile_q, it.n_q - it.q0) * p.g;  // rows of the tile that are queries
   if (rows <= 0) return;
   // keys that any row sees, in tiles; a tree's own nodes are a tile behind the segment's
-  const int last_q = it.q0 + min(p.tile_q, it.n_q - it.q0) - 1;
-  const int seen = kTree ? it.n_keys : (p.causal ? max(0, min(it.n_keys, last_q + it.shift + 1)) : it.n_keys);
-  const int main_tiles = (seen + N - 1) / N, tiles = main_tiles + (kTree ? 1 : 0);
-  const int nb = shares_of(p, tiles);
+  const int tiles = item_tiles<kTree>(p, it), main_tiles = tiles - (kTree ? 1 : 0), nb = shares_of(p, tiles);
+  if (slot >= nb) return;
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
 
   float m[4], l[4];
@@ -95,7 +92,7 @@ __global__ void __launch_bounds__(NT, 2) attn_plain_kernel(const __grid_constant
 #pragma unroll
     for (int c = 0; c < CO; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  if (slot < nb) {
+  {
     const T* q = reinterpret_cast<const T*>(p.q) + it.q_at;
     for (int x = tid; x < M * C4; x += NT) {
       const int r = x / C4, c = x % C4 * 4;
@@ -225,7 +222,7 @@ __global__ void __launch_bounds__(NT, 2) attn_plain_kernel(const __grid_constant
     for (int x = tx; x < D * (int)sizeof(T) / 16; x += 16) dst[x] = src[x];
   };
   T* out = reinterpret_cast<T*>(p.out) + it.out_at;
-  if (p.slots == 1) {
+  if (nb == 1) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = ty * 4 + i;
@@ -240,73 +237,14 @@ __global__ void __launch_bounds__(NT, 2) attn_plain_kernel(const __grid_constant
     return;
   }
   auto part_row = [&](int x, int r) { return ((int64_t)y * p.slots + x) * p.tile_rows + r; };
-  if (slot < nb) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = ty * 4 + i;
-      if (r >= rows) continue;
-      const int64_t at = part_row(slot, r);
-#pragma unroll
-      for (int c = 0; c < CO; ++c) __stcg(reinterpret_cast<float4*>(p.part + at * D + tx * 4 + 64 * c), o[i][c]);
-      if (tx == 0) __stcg(p.part_ml + at, make_float2(m[i], l[i]));
-    }
-  }
-  __syncthreads();
-  if (tid == 0) sm.last = arrive_inc(p.counter + y, (unsigned)p.slots - 1u);  // (wraps to 0: ready for the next call)
-  __syncthreads();
-  if (sm.last != (unsigned)p.slots - 1u) return;
-  // the shares' statistics by the 16 threads of a row, then their results two at a time
-  float fac[4][2], sum[4], top[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = ty * 4 + i;
-    float2 ml[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      ml[h] = r < rows && tx + 16 * h < nb ? __ldcg(p.part_ml + part_row(tx + 16 * h, r)) : make_float2(-INFINITY, 0.f);
-    top[i] = fmaxf(ml[0].x, ml[1].x);
-#pragma unroll
-    for (int x = 8; x >= 1; x >>= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
-    const float base = top[i] == -INFINITY ? 0.f : top[i];
-    fac[i][0] = exp2f(ml[0].x - base);
-    fac[i][1] = exp2f(ml[1].x - base);
-    sum[i] = ml[0].y * fac[i][0] + ml[1].y * fac[i][1];
-#pragma unroll
-    for (int x = 8; x >= 1; x >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], x);
-#pragma unroll
-    for (int c = 0; c < CO; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-#pragma unroll 1
-  for (int x0 = 0; x0 < nb; x0 += 2) {
-    float4 z[2][4][CO];
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int c = 0; c < CO; ++c)
-          z[x][i][c] = x0 + x < nb && ty * 4 + i < rows
-                           ? __ldcg(reinterpret_cast<const float4*>(p.part + part_row(x0 + x, ty * 4 + i) * D + tx * 4 + 64 * c))
-                           : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float f = __shfl_sync(0xffffffffu, x0 + x < 16 ? fac[i][0] : fac[i][1], (tid & 16) + ((x0 + x) & 15));  // (0 beyond the last share)
-#pragma unroll
-        for (int c = 0; c < CO; ++c) o[i][c].x += z[x][i][c].x * f, o[i][c].y += z[x][i][c].y * f, o[i][c].z += z[x][i][c].z * f, o[i][c].w += z[x][i][c].w * f;
-      }
-  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = ty * 4 + i;
     if (r >= rows) continue;
-    const float z = row_factor(sum[i]);
-    T* dst = out + (int64_t)(it.q0 + group_of(p, r)) * p.so.token + (r - group_of(p, r) * p.g) * p.so.head;
+    const int64_t at = part_row(slot, r);
 #pragma unroll
-    for (int c = 0; c < CO; ++c)
-      store4(dst + tx * 4 + 64 * c, make_float4(o[i][c].x * z, o[i][c].y * z, o[i][c].z * z, o[i][c].w * z));
-    finish_row(r, top[i], sum[i]);
+    for (int c = 0; c < CO; ++c) *reinterpret_cast<float4*>(p.part + at * D + tx * 4 + 64 * c) = o[i][c];
+    if (tx == 0) p.part_ml[at] = make_float2(m[i], l[i]);
   }
 }
 
@@ -320,7 +258,8 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   if (p.n_items * p.slots > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>)) != cudaSuccess) return MADAKV_ECUDA;
   launch_pdl(kernel, dim3((unsigned)(p.n_items * p.slots)), dim3(NT), sizeof(Smem<D>), st, p);
-  return launch_status();
+  const int rc = launch_status();
+  return rc || p.slots == 1 ? rc : launch_attn_join(p, c, kTree, st);
 }
 
 }  // namespace

@@ -26,11 +26,10 @@ struct Geo {
   static_assert(kO + D <= kTmemCols, "tensor memory");
 };
 struct Barriers {
-  uint64_t q_full, k_full[2], k_empty[2], v_full, v_empty, s_full[2], p_full, o_full, met, drain;
+  uint64_t q_full, k_full[2], k_empty[2], v_full, v_empty, s_full[2], p_full, o_full, drain;
   AttnItem item;
   int there, abort;
   uint32_t tmem;
-  unsigned last;
 };
 template <int D>
 constexpr int smem_bytes() {
@@ -69,7 +68,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
     mbar_init(&sb.v_empty, 1);
     mbar_init(&sb.p_full, 4);
     mbar_init(&sb.o_full, 1);
-    mbar_init(&sb.met, 4);
     mbar_init(&sb.drain, 1);
     sb.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -96,8 +94,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
   const uint32_t tmem = sb.tmem;
   const AttnItem& it = sb.item;
   const int queries = sb.there ? min(p.tile_q, it.n_q - it.q0) : 0;
-  const int seen = kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, it.q0 + queries + it.shift));
-  const int main_tiles = (seen + N - 1) / N, tiles_all = main_tiles + (kTree ? 1 : 0), nb = shares_of(p, tiles_all);
+  const int tiles_all = sb.there ? item_tiles<kTree>(p, it) : 0, main_tiles = tiles_all - (kTree ? 1 : 0), nb = shares_of(p, tiles_all);
   int begin = 0, end = 0;
   if (queries > 0 && slot < nb) share_tiles(nb, tiles_all, slot, begin, end);
   const int tiles = end - begin;
@@ -229,20 +226,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
           for (int i = 0; i < 8; ++i) x[i] = none ? 0u : __float_as_uint(o[c + i] * norm);
           store32(dst + c, x, split || p.wide_out);
         }
-        if (split) __stcg(p.part_ml + row, make_float2(m, l));
+        if (split) p.part_ml[row] = make_float2(m, l);
         else finish(t, r_head, row_lse(m, l));
-      }
-      if (split) {
-        uint32_t n_met = 0;
-        auto meet = [&] {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sb.met);
-          wait.all(&sb.met, n_met++ & 1, kSiteTile);
-        };
-        meet();
-        if (threadIdx.x == 0 && !wait.dead) sb.last = arrive_inc(p.counter + y, (unsigned)nb - 1u);  // (wraps to 0: ready for the next call)
-        meet();
-        if (!wait.dead && sb.last == (unsigned)nb - 1u) join_shares<float, D, 4>(p, it, y, nb, queries * p.g, 1.f, warp, lane, finish);
       }
     }
   } else {
@@ -372,7 +357,8 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   auto kernel = attn_split_kernel<D, kTree>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()) != cudaSuccess) return MADAKV_ECUDA;
   launch_pdl(kernel, dim3((unsigned)(p.n_items * p.slots)), dim3(kThreads), smem_bytes<D>(), st, p);
-  return launch_status();
+  const int rc = launch_status();
+  return rc || p.slots == 1 ? rc : launch_attn_join(p, c, kTree, st);
 }
 
 }  // namespace

@@ -45,7 +45,6 @@ struct Barriers {
   float2 stats[2][kRows];
   uint32_t tmem;
   int abort;
-  unsigned last;
   int mend_stage[2];  // where the copies that landed[] counts go
 };
 template <int D>
@@ -296,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         if (valid && (!dual || s == 0)) {
-          if (split) __stcg(p.part_ml + row, make_float2(m, l));
+          if (split) p.part_ml[row] = make_float2(m * p.scale2, l);
         }
       }
       auto finish = [&](int tt, int j, float lse) {
@@ -316,14 +315,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!split && valid && (!dual || s == 0) && !wait.dead) finish(t, r_head, row_lse(m * p.scale2, l));
       tc_fence_before();
       if (dual) meet();  // (both accumulators have been read before either is written again)
-      if (split) {
-        meet();
-        if (threadIdx.x == 0 && !wait.dead) sb.last = arrive_inc(p.counter + w.y, (unsigned)w.nb - 1u);  // (wraps to 0: ready for the next call)
-        meet();
-        if (!wait.dead && sb.last == (unsigned)w.nb - 1u) {
-          join_shares<__nv_bfloat16, D, 8>(p, it, w.y, w.nb, (w.tok0 + w.tok1) * p.g, p.scale2, warp, lane, finish);
-        }
-      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sb.item_empty[round % kRing]);
       if (wait.dead) break;
@@ -488,7 +479,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         // (all items of a share before the next share: tiles of rows that read the same keys do so at the same time)
         w.slot = p.slots == 1 ? 0 : (int)(at / (unsigned)p.n_items);
         w.y = p.slots == 1 ? at : at % (unsigned)p.n_items;
-        const bool there = kTree ? tree_item(p, w.y, w.it) : prompt_item(p, w.y, w.it);
+        bool there = true;
+        if (kTree && p.order) {
+          there = at < (unsigned)p.order[0];
+          w.y = there ? (unsigned)p.order[1 + at] : 0u;
+        }
+        there = there && (kTree ? tree_item(p, w.y, w.it) : prompt_item(p, w.y, w.it));
         w.valid = p.slots == 1 ? there : w.slot < p.slots;
         if (w.valid) {
           if (!there) continue;
@@ -498,9 +494,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           w.tok0 = min(tok_m, toks);
           w.tok1 = toks - w.tok0;
           w.dual = w.tok1 == 0;
-          auto seen_by = [&](int last) { return kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, last + it.shift + 1)); };
-          w.main_tiles = (seen_by(it.q0 + toks - 1) + kKeys - 1) / kKeys;
-          const int tiles = w.main_tiles + (kTree ? 1 : 0), tiles0 = (seen_by(it.q0 + w.tok0 - 1) + kKeys - 1) / kKeys + (kTree ? 1 : 0);
+          const int tiles = item_tiles<kTree>(p, it);
+          w.main_tiles = tiles - (kTree ? 1 : 0);
+          const int seen0 = kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, it.q0 + w.tok0 + it.shift));  // by the first tile of rows
+          const int tiles0 = (seen0 + kKeys - 1) / kKeys + (kTree ? 1 : 0);
           w.nb = shares_of(p, tiles);
           if (w.slot >= w.nb) continue;
           share_tiles(w.nb, tiles, w.slot, w.begin, w.end);
@@ -567,6 +564,58 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
+// The items of a tree call by what they cost, the most first, in classes: blocks take them in rounds, to and fro, and end together. (896
+// segments of 1000 to 4000 rows, trees of 6 to 41 nodes, in the order of memory: blocks end up to 30 % apart.) One block.
+constexpr int kClasses = 1024;
+__global__ void __launch_bounds__(kClasses) order_kernel(const __grid_constant__ AttnParams p, float classes_per_cost) {
+  __shared__ int start[kClasses], warps[kClasses / 32];
+  const int tid = threadIdx.x;
+  start[tid] = 0;
+  pdl_wait();
+  pdl_go();
+  __syncthreads();
+  auto class_of = [&](unsigned i) {
+    AttnItem it;
+    tree_item(p, i, it);
+    const int queries = min(p.tile_q, it.n_q - it.q0);
+    if (queries <= 0) return -1;
+    // (a tile of keys takes 1.7 us for two tiles of rows, 0.95 for one; an item 4 us beside)
+    const float cost = item_tiles<true>(p, it) * (queries > p.tile_q / 2 ? 1.7f : 0.95f) + 4.f;
+    return max(0, kClasses - 1 - (int)(cost * classes_per_cost));
+  };
+  for (unsigned i = tid; i < (unsigned)p.n_items; i += kClasses) {
+    const int c = class_of(i);
+    if (c >= 0) atomicAdd(&start[c], 1);
+  }
+  __syncthreads();
+  const int own = start[tid];
+  int sum = own;
+#pragma unroll
+  for (int i = 1; i < 32; i *= 2) {
+    const int x = __shfl_up_sync(0xffffffffu, sum, i);
+    if (tid % 32 >= i) sum += x;
+  }
+  if (tid % 32 == 31) warps[tid / 32] = sum;
+  __syncthreads();
+  if (tid < 32) {
+    int x = warps[tid], all = x;
+#pragma unroll
+    for (int i = 1; i < 32; i *= 2) {
+      const int z = __shfl_up_sync(0xffffffffu, all, i);
+      if (tid >= i) all += z;
+    }
+    warps[tid] = all - x;
+    if (tid == 31) p.order[0] = all;
+  }
+  __syncthreads();
+  start[tid] = warps[tid / 32] + sum - own;
+  __syncthreads();
+  for (unsigned i = tid; i < (unsigned)p.n_items; i += kClasses) {
+    const int c = class_of(i);
+    if (c >= 0) p.order[1 + atomicAdd(&start[c], 1)] = (int)i;  // (within a class in any order: results do not depend on it)
+  }
+}
+
 // [batch, layers, heads, rows, d] with element strides, boxes of 128 rows by 64 elements; without layers in four dimensions.
 bool make_rows_map(CUtensorMap* map, const void* base, int d, int64_t rows, int heads, int layers, int batch, madakv_strides s) {
   if ((heads > 1 && s.head <= 0) || (layers > 1 && s.layer <= 0) || (batch > 1 && s.batch <= 0)) return false;
@@ -626,7 +675,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   const void* q = kTree && !all ? (const char*)p.q + p.layer * p.sq.layer * 2 : p.q;
   if (!make_query_map(&mq, q, D, p.g, p.q_rows, p.Hkv, outer, all && p.L > 1 ? p.sq.layer : p.sq.batch, p.sq, p.tile_q / 2)) return -1;
   attn_items(p, kTree);
-  attn_slots(p, c, kTree, kKeys, 2 * 148, 4);
+  attn_slots(p, c, kTree, kKeys, 2 * 148, 2);
   attn_waits(p);
   if (p.n_items * p.slots > 0x7ffffff0ll) return MADAKV_EUNSUPPORTED;
   auto wide = [](const void* x, const madakv_strides& t) {
@@ -634,13 +683,20 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   };
   p.wide_out = wide(p.out, p.so);
   p.wide_q = wide(p.q, p.sq) && (uintptr_t)p.q_win % 32 == 0;
+  if (kTree && p.slots == 1 && p.n_items > 148 && p.n_items < (int64_t)kAttnPartRows * D) {
+    p.order = reinterpret_cast<int*>(p.part);  // (no shares: the place of their results is free)
+    const float most = 1.7f * (float)(((int64_t)c.max_seq_len + c.max_new_tokens) / kKeys + 2) + 4.f;
+    launch_pdl(order_kernel, dim3(1), dim3(kClasses), 0, st, p, (kClasses - 1) / most);
+    if (const int rc = launch_status()) return rc;
+  }
   auto kernel = attn_tc_kernel<D, kTree>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()) != cudaSuccess) return MADAKV_ECUDA;
   // (few works: as many blocks as all get the same number of them)
   const int64_t works = p.n_items * p.slots, each = p.slots > 1 ? (works + 147) / 148 : 1;
   const int64_t blocks = (works + each - 1) / each;
   launch_pdl(kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < 148 ? blocks : 148)), dim3(kThreads), smem_bytes<D>(), st, mk, mv, tk, tv, mq, p);
-  return launch_status();
+  const int rc = launch_status();
+  return rc || p.slots == 1 ? rc : launch_attn_join(p, c, kTree, st);
 }
 
 }  // namespace

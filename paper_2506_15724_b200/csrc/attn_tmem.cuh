@@ -1,4 +1,4 @@
-// What the tensor-core kernels of prompt and tree attention share: waits, tensor memory, row stores, the join of shares of the keys.
+// What the tensor-core kernels of prompt and tree attention share: waits, tensor memory, row stores.
 #pragma once
 
 #include <type_traits>
@@ -110,82 +110,6 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return r;
 }
 
-
-// The results of an item's nb shares to where the caller wants them, by kWarps warps; part_ml holds maxima in units of 1 / scale.
-// A warp joins R rows at a time, a lane has V of a row's columns; lane k keeps the sums of the warp's k-th row. Bound by the latency of what
-// stands between a row's loads: with one row at a time and divisions 2250 clocks a row.
-template <typename T, int D, int kWarps, typename Finish>
-__device__ __forceinline__ void join_shares(const AttnParams& p, const AttnItem& it, unsigned y, int nb, int rows, float scale, int warp, int lane,
-                                  Finish finish) {
-  constexpr int V = D / 32, N = 4, R = 4;
-  using Piece = std::conditional_t<V == 4, float4, float2>;
-  const int pitch = p.tile_rows;
-  const float2* ml_at = p.part_ml + (int64_t)y * p.slots * pitch + lane * pitch;
-  const Piece* part_at = reinterpret_cast<const Piece*>(p.part + (int64_t)y * p.slots * pitch * D) + lane;
-  float my_top = -INFINITY, my_sum = 0.f;
-#pragma unroll 1
-  for (int k = 0; warp + kWarps * k < rows; k += R) {
-    float2 ml[R];
-    Piece v[R][N];
-    auto ask = [&](int i0) {
-#pragma unroll
-      for (int q = 0; q < R; ++q)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int r = warp + kWarps * (k + q);
-          v[q][i] = i0 + i < nb && r < rows ? __ldcg(part_at + ((i0 + i) * pitch + r) * 32) : Piece();
-        }
-    };
-#pragma unroll
-    for (int q = 0; q < R; ++q) {
-      const int r = warp + kWarps * (k + q);
-      ml[q] = lane < nb && r < rows ? __ldcg(ml_at + r) : make_float2(-INFINITY, 0.f);
-    }
-    ask(0);
-    float fac[R], sum[R], acc[R][V] = {};
-#pragma unroll
-    for (int q = 0; q < R; ++q) {
-      const float top = warp_max(ml[q].x);
-      fac[q] = ex2((ml[q].x - (top == -INFINITY ? 0.f : top)) * scale);
-      sum[q] = ml[q].y * fac[q];
-      if (lane == k + q) my_top = top;
-    }
-#pragma unroll
-    for (int i = 16; i >= 1; i >>= 1)
-#pragma unroll
-      for (int q = 0; q < R; ++q) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], i);
-#pragma unroll 1
-    for (int i0 = 0; i0 < nb; i0 += N) {
-      if (i0) ask(i0);
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int q = 0; q < R; ++q) {
-          const float f = __shfl_sync(0xffffffffu, fac[q], i0 + i);
-#pragma unroll
-          for (int e = 0; e < V; ++e) acc[q][e] += reinterpret_cast<const float*>(&v[q][i])[e] * f;  // (0 times 0 beyond the last share)
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < R; ++q) {
-      const int r = warp + kWarps * (k + q), tq = group_of(p, r);
-      if (lane == k + q) my_sum = sum[q];
-      const float z = row_factor(sum[q]);
-      T* to = reinterpret_cast<T*>(p.out) + it.out_at + (it.q0 + tq) * p.so.token + (r - tq * p.g) * p.so.head + lane * V;
-      if (r < rows) {
-#pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          if constexpr (sizeof(T) == 2)
-            *reinterpret_cast<uint32_t*>(to + e) = pack_bf16x2(acc[q][e] * z, acc[q][e + 1] * z);
-          else
-            *reinterpret_cast<float2*>(to + e) = make_float2(acc[q][e] * z, acc[q][e + 1] * z);
-        }
-      }
-    }
-  }
-  const int r = warp + kWarps * lane, tq = group_of(p, r);
-  if (r < rows) finish(it.q0 + tq, r - tq * p.g, row_lse(my_top * scale, my_sum));
-}
 
 // Bounds of the waits. Failure-path test (no GPU fault involved), as in decode attention: the copies are withheld, waits last that many clocks.
 inline void attn_waits(AttnParams& p) {
