@@ -237,62 +237,95 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
       // ---- operands ----------------------------------------------------------------------------------------------------------
       const int tid = threadIdx.x - 128;
       constexpr int CPR = D / 8;  // pieces of 8 elements of a row
-      // rows of `at(row)` (null: zeros), `rows` of them, as terms
-      auto bring = [&](uint32_t to, int rows, int block, int term, auto at) {
-        for (int x0 = tid; x0 < rows * CPR; x0 += 4 * 256) {
-          float4 a[4], b[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int x = x0 + i * 256;
-            const float* src = at(x / CPR);
-            a[i] = src ? *reinterpret_cast<const float4*>(src + x % CPR * 8) : make_float4(0.f, 0.f, 0.f, 0.f);
-            b[i] = src ? *reinterpret_cast<const float4*>(src + x % CPR * 8 + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int x = x0 + i * 256, r = x / CPR, c = x % CPR;
-            uint32_t t[4][kTerms];
-            split2(finite(a[i].x), finite(a[i].y), t[0]);
-            split2(finite(a[i].z), finite(a[i].w), t[1]);
-            split2(finite(b[i].x), finite(b[i].y), t[2]);
-            split2(finite(b[i].z), finite(b[i].w), t[3]);
-            const uint32_t dst = to + (c / 8) * block + r * 128 + ((c % 8) ^ (r & 7)) * 16;
-#pragma unroll
-            for (int k = 0; k < kTerms; ++k)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + k * term), "r"(t[0][k]), "r"(t[1][k]), "r"(t[2][k]), "r"(t[3][k]) : "memory");
-          }
-        }
-        fence_async();
+      // Four pieces of 8 elements of a thread, of the rows that at(row) says (null: zeros), from piece x0 on ...
+      struct Pieces {
+        float4 a[4], b[4];
       };
+      auto fetch = [&](Pieces& w, int x0, auto at) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int x = x0 + i * 256;
+          const float* src = at(x / CPR);
+          w.a[i] = src ? *reinterpret_cast<const float4*>(src + x % CPR * 8) : make_float4(0.f, 0.f, 0.f, 0.f);
+          w.b[i] = src ? *reinterpret_cast<const float4*>(src + x % CPR * 8 + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      };
+      // ... and their terms to shared memory
+      auto put = [&](Pieces& w, int x0, uint32_t to, int block, int term) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int x = x0 + i * 256, r = x / CPR, c = x % CPR;
+          const float big = fmaxf(max3f(max3f(fabsf(w.a[i].x), fabsf(w.a[i].y), fabsf(w.a[i].z)), fabsf(w.a[i].w), fabsf(w.b[i].x)),
+                                  max3f(fabsf(w.b[i].y), fabsf(w.b[i].z), fabsf(w.b[i].w)));
+          if (big == INFINITY) {
+            w.a[i] = make_float4(finite(w.a[i].x), finite(w.a[i].y), finite(w.a[i].z), finite(w.a[i].w));
+            w.b[i] = make_float4(finite(w.b[i].x), finite(w.b[i].y), finite(w.b[i].z), finite(w.b[i].w));
+          }
+          uint32_t t[4][kTerms];
+          split2(w.a[i].x, w.a[i].y, t[0]);
+          split2(w.a[i].z, w.a[i].w, t[1]);
+          split2(w.b[i].x, w.b[i].y, t[2]);
+          split2(w.b[i].z, w.b[i].w, t[3]);
+          const uint32_t dst = to + (c / 8) * block + r * 128 + ((c % 8) ^ (r & 7)) * 16;
+#pragma unroll
+          for (int k = 0; k < kTerms; ++k)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + k * term), "r"(t[0][k]), "r"(t[1][k]), "r"(t[2][k]), "r"(t[3][k]) : "memory");
+        }
+      };
+      auto rows_of = [&](int x, bool is_v) {
+        const int tile = begin + x;
+        const bool own = kTree && tile == main_tiles;
+        const int there = x >= tiles ? 0 : own ? it.nodes : it.n_keys - tile * N;
+        const float* from;
+        int64_t step;
+        if (kTree && !own) {
+          from = reinterpret_cast<const float*>(is_v ? p.v_c : p.k_c) + (it.key_row + tile * N) * D;
+          step = D;
+        } else {
+          step = is_v ? p.sv.token : p.sk.token;
+          from = reinterpret_cast<const float*>(is_v ? p.v : p.k) + (is_v ? it.v_at : it.k_at) + (own ? 0 : (int64_t)tile * N * step);
+        }
+        return [=](int r) -> const float* { return r < there ? from + r * step : nullptr; };
+      };
+      static_assert(N * CPR == 4 * 256, "a tile of keys is four pieces a thread");
       const float* q = reinterpret_cast<const float*>(p.q) + it.q_at;
-      bring(q_smem, kRows, G::kQBlock, G::kQTerm, [&](int r) -> const float* {
+      auto q_row = [&](int r) -> const float* {
         const int rq = group_of(p, r);
         return rq < queries ? q + (it.q0 + rq) * p.sq.token + (r - rq * p.g) * p.sq.head : nullptr;
-      });
+      };
+      Pieces k, v;  // (a tile's rows are on their way while the rows before are split)
+      fetch(v, tid, q_row);
+      fetch(k, tid, rows_of(0, false));
+      put(v, tid, q_smem, G::kQBlock, G::kQTerm);
+      if constexpr (D == 128) {
+        fetch(v, tid + 1024, q_row);
+        put(v, tid + 1024, q_smem, G::kQBlock, G::kQTerm);
+      }
+      fence_async();
       mbar_arrive(&sb.q_full);
-      for (int x = 0; x < tiles; ++x) {
-        const int tile = begin + x, buf = G::kKeyBuffers == 2 ? x & 1 : 0, use = G::kKeyBuffers == 2 ? x >> 1 : x;
-        const bool own = kTree && tile == main_tiles;
-        const int there = own ? it.nodes : it.n_keys - tile * N;
-        auto rows_of = [&](bool is_v) {
-          const float* from;
-          int64_t step;
-          if (kTree && !own) {
-            from = reinterpret_cast<const float*>(is_v ? p.v_c : p.k_c) + (it.key_row + tile * N) * D;
-            step = D;
-          } else {
-            step = is_v ? p.sv.token : p.sk.token;
-            from = reinterpret_cast<const float*>(is_v ? p.v : p.k) + (is_v ? it.v_at : it.k_at) + (own ? 0 : (int64_t)tile * N * step);
-          }
-          return [=](int r) -> const float* { return r < there ? from + r * step : nullptr; };
-        };
-        if (p.hold_copies) continue;
-        if (!wait.all(&sb.k_empty[buf], (use & 1) ^ 1, kSiteStage)) break;
-        bring(k_smem + buf * G::kTile, N, G::kBlock, G::kTerm, rows_of(false));
+      // K of the next tile goes before V of this one: V's place is free when the product of the tile before is done, S should not wait for it.
+      auto put_k = [&](int x) {
+        const int buf = G::kKeyBuffers == 2 ? x & 1 : 0, use = G::kKeyBuffers == 2 ? x >> 1 : x;
+        if (!wait.all(&sb.k_empty[buf], (use & 1) ^ 1, kSiteStage)) return;
+        put(k, tid, k_smem + buf * G::kTile, G::kBlock, G::kTerm);
+        fence_async();
         mbar_arrive(&sb.k_full[buf]);
-        if (!wait.all(&sb.v_empty, (x & 1) ^ 1, kSiteStage)) break;
-        bring(v_smem, N, G::kBlock, G::kTerm, rows_of(true));
-        mbar_arrive(&sb.v_full);
+      };
+      if (!p.hold_copies) {
+        fetch(v, tid, rows_of(0, true));
+        put_k(0);
+        fetch(k, tid, rows_of(1, false));
+        for (int x = 0; x < tiles && !wait.dead; ++x) {
+          if (x + 1 < tiles) {
+            put_k(x + 1);
+            fetch(k, tid, rows_of(x + 2, false));
+          }
+          if (!wait.all(&sb.v_empty, (x & 1) ^ 1, kSiteStage)) break;
+          put(v, tid, v_smem, G::kBlock, G::kTerm);
+          fence_async();
+          mbar_arrive(&sb.v_full);
+          fetch(v, tid, rows_of(x + 1, true));
+        }
       }
     } else if (warp == 12) {
       // ---- matrix products: one thread ----------------------------------------------------------------------------------------
@@ -350,7 +383,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   p.tile_q = kRows / p.g;
   attn_items(p, kTree);
   if (p.n_items == 0) p.n_items = 1;  // (the window's missing rows are still filled)
-  attn_slots(p, c, kTree, Geo<D>::N, 2 * 148, 2);
+  attn_slots(p, c, kTree, Geo<D>::N, 148, 2);
   if (p.n_items * p.slots > 0x7ffffff0ll) return MADAKV_EUNSUPPORTED;
   attn_waits(p);
   p.wide_out = ((uintptr_t)p.out % 32 | p.so.batch * 4 % 32 | p.so.layer * 4 % 32 | p.so.head * 4 % 32 | p.so.token * 4 % 32) == 0;
