@@ -312,6 +312,49 @@ def test_prefill_numbers_that_are_none(dtype):
     check(dtype, q[0, 0, 0, :170], k[0, 0, 0, :170], v[0, 0, 0, :170], see, d ** -0.5, out[0, 0, 0, :170], lse[0, 0, 0, :170])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [260.0, 14.0, -300.0])
+def test_prefill_logits_far_apart(d, size):
+    """Single keys, at every place of a tile in turn, whose logits stand far above or below all of the tiles before: first tiles of a
+    row, later ones, the last. The others stay where they were."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    n = 1300
+    cfg = config("bf16", 1, 1, 2, 1, d, n)
+    q, k, v = torch.full((1, 1, 2, n, d), d ** -0.5, device="cuda").bfloat16(), normal(gen, (1, 1, 1, n, d), "bf16"), normal(gen, (1, 1, 1, n, d), "bf16")
+    q[:, :, 1] *= 0.5
+    at = torch.arange(0, n, 37, device="cuda")  # (37 and 128 share no factor)
+    k[0, 0, 0, at] = (size * (1.0 + at / n * 0.5)).to(torch.bfloat16).unsqueeze(1)
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 2, n), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    see = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+    for h in range(2):
+        check("bf16", q[0, 0, h], k[0, 0, 0], v[0, 0, 0], see, d ** -0.5, out[0, 0, h], lse[0, 0, h])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [2, 147, 386, 640, 659])
+def test_prefill_one_bad_key(d, at):
+    """One key of NaN, infinities of both signs, in places of a tile that are computed in different ways."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    n = 700
+    cfg = config("bf16", 1, 1, 1, 1, d, n)
+    q, k, v = normal(gen, (1, 1, 1, n, d), "bf16").abs() + 0.25, normal(gen, (1, 1, 1, n, d), "bf16"), normal(gen, (1, 1, 1, n, d), "bf16")
+    ws, lens = mk.new_workspace(cfg), torch.tensor([n], dtype=torch.int32, device="cuda")
+    see = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+    for bad in (math.nan, math.inf, -math.inf):
+        k[0, 0, 0, at] = bad
+        out, lse = torch.empty_like(q), torch.empty((1, 1, 1, n), device="cuda")
+        mk.madakv_prefill_attn(cfg, 0, q, k, v, out, ws, lse_out=lse, seq_len=lens)
+        check("bf16", q[0, 0, 0, :at], k[0, 0, 0, :at], v[0, 0, 0, :at], see[:at, :at], d ** -0.5, out[0, 0, 0, :at], lse[0, 0, 0, :at])
+        if bad == -math.inf:  # as if it were not there
+            rest = torch.arange(n, device="cuda") != at
+            check("bf16", q[0, 0, 0, at + 1:], k[0, 0, 0, rest], v[0, 0, 0, rest], see[at + 1:, rest], d ** -0.5, out[0, 0, 0, at + 1:], lse[0, 0, 0, at + 1:])
+        else:
+            assert out[0, 0, 0, at:].isnan().all() and not lse[0, 0, 0, at:].isfinite().any()
+
+
 # ------------------------------------------------------------------------------------------------- drafted trees
 def tree_masks(rng, B, T, kind):
     """[B, T] masks as Python integers: of random trees, of any bits, or none."""
