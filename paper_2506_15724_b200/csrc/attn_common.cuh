@@ -42,7 +42,7 @@ struct AttnParams {
   // shares of the keys: partial results [item, slot, row of the tile, D] and their (max, in the logarithm to base 2, sum) [item, slot, row]
   float* part;
   float2* part_ml;
-  int slots, min_tiles;
+  int slots, least_tiles;
   int tile_keys;       // keys of a tile
   int* order;          // tree, null or: the number of items that have rows, then those items, the longest first
   int tile_q;          // queries of an item
@@ -204,10 +204,8 @@ __device__ __forceinline__ int item_tiles(const AttnParams& p, const AttnItem& i
   const int seen = kTree || !p.causal ? it.n_keys : max(0, min(it.n_keys, min(it.q0 + p.tile_q, it.n_q) + it.shift));
   return (seen + p.tile_keys - 1) / p.tile_keys + (kTree ? 1 : 0);
 }
-// Shares of `tiles` tiles of keys that get work, and the tiles of share x. Share 0 always takes part.
-__device__ __forceinline__ int shares_of(const AttnParams& p, int tiles) {
-  return max(1, min(p.slots, (tiles + p.min_tiles - 1) / p.min_tiles));
-}
+// Shares of `tiles` tiles of keys that get work, and the tiles of share x: two each at least. Share 0 always takes part.
+__device__ __forceinline__ int shares_of(const AttnParams& p, int tiles) { return tiles < p.least_tiles ? 1 : min(p.slots, (tiles + 1) / 2); }
 __device__ __forceinline__ void share_tiles(int nb, int tiles, int x, int& begin, int& end) {
   begin = tiles * x / nb;  // (at most 2^14 tiles, 2^5 shares)
   end = tiles * (x + 1) / nb;
@@ -240,20 +238,34 @@ inline void attn_items(AttnParams& p, bool tree) {
   const int64_t packed = p.q_rows / p.tile_q + p.B;
   p.n_items = (p.q_off && packed < tiles ? packed : tiles) * p.Hkv;
 }
-// Shares of the keys: as many as give `blocks` blocks, of at least min_tiles tiles of tile_keys keys by the longest sequence or the mean
-// segment, and no more than there is room for their results.
-inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int tile_keys, int blocks, int min_tiles) {
+// What a kernel takes, in us: a tile of keys for rows of half an item and of a whole one, an item beside its tiles; and the tiles from
+// which it shares out keys.
+struct AttnCost {
+  float half, whole, item;
+  int least;
+};
+// Shares of the keys: the number that a call should end first with, by the longest sequence or the mean segment, and no more than there is
+// room for their results. Blocks go through the shares' items in rounds; shares cost a launch that joins them, and their results are
+// written and read in fp32. (28 / 4 heads: 1000 tokens 23.7 us whole and 41.8 in two shares, of which there are more than SMs; 72 tokens on
+// 8192 keys 116 us whole, 31 in 8 shares, 39 in 18.)
+inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int tile_keys, AttnCost cost) {
+  constexpr float kJoin = 6.2f, kMegabyte = 0.55f;  // us
   const int64_t units = (int64_t)c.batch * c.n_layers * c.n_kv_heads, longest = (int64_t)c.max_seq_len + c.max_new_tokens;
   const int64_t keys = !tree ? (p.k_rows < p.n_max ? p.k_rows : p.n_max) : p.capacity / units < longest ? p.capacity / units : longest;
+  const int64_t queries = p.q_rows < p.n_max ? p.q_rows : p.n_max;
   p.tile_rows = (int)(p.tile_q < p.q_rows ? p.tile_q : p.q_rows) * p.g;
-  int64_t slots = p.n_items ? blocks / p.n_items : 1;
-  const int64_t by_keys = (keys / tile_keys + min_tiles) / min_tiles, by_room = p.n_items ? kAttnPartRows / (p.n_items * p.tile_rows) : 1;
-  if (slots > by_keys) slots = by_keys;
-  if (slots > by_room) slots = by_room;
-  if (slots > kAttnSlots) slots = kAttnSlots;
-  if (slots < 1) slots = 1;
-  p.slots = (int)slots;
-  p.min_tiles = min_tiles;
+  const float most = (float)(keys / tile_keys + 1), mean = most - (!tree && p.causal ? (float)(queries < keys ? queries : keys) / (2 * tile_keys) : 0.f);
+  const float tile = p.q_rows > p.tile_q / 2 ? cost.whole : cost.half;
+  const int64_t by_room = p.n_items ? kAttnPartRows / (p.n_items * p.tile_rows) : 1;
+  float best = 0.f;
+  p.slots = 1;
+  for (int s = 1; s <= kAttnSlots && (s == 1 || (s <= by_room && 2 * s <= most + 1.f && most >= (float)cost.least)); ++s) {
+    const float rounds = (float)((p.n_items * s + 147) / 148), one = most / s * tile + cost.item, all = rounds * (mean / s * tile + cost.item);
+    const float join = s == 1 ? 0.f : kJoin + kMegabyte * 1e-6f * (float)(p.n_items * s * p.tile_rows) * (float)c.head_dim * 4.f;
+    const float t = (one > all ? one : all) + join;
+    if (s == 1 || t < best) best = t, p.slots = s;
+  }
+  p.least_tiles = cost.least;
   p.tile_keys = tile_keys;
   p.part = reinterpret_cast<float*>((char*)p.ws + ws_layout(c).decode_off);
   p.part_ml = reinterpret_cast<float2*>(p.part + (int64_t)kAttnPartRows * c.head_dim);

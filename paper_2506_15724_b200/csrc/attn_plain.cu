@@ -253,7 +253,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   p.tile_q = M / p.g;
   attn_items(p, kTree);
   if (p.n_items == 0) p.n_items = 1;  // (the window's missing rows are still filled)
-  attn_slots(p, c, kTree, N, 2 * 148, 2);
+  attn_slots(p, c, kTree, N, {15.f, 15.f, 10.f, 2});
   auto kernel = attn_plain_kernel<D, kTree>;
   if (p.n_items * p.slots > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>)) != cudaSuccess) return MADAKV_ECUDA;

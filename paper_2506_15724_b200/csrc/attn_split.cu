@@ -383,7 +383,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   p.tile_q = kRows / p.g;
   attn_items(p, kTree);
   if (p.n_items == 0) p.n_items = 1;  // (the window's missing rows are still filled)
-  attn_slots(p, c, kTree, Geo<D>::N, 148, 2);
+  attn_slots(p, c, kTree, Geo<D>::N, {4.7f, 4.7f, 10.f, 2});
   if (p.n_items * p.slots > 0x7ffffff0ll) return MADAKV_EUNSUPPORTED;
   attn_waits(p);
   p.wide_out = ((uintptr_t)p.out % 32 | p.so.batch * 4 % 32 | p.so.layer * 4 % 32 | p.so.head * 4 % 32 | p.so.token * 4 % 32) == 0;

@@ -79,6 +79,8 @@ __host__ __device__ constexpr uint32_t instr_desc_pv(int n) { return instr_desc_
 // 2^x of two numbers without the exponential unit, which is what bounds narrow heads: x = j + f, |f| <= 1/2; 2^f as the polynomial of
 // degree 5 with the least largest relative error (7.5e-8, by exchange; 2.1e-7 with its roundings, as good as the unit's), j added to its
 // exponent. At most 2^-126 from -126 down, and above 2^16 from there up and for NaN: the tile is then done again, by the unit.
+// (Of 8 pairs one: 32 / 8 heads of 64, 16384 tokens 1426 -> 1359 us, 809 TFLOP/s; of 16 pairs one or three and of 4 pairs one gain less,
+// of 8 pairs three nothing. Heads of 128, which the products bound, lose by any.)
 __device__ __forceinline__ void exp2_pair(float& lo, float& hi) {
   constexpr float kC0 = 1.00000012f, kC1 = 0.693146944f, kC2 = 0.240221202f, kC3 = 0.0555071309f, kC4 = 0.00967554096f, kC5 = 0.00132764725f;
   constexpr float kRound = 12582912.f;  // 1.5 * 2^23: a sum's last bit is 1
@@ -765,7 +767,8 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   const void* q = kTree && !all ? (const char*)p.q + p.layer * p.sq.layer * 2 : p.q;
   if (!make_query_map(&mq, q, D, p.g, p.q_rows, p.Hkv, outer, all && p.L > 1 ? p.sq.layer : p.sq.batch, p.sq, p.tile_q / 2)) return -1;
   attn_items(p, kTree);
-  attn_slots(p, c, kTree, kKeys, 2 * 148, 2);
+  // (28 / 4 heads, one token, 512 keys: 11 us whole, 14 in two shares; 1024 keys: 14.1 and in four 14.6; 2048: 20.7 and in eight 15.4)
+  attn_slots(p, c, kTree, kKeys, {0.85f, 1.7f, 4.f, 8});
   attn_waits(p);
   if (p.n_items * p.slots > 0x7ffffff0ll) return MADAKV_EUNSUPPORTED;
   auto wide = [](const void* x, const madakv_strides& t) {
