@@ -346,11 +346,15 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  *   q_win   [B, L, H_q, w, d] dtype, contiguous: the queries of the proxy tokens (window row r is query m - w + r; a row that is
  *           none of the call's queries is 0)
  *   lse_win [B, L, H_q, w] fp32, contiguous: their log-sum-exps (-inf for those rows), as madakv_score_lse takes them
- * H_q / H_kv is at most 64. bf16: products of bf16 with fp32 sums; the weights, at most 2^8 against the running maximum that they are
- * taken to, are rounded to bf16 before the product with v (their sum is not), out is rounded once. fp32: fp32 throughout.
+ * H_q / H_kv is at most 64. bf16: products of bf16 with fp32 sums; a row's weights, taken against the maximum of some of its keys, are
+ * rounded to bf16 before the product with v (their sum is not), out is rounded once. fp32: an element counts as three bf16 terms (24 bits),
+ * a product as those of their products that are not below 2^-24 of it, sums are fp32; an infinite element counts as the largest finite
+ * bf16 number, 3.39e38, and elements below 2^-110 keep fewer bits.
  * Every query of a sequence reads whole tiles of up to 128 keys: a row of v that is not finite makes NaN of results of the same sequence
  * whose query stands up to 127 positions before it too. What stands behind a sequence's last key is never used.
- * Deterministic. Few queries share out their keys over blocks, with the partial results in the workspace.           */
+ * Deterministic. Where few queries see many keys the keys are shared out over blocks; a second launch joins the partial results, which stand
+ * in the workspace. A bounded wait that runs out is recorded as MADAKV_ETIMEOUT; the call's results are then not to be used, the next
+ * call's are whole.                                                                                             */
 int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
                         const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
                         madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
@@ -367,7 +371,8 @@ int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, 
  * madakv_tree_attn: node i attends to all rows of every segment and to the nodes that it sees. A node that sees nothing (an empty segment, no
  * bit set) gets out = 0 and lse = -inf; a segment that selection refused counts as empty. The cache is only read.
  *   lse_out [B, L, H_q, T] fp32, contiguous, or null
- * Rows of out and lse_out of nodes that are not there are left as they were. Roundings as in madakv_prefill_attn; H_q / H_kv at most 64. */
+ * Rows of out and lse_out of nodes that are not there are left as they were. Roundings as in madakv_prefill_attn; H_q / H_kv at most 64. A
+ * row of the segment's or of a node's value that is not finite makes NaN of the results of all nodes of the sequence, seen or not. */
 int madakv_tree_attn(const madakv_config* cfg, int32_t layer, int32_t nodes, const void* q, madakv_strides sq, const void* k_tree,
                      madakv_strides sk, const void* v_tree, madakv_strides sv, const uint64_t* mask, const int32_t* n_nodes,
                      const void* k_c, const void* v_c, const int64_t* seg_off, const int32_t* kept_len, int64_t capacity,
