@@ -49,6 +49,7 @@ struct AttnParams {
   int tile_rows;       // rows of an item at most
   int g_inverse;       // 2^16 / g, rounded up
   int wide_q, wide_out;  // rows begin on 32-byte boundaries
+  int copy_out;          // tensor copies can write whole tiles of results
   int64_t n_items;     // items (without slots) at most; items times slots are fewer than 2^31
   int q_tiles;         // tree: tiles of a unit's rows
   void* ws;

@@ -23,10 +23,13 @@ namespace {
 constexpr int kRows = 128, kKeys = 128, kThreads = 384, kRing = 4;
 constexpr float kMostSum = 65536.f;   // of a tile's weights, against the reference
 
-template <int D>
+template <int D, bool kTree>
 struct Geo {
   static constexpr int kTile = 128 * D * 2;  // bytes of 128 rows: D / 64 blocks of 128 rows of 128 bytes, swizzled
-  static constexpr int kStages = D == 128 ? 5 : 10;
+  // Bytes of 64 columns of a tile's results, on their way out: prompts only. (Trees, which stream from memory, need the stage of keys more:
+  // 896 segments 290 us with five, 297 with four.)
+  static constexpr int kOut = kTree ? 0 : 128 * 128;
+  static constexpr int kStages = D == 64 ? 10 : kTree ? 5 : 4;
   // Tensor memory columns: S and O of either tile of rows, and where narrow heads leave room P, which else lies over the S that it was
   // made of. Apart, S of the next tile of keys is computed as soon as S is in registers, and no product stands in a row's chain
   // (32 / 8 heads of 64, 16384 tokens: 1519 -> 1426 us, 772 TFLOP/s).
@@ -46,18 +49,18 @@ struct Work {
 };
 
 struct Barriers {
-  uint64_t full[10], empty[10], s_full[2], s_empty[2], p_full[2], o_tile[2], o_done[2], q_full, q_empty, item_full[kRing], item_empty[kRing], pair, landed[2], mended[2], drain;
+  uint64_t full[10], empty[10], s_full[2], s_empty[2], p_full[2], o_tile[2], o_done[2], q_full, q_empty, item_full[kRing], item_empty[kRing], pair, landed[2], mended[2], out_free[2], out_there[2], drain;
   Work ring[kRing];
   float2 stats[2][kRows];
   uint32_t tmem;
   int abort;
   int mend_stage[2];  // where the copies that landed[] counts go
 };
-template <int D>
+template <int D, bool kTree>
 constexpr int smem_bytes() {
-  return 2 * Geo<D>::kTile + Geo<D>::kStages * Geo<D>::kTile + (int)sizeof(Barriers);
+  return 2 * Geo<D, kTree>::kTile + Geo<D, kTree>::kStages * Geo<D, kTree>::kTile + 2 * Geo<D, kTree>::kOut + (int)sizeof(Barriers);
 }
-static_assert(smem_bytes<128>() <= 227 * 1024 && smem_bytes<64>() <= 227 * 1024, "shared memory of a block");
+static_assert(smem_bytes<128, false>() <= 227 * 1024 && smem_bytes<128, true>() <= 227 * 1024 && smem_bytes<64, false>() <= 227 * 1024, "shared memory of a block");
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
   asm volatile(
@@ -70,6 +73,12 @@ __device__ __forceinline__ void tma_load_5d_plain(uint32_t dst, const CUtensorMa
       "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
       "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
       : "memory");
+}
+__device__ __forceinline__ void tma_store_5d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3, int c4) {
+  asm volatile("cp.async.bulk.tensor.5d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5, %6}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1),
+               "r"(c2), "r"(c3), "r"(c4)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 // Descriptor of V as the operand whose rows are the contraction: 64 columns (128 bytes) by 8 keys are 1024 bytes, swizzled; the next
 // 8 keys follow 1024 bytes on (the stride offset, as for the other operands), the next 64 columns a block of 128 keys on.
@@ -123,13 +132,14 @@ __device__ __forceinline__ int keys_there(const Work& w, int tile, bool own) { r
 template <int D, bool kTree>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_tk,
-                   const __grid_constant__ CUtensorMap map_tv, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ AttnParams p) {
+                   const __grid_constant__ CUtensorMap map_tv, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_out,
+                   const __grid_constant__ AttnParams p) {
   extern __shared__ __align__(1024) unsigned char base[];
-  constexpr int TILE = Geo<D>::kTile, NST = Geo<D>::kStages, BLOCK = kRows * 128;
-  constexpr bool kApart = Geo<D>::kApart;
-  constexpr int kO = Geo<D>::kO, kP = Geo<D>::kP, kPStep = Geo<D>::kPStep;
-  const uint32_t q_smem = smem_u32(base), ring_smem = q_smem + 2 * TILE;
-  Barriers& sb = *reinterpret_cast<Barriers*>(base + 2 * TILE + NST * TILE);
+  constexpr int TILE = Geo<D, kTree>::kTile, NST = Geo<D, kTree>::kStages, BLOCK = kRows * 128;
+  constexpr bool kApart = Geo<D, kTree>::kApart;
+  constexpr int kO = Geo<D, kTree>::kO, kP = Geo<D, kTree>::kP, kPStep = Geo<D, kTree>::kPStep;
+  const uint32_t q_smem = smem_u32(base), ring_smem = q_smem + 2 * TILE, out_smem = ring_smem + NST * TILE;
+  Barriers& sb = *reinterpret_cast<Barriers*>(base + 2 * TILE + NST * TILE + 2 * Geo<D, kTree>::kOut);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (q_smem & 1023) {  // (the swizzle pattern is one of addresses; the driver places dynamic shared memory so)
     if (threadIdx.x == 0) set_status(p.ws, MADAKV_ECUDA);
@@ -149,7 +159,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&sb.q_empty, 1);
     for (int i = 0; i < kRing; ++i) mbar_init(&sb.item_full[i], 1), mbar_init(&sb.item_empty[i], 1 + 1 + 1 + 8);
     mbar_init(&sb.pair, 8);
-    for (int i = 0; i < 2; ++i) mbar_init(&sb.landed[i], 1), mbar_init(&sb.mended[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sb.landed[i], 1);
+      mbar_init(&sb.mended[i], 1);
+      mbar_init(&sb.out_free[i], 1);
+      mbar_init(&sb.out_there[i], 4);
+    }
     mbar_init(&sb.drain, 1);
     sb.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -174,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = tmem + ((uint32_t)((warp % 4) * 32) << 16), s_tm = lanes + s * 128, o_tm = lanes + kO + s * D, p_tm = lanes + kP + s * kPStep;
     const int r_q = group_of(p, r), r_head = r - r_q * p.g;
     const uint64_t scale2x = pack2(p.scale2, p.scale2);
-    uint32_t n_s = 0, n_o = 0, n_pair = 0;  // tiles of keys done, meetings of the eight warps
+    uint32_t n_s = 0, n_o = 0, n_pair = 0, n_out = 0;  // tiles of keys done, meetings of the eight warps, copies of results
     auto meet = [&] {
       __syncwarp();
       if (lane == 0) mbar_arrive(&sb.pair);
@@ -318,7 +333,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float norm = split ? 1.f : row_factor(l);
       const int64_t row = ((int64_t)w.y * p.slots + w.slot) * p.tile_rows + mt * tok_m * p.g + r;
       __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + it.out_at + (int64_t)t * p.so.token + r_head * p.so.head;
-      if (active && !wait.dead) {
+      if (!kTree && p.copy_out && !dual && !split && (mt ? w.tok1 : w.tok0) == tok_m) {
+        // a whole tile of rows: 64 columns at a time through shared memory, swizzled, and out by a copy. (Rows as they stand in the threads
+        // are 32 lines a store, 2000 clocks a tile: 16 sequences of 1024 tokens 171 -> 165 us, 8 of 4096 995 -> 976.)
+        const bool none = !(l > 0.f || l != l);
+        for (int c = 0; c < D; c += 64) {
+          if (warp % 4 == 0 && lane == 0) {
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            mbar_arrive(&sb.out_free[s]);
+          }
+          __syncwarp();
+          if (!wait.all(&sb.out_free[s], n_out & 1, kSiteDrain)) break;
+#pragma unroll
+          for (int h = 0; h < 64; h += 32) {
+            uint32_t a[32];
+            tmem_ld32(o_tm + c + h, a);
+            tmem_wait_ld();
+            tie32(a);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              a[i] = none || !some ? 0u : pack_bf16x2(__uint_as_float(a[2 * i]) * norm, __uint_as_float(a[2 * i + 1]) * norm);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out_smem + s * Geo<D, kTree>::kOut + r * 128 + (((h / 8 + i) ^ (r & 7)) << 4)),
+                           "r"(a[4 * i]), "r"(a[4 * i + 1]), "r"(a[4 * i + 2]), "r"(a[4 * i + 3])
+                           : "memory");
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sb.out_there[s]);
+          if (warp % 4 == 0) {
+            if (!wait.all(&sb.out_there[s], n_out & 1, kSiteDrain)) break;
+            if (lane == 0) tma_store_5d(&map_out, out_smem + s * Geo<D, kTree>::kOut, c, 0, w.q_row + mt * tok_m, it.h, w.q_outer);
+          }
+          ++n_out;
+        }
+      } else if (active && !wait.dead) {
 #pragma unroll 1
         for (int c = c_begin; c < c_end; c += 32) {
           uint32_t a[32], b[32];
@@ -371,6 +421,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) mbar_arrive(&sb.item_empty[round % kRing]);
       if (wait.dead) break;
     }
+    if (!kTree && warp % 4 == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 8) {
@@ -747,7 +798,7 @@ bool make_query_map(CUtensorMap* map, const void* base, int d, int g, int64_t ro
 
 template <int D, bool kTree>
 int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
-  CUtensorMap mk, mv, tk, tv, mq;
+  CUtensorMap mk, mv, tk, tv, mq, mo;
   p.tile_q = kRows / p.g * 2;
   if constexpr (kTree) {
     const madakv_strides rows{0, 0, 0, D};
@@ -766,6 +817,8 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   const int64_t outer = all ? (int64_t)p.B * p.L : !kTree && p.q_off ? 1 : p.B;
   const void* q = kTree && !all ? (const char*)p.q + p.layer * p.sq.layer * 2 : p.q;
   if (!make_query_map(&mq, q, D, p.g, p.q_rows, p.Hkv, outer, all && p.L > 1 ? p.sq.layer : p.sq.batch, p.sq, p.tile_q / 2)) return -1;
+  p.copy_out = !kTree && make_query_map(&mo, p.out, D, p.g, p.q_rows, p.Hkv, outer, p.so.batch, p.so, p.tile_q / 2);
+  if (!p.copy_out) mo = mq;
   attn_items(p, kTree);
   // (28 / 4 heads, one token, 512 keys: 11 us whole, 14 in two shares; 1024 keys: 14.1 and in four 14.6; 2048: 20.7 and in eight 15.4)
   attn_slots(p, c, kTree, kKeys, {0.85f, 1.7f, 4.f, 8});
@@ -783,11 +836,11 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
     if (const int rc = launch_status()) return rc;
   }
   auto kernel = attn_tc_kernel<D, kTree>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>()) != cudaSuccess) return MADAKV_ECUDA;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, kTree>()) != cudaSuccess) return MADAKV_ECUDA;
   // (few works: as many blocks as all get the same number of them)
   const int64_t works = p.n_items * p.slots, each = p.slots > 1 ? (works + 147) / 148 : 1;
   const int64_t blocks = (works + each - 1) / each;
-  launch_pdl(kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < 148 ? blocks : 148)), dim3(kThreads), smem_bytes<D>(), st, mk, mv, tk, tv, mq, p);
+  launch_pdl(kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < 148 ? blocks : 148)), dim3(kThreads), smem_bytes<D, kTree>(), st, mk, mv, tk, tv, mq, mo, p);
   const int rc = launch_status();
   return rc || p.slots == 1 ? rc : launch_attn_join(p, c, kTree, st);
 }
