@@ -208,7 +208,7 @@ __device__ __forceinline__ int item_tiles(const AttnParams& p, const AttnItem& i
 // Shares of `tiles` tiles of keys that get work, and the tiles of share x: two each at least. Share 0 always takes part.
 __device__ __forceinline__ int shares_of(const AttnParams& p, int tiles) { return tiles < p.least_tiles ? 1 : min(p.slots, (tiles + 1) / 2); }
 __device__ __forceinline__ void share_tiles(int nb, int tiles, int x, int& begin, int& end) {
-  begin = tiles * x / nb;  // (at most 2^14 tiles, 2^5 shares)
+  begin = tiles * x / nb;  // (at most 2^25 tiles, 2^5 shares)
   end = tiles * (x + 1) / nb;
 }
 
