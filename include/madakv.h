@@ -352,6 +352,7 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  * bf16 number, 3.39e38, and elements below 2^-110 keep fewer bits.
  * Every query of a sequence reads whole tiles of up to 128 keys: a row of v that is not finite makes NaN of results of the same sequence
  * whose query stands up to 127 positions before it too. What stands behind a sequence's last key is never used.
+ * out, lse_out, q_win and lse_win overlap neither one another nor an input; out has no dimension of stride 0.
  * Deterministic. Where few queries see many keys the keys are shared out over blocks; a second launch joins the partial results, which stand
  * in the workspace. A bounded wait that runs out is recorded as MADAKV_ETIMEOUT; the call's results are then not to be used, the next
  * call's are whole.                                                                                             */

@@ -218,6 +218,16 @@ def test_prefill_keys_shared_out(dtype, queries):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [0, 1])
+def test_prefill_shares_of_several_items(dtype, causal):
+    """Shares of items of one and of two tiles of rows, of unequal sequences, of either head size."""
+    prompt(dtype, [9001, 1200, 300], 4, 2, 64, queries=[300, 77, 90], causal=causal, seed=1)
+    prompt(dtype, [6007], 7, 1, 128, queries=[57], causal=causal, seed=2)
+    prompt(dtype, [3300, 2047], 2, 2, 128, causal=causal, seed=3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prefill_many_sequences(dtype):
     """More sequences than a warp has lanes, some empty, packed and padded."""
     lens = [(i * 37) % 200 for i in range(75)]
