@@ -52,6 +52,23 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t (&t)[kTerms]) 
 // An infinity as the largest finite bf16 number: its products with terms that are 0 would not be numbers.
 __device__ __forceinline__ float finite(float x) { return fabsf(x) == INFINITY ? copysignf(3.38953139e38f, x) : x; }
 
+// The terms of 8 elements to shared memory, a term's place `term` bytes behind the one before.
+__device__ __forceinline__ void put8(float4 a, float4 b, uint32_t dst, int term) {
+  const float big = fmaxf(max3f(max3f(fabsf(a.x), fabsf(a.y), fabsf(a.z)), fabsf(a.w), fabsf(b.x)), max3f(fabsf(b.y), fabsf(b.z), fabsf(b.w)));
+  if (big == INFINITY) {
+    a = make_float4(finite(a.x), finite(a.y), finite(a.z), finite(a.w));
+    b = make_float4(finite(b.x), finite(b.y), finite(b.z), finite(b.w));
+  }
+  uint32_t t[4][kTerms];
+  split2(a.x, a.y, t[0]);
+  split2(a.z, a.w, t[1]);
+  split2(b.x, b.y, t[2]);
+  split2(b.z, b.w, t[3]);
+#pragma unroll
+  for (int k = 0; k < kTerms; ++k)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + k * term), "r"(t[0][k]), "r"(t[1][k]), "r"(t[2][k]), "r"(t[3][k]) : "memory");
+}
+
 template <int D, bool kTree>
 __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_constant__ AttnParams p) {
   extern __shared__ __align__(1024) unsigned char base[];
@@ -65,7 +82,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
     return;
   }
   if (threadIdx.x == 0) {
-    mbar_init(&sb.q_full, 256);
+    mbar_init(&sb.q_full, 128);
     for (int i = 0; i < 2; ++i) mbar_init(&sb.k_full[i], 256), mbar_init(&sb.k_empty[i], 1), mbar_init(&sb.s_full[i], 1);
     mbar_init(&sb.v_full, 256);
     mbar_init(&sb.v_empty, 1);
@@ -115,6 +132,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
       const int visible_all = __reduce_min_sync(0xffffffffu, visible);
       uint64_t nodes = 0;
       if constexpr (kTree) nodes = valid ? node_mask(p, it, t) : 0;
+      if (tiles > 0) {  // the row's query, while the other warps bring keys
+        const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.q) + it.q_at + (int64_t)t * p.sq.token + r_head * p.sq.head);
+#pragma unroll 4
+        for (int c = 0; c < D / 8; ++c) {
+          const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+          put8(valid ? src[2 * c] : none, valid ? src[2 * c + 1] : none, q_smem + (c / 8) * G::kQBlock + r * 128 + ((c % 8) ^ (r & 7)) * 16, G::kQTerm);
+        }
+        fence_async();
+        mbar_arrive(&sb.q_full);
+      }
       float m = -INFINITY, l = 0.f, o[D];
 #pragma unroll
       for (int c = 0; c < D; ++c) o[c] = 0.f;
@@ -258,21 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int x = x0 + i * 256, r = x / CPR, c = x % CPR;
-          const float big = fmaxf(max3f(max3f(fabsf(w.a[i].x), fabsf(w.a[i].y), fabsf(w.a[i].z)), fabsf(w.a[i].w), fabsf(w.b[i].x)),
-                                  max3f(fabsf(w.b[i].y), fabsf(w.b[i].z), fabsf(w.b[i].w)));
-          if (big == INFINITY) {
-            w.a[i] = make_float4(finite(w.a[i].x), finite(w.a[i].y), finite(w.a[i].z), finite(w.a[i].w));
-            w.b[i] = make_float4(finite(w.b[i].x), finite(w.b[i].y), finite(w.b[i].z), finite(w.b[i].w));
-          }
-          uint32_t t[4][kTerms];
-          split2(w.a[i].x, w.a[i].y, t[0]);
-          split2(w.a[i].z, w.a[i].w, t[1]);
-          split2(w.b[i].x, w.b[i].y, t[2]);
-          split2(w.b[i].z, w.b[i].w, t[3]);
-          const uint32_t dst = to + (c / 8) * block + r * 128 + ((c % 8) ^ (r & 7)) * 16;
-#pragma unroll
-          for (int k = 0; k < kTerms; ++k)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + k * term), "r"(t[0][k]), "r"(t[1][k]), "r"(t[2][k]), "r"(t[3][k]) : "memory");
+          put8(w.a[i], w.b[i], to + (c / 8) * block + r * 128 + ((c % 8) ^ (r & 7)) * 16, term);
         }
       };
       auto rows_of = [&](int x, bool is_v) {
@@ -291,21 +304,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
         return [=](int r) -> const float* { return r < there ? from + r * step : nullptr; };
       };
       static_assert(N * CPR == 4 * 256, "a tile of keys is four pieces a thread");
-      const float* q = reinterpret_cast<const float*>(p.q) + it.q_at;
-      auto q_row = [&](int r) -> const float* {
-        const int rq = group_of(p, r);
-        return rq < queries ? q + (it.q0 + rq) * p.sq.token + (r - rq * p.g) * p.sq.head : nullptr;
-      };
       Pieces k, v;  // (a tile's rows are on their way while the rows before are split)
-      fetch(v, tid, q_row);
       fetch(k, tid, rows_of(0, false));
-      put(v, tid, q_smem, G::kQBlock, G::kQTerm);
-      if constexpr (D == 128) {
-        fetch(v, tid + 1024, q_row);
-        put(v, tid + 1024, q_smem, G::kQBlock, G::kQTerm);
-      }
-      fence_async();
-      mbar_arrive(&sb.q_full);
       // K of the next tile goes before V of this one: V's place is free when the product of the tile before is done, S should not wait for it.
       auto put_k = [&](int x) {
         const int buf = G::kKeyBuffers == 2 ? x & 1 : 0, use = G::kKeyBuffers == 2 ? x >> 1 : x;
