@@ -1,6 +1,8 @@
 // Attention of a prompt and of drafted trees in fp32 on the tensor cores: every operand as three bf16 terms that add up to it exactly
 // (8 leading bits each), a product as the six partial products not below 2^-24 of it, the small ones first, with fp32 sums:
-//   S = Q K^T,  P = exp2(scale * log2(e) * S - m),  O = (O + P' V') * exp2(m' - m),  m the running maximum
+//   S = Q K^T,  P = exp2(scale * log2(e) * S - m),  O = (O + P' V') * exp2(m' - m)
+// with m the maximum up to the tile before which it was last looked at: it stays until a tile's weights add up to more than 2^16 (fp32 has
+// the range, relative errors are the same), and only then the tile is done again with its maximum.
 // The tensor core truncates where it adds, so the results of a tile of keys are summed up on their own and added to O, which a row's thread
 // has in registers, with rounding to the nearest. A block has one item: 128 rows, and its share of their keys, N at a time.
 //   warps 0-3    a row per thread: weights, results
@@ -17,6 +19,7 @@ namespace madakv {
 namespace {
 
 constexpr int kRows = 128, kThreads = 512, kTerms = 3;
+constexpr float kMostSum = 65536.f;  // of a tile's weights, against the reference
 
 template <int D>
 struct Geo {
@@ -145,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
       float m = -INFINITY, l = 0.f, o[D];
 #pragma unroll
       for (int c = 0; c < D; ++c) o[c] = 0.f;
-      auto add_tile = [&](float f) {  // O of the tile before, and what all of it is scaled down by
+      auto add_tile = [&] {  // O of the tile before
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
           uint32_t x[32];
@@ -153,16 +156,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
           tmem_wait_ld();
           tie32(x);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[c + i] = (o[c + i] + __uint_as_float(x[i])) * f;
+          for (int i = 0; i < 32; ++i) o[c + i] += __uint_as_float(x[i]);
         }
       };
       const uint64_t scale2x = pack2(p.scale2, p.scale2);
+      bool look = true;  // rows without a reference
       for (int x = 0; x < tiles; ++x) {
         if (!wait.all(&sb.s_full[x & 1], x >> 1 & 1, kSiteFull)) break;
         tc_fence_after();
-        float f = 1.f;
+        float f = 1.f, part = 0.f;
         uint32_t z[N];
-        if (active) {
+        bool fresh = look;  // the reference is the maximum so far with this tile's (else it has been for a while)
+        while (active) {
 #pragma unroll
           for (int c = 0; c < N; c += 32) tmem_ld32(lanes + G::kS + (x & 1) * N + c, z + c);
           tmem_wait_ld();
@@ -179,16 +184,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
             for (int c = 0; c < N; ++c)
               if (c >= left) z[c] = 0xff800000u;
           }
-          float top[2] = {-INFINITY, -INFINITY};
+          if (fresh) {
+            float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < N; c += 4) {
-            top[0] = max3f(top[0], __uint_as_float(z[c]), __uint_as_float(z[c + 1]));
-            top[1] = max3f(top[1], __uint_as_float(z[c + 2]), __uint_as_float(z[c + 3]));
+            for (int c = 0; c < N; c += 4) {
+              top[0] = max3f(top[0], __uint_as_float(z[c]), __uint_as_float(z[c + 1]));
+              top[1] = max3f(top[1], __uint_as_float(z[c + 2]), __uint_as_float(z[c + 3]));
+            }
+            const float now = fmaxf(m, fmaxf(top[0], top[1]) * p.scale2);
+            f = ex2(m - (now == -INFINITY ? 0.f : now));
+            m = now;
+            look = __any_sync(0xffffffffu, valid && m == -INFINITY);
           }
-          const float now = fmaxf(m, fmaxf(top[0], top[1]) * p.scale2), at = now == -INFINITY ? 0.f : now;
-          f = ex2(m - at);
-          m = now;
-          const uint64_t off2 = pack2(-at, -at);
+          const float off = m == -INFINITY ? 0.f : -m;
+          const uint64_t off2 = pack2(off, off);
           uint64_t sum[2] = {0, 0};
 #pragma unroll
           for (int c = 0; c < N; c += 2) {
@@ -202,12 +211,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
           }
           float lo, hi;
           unpack2(add2(sum[0], sum[1]), lo, hi);
-          l = l * f + (lo + hi);
+          part = lo + hi;
+          if (fresh || __all_sync(0xffffffffu, part <= kMostSum || !valid)) break;
+          fresh = true;
         }
+        l = l * f + part;
         if (x > 0) {  // (the product of the tile before is done: its results are added, its weights may be written over)
           if (!wait.all(&sb.o_full, (x - 1) & 1, kSiteDrain)) break;
           tc_fence_after();
-          if (active) add_tile(f);
+          if (active) {
+            add_tile();
+            if (fresh) {
+#pragma unroll
+              for (int c = 0; c < D; ++c) o[c] *= f;
+            }
+          }
         }
         if (active) {
 #pragma unroll
@@ -231,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
       }
       if (tiles > 0 && wait.all(&sb.o_full, (tiles - 1) & 1, kSiteDrain)) {
         tc_fence_after();
-        if (active) add_tile(1.f);
+        if (active) add_tile();
       }
       tc_fence_before();
       // ---- results ----

@@ -344,6 +344,25 @@ def test_prefill_logits_far_apart(d, size):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [260.0, 14.0, -300.0])
+def test_prefill_logits_far_apart_in_fp32(d, size):
+    """The same in fp32, with rows whose first keys are the smallest and rows whose first are the largest."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    n = 700
+    cfg = config("f32", 1, 1, 2, 1, d, n)
+    q, k, v = torch.full((1, 1, 2, n, d), d ** -0.5, device="cuda"), normal(gen, (1, 1, 1, n, d), "f32"), normal(gen, (1, 1, 1, n, d), "f32")
+    q[:, :, 1] *= -1.0
+    at = torch.arange(0, n, 37, device="cuda")
+    k[0, 0, 0, at] = (size * (1.0 + at / n * 0.5)).unsqueeze(1)
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 2, n), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    see = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+    for h in range(2):
+        check("f32", q[0, 0, h], k[0, 0, 0], v[0, 0, 0], see, d ** -0.5, out[0, 0, h], lse[0, 0, h])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("at", [2, 147, 386, 640, 659])
 def test_prefill_one_bad_key(d, at):
     """One key of NaN, infinities of both signs, in places of a tile that are computed in different ways."""
