@@ -354,7 +354,8 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  * whose query stands up to 127 positions before it too. What stands behind a sequence's last key is never used.
  * out, lse_out, q_win and lse_win overlap neither one another nor an input; out has no dimension of stride 0.
  * Deterministic. Where few queries see many keys the keys are shared out over blocks; a second launch joins the partial results, which stand
- * in the workspace. A bounded wait that runs out is recorded as MADAKV_ETIMEOUT; the call's results are then not to be used, the next
+ * in the workspace. (How many shares goes by q_rows, k_rows and n_max, which the host knows: few queries in a large buffer, with q_len
+ * saying so, are not shared out. Pass a view of the rows that are there.) A bounded wait that runs out is recorded as MADAKV_ETIMEOUT; the call's results are then not to be used, the next
  * call's are whole.                                                                                             */
 int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
                         const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,

@@ -10,7 +10,6 @@
 namespace madakv {
 
 constexpr int kAttnSlots = 32;  // shares of a row's keys at most
-constexpr int kMaxNodes = 64;   // drafted tokens of a tree
 constexpr int kMaxGroup = 64;
 
 struct AttnParams {

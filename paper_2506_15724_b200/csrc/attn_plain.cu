@@ -11,7 +11,6 @@ namespace madakv {
 namespace {
 
 constexpr int M = 64, N = 64, NT = 256;
-constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
