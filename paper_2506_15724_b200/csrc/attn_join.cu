@@ -21,6 +21,14 @@ __global__ void __launch_bounds__(NT) attn_join_kernel(const __grid_constant__ A
   const int per = (p.tile_rows + kRowsOfBlock - 1) / kRowsOfBlock, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const unsigned y = blockIdx.x / per;
   const int r = (int)(blockIdx.x % per) * kRowsOfBlock + warp;
+  // (results are on their way before it is known how many of the places hold some: what the others hold is not used)
+  const int64_t first = (int64_t)y * p.slots * p.tile_rows + r;
+  const Piece* part = reinterpret_cast<const Piece*>(p.part + first * D) + lane;
+  const bool row_there = r < p.tile_rows;
+  float2 ml = row_there && lane < p.slots ? __ldcg(p.part_ml + first + lane * p.tile_rows) : make_float2(-INFINITY, 0.f);
+  Piece v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = row_there && i < p.slots ? __ldcg(part + (int64_t)i * p.tile_rows * 32) : Piece();
   if (warp == 0) {
     AttnItem it;
     const bool there = kTree ? tree_item(p, y, it) : prompt_item(p, y, it);
@@ -31,9 +39,7 @@ __global__ void __launch_bounds__(NT) attn_join_kernel(const __grid_constant__ A
   const AttnItem& it = s_item;
   const int nb = shares_of(p, item_tiles<kTree>(p, it));
   if (nb == 1 || r >= min(p.tile_q, it.n_q - it.q0) * p.g) return;  // (one share: its block has written the result)
-  const int64_t first = (int64_t)y * p.slots * p.tile_rows + r;
-  const float2 ml = lane < nb ? __ldcg(p.part_ml + first + lane * p.tile_rows) : make_float2(-INFINITY, 0.f);
-  const Piece* part = reinterpret_cast<const Piece*>(p.part + first * D) + lane;
+  if (lane >= nb) ml = make_float2(-INFINITY, 0.f);
   float acc[V] = {}, top = ml.x;
 #pragma unroll
   for (int i = 16; i >= 1; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
@@ -42,11 +48,13 @@ __global__ void __launch_bounds__(NT) attn_join_kernel(const __grid_constant__ A
 #pragma unroll
   for (int i = 16; i >= 1; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
   for (int i0 = 0; i0 < nb; i0 += N) {
-    Piece v[N];
+    if (i0 > 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i0 + i < nb ? __ldcg(part + (int64_t)(i0 + i) * p.tile_rows * 32) : Piece();
+      for (int i = 0; i < N; ++i) v[i] = i0 + i < nb ? __ldcg(part + (int64_t)(i0 + i) * p.tile_rows * 32) : Piece();
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      if (i0 + i >= nb) break;
       const float f = __shfl_sync(0xffffffffu, fac, i0 + i);  // (0 beyond the last share)
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[e] += reinterpret_cast<const float*>(&v[i])[e] * f;
