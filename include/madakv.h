@@ -128,7 +128,7 @@ int madakv_score(const madakv_config* cfg, const void* q_win, madakv_strides sq,
  * prompt's last w queries was computed during prefill (Eq. 5), and its log-sum-exp per row is what a fused attention
  * kernel keeps anyway. Same arguments and result as madakv_score, except that
  *   lse     [B, L, H_q, w] fp32 is an INPUT: the natural-log sum-exp of every window row's scaled logits over the
- *           keys the row sees (what madakv_score stores in its `lse`); -inf for a row that sees no key.
+ *           keys the row sees (what madakv_score stores in its `lse`); -inf for a row that sees no key: it adds nothing.
  * psi[u][i] = sum over the group's heads and window rows of exp( scale * q.k_i - lse ). K is read once and nothing
  * is reduced over keys, so the result is only as good as the normalisers supplied. Layer by layer use: pass a
  * config with n_layers = 1 and pointers to that layer's slices.                                             */

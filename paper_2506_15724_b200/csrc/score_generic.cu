@@ -222,8 +222,8 @@ __global__ void __launch_bounds__(NT) score_psi_kernel(ScoreParams p) {
     tile_dots<D>(ks, qs, kl, rg, acc);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int vis = row_visible(p, r0 + rg * 4 + i, n);
       const float lse2 = lse_s[rg * 4 + i];
+      const int vis = lse2 == -INFINITY ? 0 : row_visible(p, r0 + rg * 4 + i, n);  // (a row without weight: exp2f(x + inf) is none)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (key0 + kl + 16 * j < vis) sum[j] += exp2f(acc[j][i] * p.scale2 - lse2);

@@ -1,0 +1,133 @@
+"""The proxy tokens' queries and log-sum-exps on their way from the attention of a prompt to eviction: prompts in one call and in chunks, what
+eviction goes on from, what it refuses. Scores are compared with Eq. 7 in 64 bits; tolerances are sums of roundings."""
+import math
+
+import pytest
+import torch
+
+from paper_2506_15724_b200 import binding as mk
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def normal(gen, shape, dtype):
+    return torch.randn(shape, generator=gen, device="cuda").to(DT[dtype])
+
+
+def i32(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def scores(q_win, k, lens, w, causal=1, drop=None):
+    """Eq. 7 in 64 bits and how far a score may be off: [B, L, H_kv, n] each. drop [B, L, H_q, w]: rows without weight.
+    A logit is a sum of d products in fp32, each addition off by at most a step (d + 8 steps of the sum of magnitudes), once in the log-sum-exp and
+    once in the scores, where the log-sum-exp is part of the sum; it is rounded itself (four half steps), sums over keys and over rows are an addition
+    per 16 at most and 64 more, an exponential is off by less than 8 half steps."""
+    B, L, Hq, _, d = q_win.shape
+    Hkv, n = k.shape[2], k.shape[3]
+    g = Hq // Hkv
+    want, most = (torch.zeros((B, L, Hkv, n), dtype=torch.float64, device="cuda") for _ in range(2))
+    for b in range(B):
+        m = lens[b]
+        at = torch.arange(w, device="cuda") + m - w
+        see = (torch.arange(m, device="cuda") <= at.view(-1, 1)) if causal else (at >= 0).view(-1, 1).expand(w, m)
+        for l in range(L):
+            for h in range(Hq):
+                q, kk = q_win[b, l, h].double(), k[b, l, h // g, :m].double()
+                z = (q @ kk.T * d ** -0.5).masked_fill(~see, -math.inf)
+                lse = torch.logsumexp(z, 1) if m else torch.full((w,), -math.inf, dtype=torch.float64, device="cuda")
+                gone = lse.isinf() if drop is None else lse.isinf() | drop[b, l, h]
+                p = torch.exp(z - lse.masked_fill(gone, 0.0).unsqueeze(1)).masked_fill(gone.unsqueeze(1), 0.0)
+                if not m:
+                    continue
+                mag = (q.abs() @ kk.abs().T * see).amax(1) * d ** -0.5
+                size = lse.masked_fill(gone, 0.0).abs()
+                off = (d + 8) * 2.0 ** -23 * (2 * mag + size) + 4 * 2.0 ** -24 * size + (m / 16 + g * w / 16 + 136) * 2.0 ** -23
+                want[b, l, h // g, :m] += p.sum(0)
+                most[b, l, h // g, :m] += (p * off.unsqueeze(1)).sum(0)
+    return want, most + 1e-30
+
+
+def check_scores(psi, want, most):
+    err = (psi.double() - want).abs()
+    assert torch.all(err <= most), float((err / most).max())  # (a NaN fails)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("path", ["auto", "generic"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,d,w", [(4, 4, 64, 8), (7, 1, 128, 32)])
+def test_rows_without_normaliser_have_no_weight(dtype, path, Hq, Hkv, d, w, monkeypatch):
+    """A log-sum-exp of -inf given for rows that do see keys: they add nothing, whichever kernel takes the call."""
+    if path == "generic":
+        monkeypatch.setenv("MADAKV_SCORE_PATH", "generic")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    B, L, n, lens = 2, 2, 300, [300, 190]
+    cfg = mk.make_config(DT[dtype], B, L, Hq, Hkv, d, n, w)
+    ws = mk.new_workspace(cfg)
+    q, k = normal(gen, (B, L, Hq, w, d), dtype), normal(gen, (B, L, Hkv, n, d), dtype)
+    lse, psi = torch.zeros((B, L, Hq, w), device="cuda"), torch.zeros((B, L, Hkv, n), device="cuda")
+    mk.madakv_score(cfg, q, k, i32(*lens), lse, psi, ws)
+    check_scores(psi, *scores(q, k, lens, w))
+    drop = torch.rand(lse.shape, generator=gen, device="cuda") < 0.4
+    drop[0, 0] = True
+    mk.madakv_score_lse(cfg, q, k, i32(*lens), lse.masked_fill(drop, -math.inf), psi, ws)
+    check_scores(psi, *scores(q, k, lens, w, drop=drop))
+    assert not psi[0, 0].any() and mk.madakv_poll_status(ws) == 0
+
+
+class Prompt:
+    """A prompt of several layers, buffers for it, and the calls of a user that goes through it."""
+
+    def __init__(self, dtype, lens, w=16, L=2, Hq=8, Hkv=2, d=64, causal=1, seed=3):
+        self.gen, self.dtype, self.lens, self.w, self.L, self.causal = torch.Generator(device="cuda").manual_seed(seed), dtype, lens, w, L, causal
+        self.B, self.Hq, self.Hkv, self.d, self.n = len(lens), Hq, Hkv, d, max(lens)
+        self.cfg = mk.make_config(DT[dtype], self.B, L, Hq, Hkv, d, self.n, w, causal=causal, max_new_tokens=4)
+        self.buf = mk.EvictionBuffers(self.cfg, self.B * L * Hkv * (self.n + 4), want_lse=True)
+        self.mask = torch.zeros((self.B, self.n), dtype=torch.uint8, device="cuda")
+        self.mask[:, 3:self.n // 2] = 1
+        self.budget = i32(*[max(1, x // 5) for x in lens])
+        self.new()
+
+    def new(self):  # another prompt of the same lengths
+        shape = lambda h: (self.B, self.L, h, self.n, self.d)  # noqa: E731
+        self.q, self.k, self.v = (normal(self.gen, shape(h), self.dtype) for h in (self.Hq, self.Hkv, self.Hkv))
+        self.out = torch.zeros_like(self.q)
+
+    def chunk(self, layer, begin, end, packed=False):
+        """Queries begin .. end - 1 of every sequence that has them; keys that come later are not there yet."""
+        keys = [min(x, end) for x in self.lens]
+        count = [max(0, x - begin) for x in keys]
+        if not packed:
+            rows = slice(begin, max(begin + 1, min(end, self.n)))
+            return self.buf.run_prefill(layer, self.q[:, :, :, rows], self.k, self.v, self.out[:, :, :, rows], seq_len=i32(*keys), q_len=i32(*count))
+        if not sum(count):
+            return
+        q = torch.cat([self.q[b, :, :, begin:begin + count[b]] for b in range(self.B)], 2)
+        off = [sum(count[:b]) for b in range(self.B + 1)]
+        out = torch.zeros_like(q)
+        self.buf.run_prefill(layer, q, self.k, self.v, out, seq_len=i32(*keys), q_off=torch.tensor(off, device="cuda"))
+        for b in range(self.B):
+            self.out[b, layer, :, begin:begin + count[b]] = out[layer, :, off[b]:off[b + 1]]
+
+    def whole(self, layers=None):
+        for layer in range(self.L) if layers is None else layers:
+            self.buf.run_prefill(layer, self.q, self.k, self.v, self.out, seq_len=i32(*self.lens))
+
+    def evict(self, q_win=None, lens=None):
+        self.buf.run_eviction(q_win, self.k, self.v, self.mask, i32(*(lens or self.lens)), self.budget)
+
+    def window(self):
+        x = torch.zeros((self.B, self.L, self.Hq, self.w, self.d), device="cuda").to(DT[self.dtype])
+        for b, m in enumerate(self.lens):
+            x[b, :, :, max(0, self.w - m):] = self.q[b, :, :, max(0, m - self.w):m]
+        return x
+
+    def check(self):
+        """The window and the scores that the last eviction went by are those of the whole prompt."""
+        assert mk.madakv_poll_status(self.buf.ws) == 0
+        assert torch.equal(self.buf.q_win, self.window())
+        check_scores(self.buf.psi, *scores(self.window(), self.k, self.lens, self.w, self.causal))
+
+    def refused(self):
+        assert mk.madakv_poll_status(self.buf.ws) == mk.ESHAPE
