@@ -301,7 +301,7 @@ class EvictionBuffers:
         self.ws = new_workspace(cfg, device)
         self.psi = z((B, L, Hkv, n), torch.float32)
         self.lse = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
-        self.q_win = None
+        self.q_win = self.lse_win = None  # run_prefill's, a pair: lse holds those of the queries that run_eviction is given
         self.mass = z((B, L, Hkv, 2), torch.float64)
         self.pref = z((B, L, Hkv, 2), torch.float64)
         self.demand = z((B, L, Hkv, 2), torch.int32)
@@ -332,7 +332,8 @@ class EvictionBuffers:
         if self.q_win is None:
             c = self.cfg
             self.q_win = torch.zeros((c.batch, c.n_layers, c.n_q_heads, c.window, c.head_dim), dtype=self.out.dtype, device=self.out.device)
-        madakv_prefill_attn(self.cfg, layer, q, k, v, out, self.ws, q_win=self.q_win, lse_win=self.lse, **lengths)
+            self.lse_win = torch.zeros_like(self.lse)
+        madakv_prefill_attn(self.cfg, layer, q, k, v, out, self.ws, q_win=self.q_win, lse_win=self.lse_win, **lengths)
 
     def run_eviction(self, q_win, k, v, mask, seq_len, budget):
         """Stages 1-4, enqueued on the current stream. q_win None: the queries and log-sum-exps that run_prefill has kept of every layer, with
@@ -341,7 +342,7 @@ class EvictionBuffers:
         if q_win is None:
             if self.q_win is None:
                 raise ValueError("run_eviction: no q_win, and no run_prefill that has kept it")
-            madakv_score_lse(c, self.q_win, k, seq_len, self.lse, self.psi, self.ws)
+            madakv_score_lse(c, self.q_win, k, seq_len, self.lse_win, self.psi, self.ws)
         else:
             madakv_score(c, q_win, k, seq_len, self.lse, self.psi, self.ws)
         madakv_allocate(c, self.psi, mask, seq_len, budget, self.mass, self.pref, self.demand, self.phi, self.budgets,

@@ -131,3 +131,15 @@ class Prompt:
 
     def refused(self):
         assert mk.madakv_poll_status(self.buf.ws) == mk.ESHAPE
+
+
+@pytest.mark.gpu
+def test_a_given_window_leaves_the_kept_one_alone():
+    """Eviction by queries of the caller's between a prefill and the eviction that goes on from it."""
+    p = Prompt("bf16", [300, 200])
+    p.whole()
+    other = normal(p.gen, p.window().shape, "bf16") * 2.0
+    p.evict(other)
+    check_scores(p.buf.psi, *scores(other, p.k, p.lens, p.w))
+    p.evict()
+    p.check()
