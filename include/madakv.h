@@ -12,7 +12,7 @@
  *   a ragged cache in 4 bits      madakv_compact_quant, madakv_decode_attn_quant, madakv_expand_quant
  *   a cache that stays bounded    madakv_decode_attn_track, madakv_evict, madakv_evict_quant
  * and the attention on either side of it, which the paper takes as given:
- *   before it, of the prompt      madakv_prefill_attn (its log-sum-exps are what madakv_score_lse reads)
+ *   before it, of the prompt      madakv_prefill_attn (its log-sum-exps are what madakv_score_lse reads), madakv_prefill_attn_keep
  *   after it, of drafted tokens   madakv_tree_attn, madakv_tree_commit
  *
  * General rules for every entry point
@@ -361,6 +361,21 @@ int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, 
                         const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
                         madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
                         madakv_strides so, float* lse_out, void* q_win, float* lse_win, void* ws, size_t ws_bytes, void* stream);
+
+/* The same, for prompts that come in several calls (chunks) and go on to eviction: q_win and lse_win, which must be given, keep what earlier calls have
+ * left of a sequence's proxy tokens. Of sequence b with n keys and m queries in this call
+ *   m >= min(w, n)  all rows are written, as above
+ *   0 < m           the rows of earlier queries move up by m places and this call's follow them, if the window was complete for a prompt of n - m
+ *                   keys and cfg->causal is set (else earlier queries have not seen all keys); otherwise the window is marked as incomplete and its
+ *                   other rows become 0 and -inf
+ *   m = 0           nothing changes
+ *   win_len [B, L] int32, in and out: the number of keys of the prompt for which a window is complete. -1 in all of it to begin with.
+ * A launch ahead of the attention moves the rows, unless the call has as many queries as keys by its arguments.                  */
+int madakv_prefill_attn_keep(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
+                             const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
+                             madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
+                             madakv_strides so, float* lse_out, void* q_win, float* lse_win, int32_t* win_len, void* ws,
+                             size_t ws_bytes, void* stream);
 
 /* ---- Drafted tokens ----------------------------------------------------------------------------------------------
  * A speculative step: T = nodes (1 .. 64) drafted tokens of every sequence, a tree, are attended to in one call, and the path of them that

@@ -25,7 +25,7 @@ EXPORTS = [
     "madakv_allocate", "madakv_allocate_layer", "madakv_demand_layer",
     "madakv_select", "madakv_compact", "madakv_decode_attn", "madakv_decode_attn_static", "madakv_poll_status",
     "madakv_compact_quant", "madakv_expand_quant", "madakv_decode_attn_quant", "madakv_decode_attn_track", "madakv_evict",
-    "madakv_evict_quant", "madakv_prefill_attn", "madakv_tree_attn", "madakv_tree_commit",
+    "madakv_evict_quant", "madakv_prefill_attn", "madakv_prefill_attn_keep", "madakv_tree_attn", "madakv_tree_commit",
 ]
 
 
@@ -86,6 +86,7 @@ def lib():
         L.madakv_evict_quant.argtypes = [cfgp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
         S = MadakvStrides
         L.madakv_prefill_attn.argtypes = [cfgp, i32, vp, S, i64, vp, vp, vp, S, vp, S, i64, vp, vp, vp, S, vp, vp, vp, vp, sz, vp]
+        L.madakv_prefill_attn_keep.argtypes = [*L.madakv_prefill_attn.argtypes[:-3], vp, vp, sz, vp]
         L.madakv_tree_attn.argtypes = [cfgp, i32, i32, vp, S, vp, S, vp, S] + [vp] * 6 + [i64, vp, S, vp, vp, sz, vp]
         L.madakv_tree_commit.argtypes = [cfgp, i32, i32, vp, vp, vp, vp, S, vp, S] + [vp] * 4 + [i64] + [vp] * 4 + [sz, vp]
         L.madakv_poll_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
@@ -250,12 +251,13 @@ def madakv_evict_quant(cfg, layer, limit, recent, acc, kept_idx, seg_off, kept_l
 
 
 def madakv_prefill_attn(cfg, layer, q, k, v, out, ws, lse_out=None, q_win=None, lse_win=None, q_off=None, k_off=None, seq_len=None,
-                        q_len=None):
+                        q_len=None, win_len=None):
     """Attention of a prompt's layer. q and out [B, L, H_q, rows, d], k and v [B, L, H_kv, rows, d], strided; with q_off (k_off) packed:
-    [L, H, rows, d]. Exactly one of k_off and seq_len is given; without q_off and q_len there are as many queries as keys."""
-    rc = _native.prefill_attn(cfg, int(layer), q, k, v, out, ws, lse_out, q_win, lse_win, q_off, k_off, seq_len, q_len)
+    [L, H, rows, d]. Exactly one of k_off and seq_len is given; without q_off and q_len there are as many queries as keys. With win_len [B, L]
+    int32 (-1 to begin with) q_win and lse_win keep the rows of earlier chunks (madakv_prefill_attn_keep)."""
+    rc = _native.prefill_attn(cfg, int(layer), q, k, v, out, ws, lse_out, q_win, lse_win, q_off, k_off, seq_len, q_len, win_len)
     if rc:
-        raise MadakvError("madakv_prefill_attn", rc)
+        raise MadakvError("madakv_prefill_attn" if win_len is None else "madakv_prefill_attn_keep", rc)
 
 
 def madakv_tree_attn(cfg, layer, q, k_tree, v_tree, mask, k_c, v_c, seg_off, kept_len, out, lse_out, ws, n_nodes=None):
@@ -301,7 +303,11 @@ class EvictionBuffers:
         self.ws = new_workspace(cfg, device)
         self.psi = z((B, L, Hkv, n), torch.float32)
         self.lse = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
-        self.q_win = self.lse_win = None  # run_prefill's, a pair: lse holds those of the queries that run_eviction is given
+        # run_prefill's proxy tokens, and for how many keys they are complete (lse holds the log-sum-exps of queries that run_eviction is given)
+        self.q_win = z((B, L, Hq, cfg.window, d), dt) if want_lse else None
+        self.lse_win = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
+        self.win_len = torch.full((B, L), -1, dtype=torch.int32, device=device) if want_lse else None
+        self.prefilled = False
         self.mass = z((B, L, Hkv, 2), torch.float64)
         self.pref = z((B, L, Hkv, 2), torch.float64)
         self.demand = z((B, L, Hkv, 2), torch.int32)
@@ -325,22 +331,19 @@ class EvictionBuffers:
         self.lse_dec = z((B, L, Hq), torch.float32)
 
     def run_prefill(self, layer, q, k, v, out, **lengths):
-        """Attention of a layer's prompt (lengths: q_off, k_off, seq_len, q_len, lse_out of madakv_prefill_attn). The proxy tokens' queries and
-        log-sum-exps are kept for run_eviction; needs want_lse."""
+        """Attention of a layer's prompt (lengths: q_off, k_off, seq_len, q_len, lse_out of madakv_prefill_attn), whole or in chunks. The proxy
+        tokens' queries and log-sum-exps are kept for run_eviction, over chunks shorter than the window too; needs want_lse."""
         if self.lse is None:
             raise ValueError("run_prefill: buffers without want_lse=True keep no log-sum-exps")
-        if self.q_win is None:
-            c = self.cfg
-            self.q_win = torch.zeros((c.batch, c.n_layers, c.n_q_heads, c.window, c.head_dim), dtype=self.out.dtype, device=self.out.device)
-            self.lse_win = torch.zeros_like(self.lse)
-        madakv_prefill_attn(self.cfg, layer, q, k, v, out, self.ws, q_win=self.q_win, lse_win=self.lse_win, **lengths)
+        madakv_prefill_attn(self.cfg, layer, q, k, v, out, self.ws, q_win=self.q_win, lse_win=self.lse_win, win_len=self.win_len, **lengths)
+        self.prefilled = True
 
     def run_eviction(self, q_win, k, v, mask, seq_len, budget):
         """Stages 1-4, enqueued on the current stream. q_win None: the queries and log-sum-exps that run_prefill has kept of every layer, with
         which K is read once."""
         c = self.cfg
         if q_win is None:
-            if self.q_win is None:
+            if not self.prefilled:
                 raise ValueError("run_eviction: no q_win, and no run_prefill that has kept it")
             madakv_score_lse(c, self.q_win, k, seq_len, self.lse_win, self.psi, self.ws)
         else:

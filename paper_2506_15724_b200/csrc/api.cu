@@ -277,24 +277,38 @@ static bool all_strides_ok(const madakv_config& c, std::initializer_list<madakv_
   return true;
 }
 
+static int prefill(const madakv_config* cfg, int32_t layer, const PromptCall& a, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  if (!a.q || !a.k || !a.v || !a.out) return MADAKV_EINVAL;
+  if ((a.k_off != nullptr) == (a.seq_len != nullptr) || (a.q_off && a.q_len)) return MADAKV_EINVAL;
+  if (layer < 0 || layer >= cfg->n_layers || a.q_rows <= 0 || a.k_rows <= 0) return MADAKV_ESHAPE;
+  if (a.q_rows > 0x7fffffffll || a.k_rows > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
+  if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.out) || !aligned16(a.q_win) || ((uintptr_t)a.q_off & 7) ||
+      ((uintptr_t)a.k_off & 7) || ((uintptr_t)a.q_len & 3) || ((uintptr_t)a.seq_len & 3) || ((uintptr_t)a.lse_out & 3) ||
+      ((uintptr_t)a.lse_win & 3) || ((uintptr_t)a.win_len & 3))
+    return MADAKV_EALIGN;
+  if (!all_strides_ok(*cfg, {a.sq, a.sk, a.sv, a.so})) return MADAKV_EALIGN;
+  if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
+  return launch_prefill_attn(*cfg, layer, a, ws, (cudaStream_t)stream);
+}
+
 int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
                         const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
                         madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
                         madakv_strides so, float* lse_out, void* q_win, float* lse_win, void* ws, size_t ws_bytes, void* stream) {
-  int rc = check_config(cfg);
-  if (rc) return rc;
-  if (!q || !k || !v || !out) return MADAKV_EINVAL;
-  if ((k_off != nullptr) == (seq_len != nullptr) || (q_off && q_len)) return MADAKV_EINVAL;
-  if (layer < 0 || layer >= cfg->n_layers || q_rows <= 0 || k_rows <= 0) return MADAKV_ESHAPE;
-  if (q_rows > 0x7fffffffll || k_rows > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(q_win) || ((uintptr_t)q_off & 7) ||
-      ((uintptr_t)k_off & 7) || ((uintptr_t)q_len & 3) || ((uintptr_t)seq_len & 3) || ((uintptr_t)lse_out & 3) ||
-      ((uintptr_t)lse_win & 3))
-    return MADAKV_EALIGN;
-  if (!all_strides_ok(*cfg, {sq, sk, sv, so})) return MADAKV_EALIGN;
-  if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
-  return launch_prefill_attn(*cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win},
-                             ws, (cudaStream_t)stream);
+  return prefill(cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win, nullptr},
+                 ws, ws_bytes, stream);
+}
+
+int madakv_prefill_attn_keep(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
+                             const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
+                             madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
+                             madakv_strides so, float* lse_out, void* q_win, float* lse_win, int32_t* win_len, void* ws,
+                             size_t ws_bytes, void* stream) {
+  if (!q_win || !lse_win || !win_len) return MADAKV_EINVAL;
+  return prefill(cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win, win_len},
+                 ws, ws_bytes, stream);
 }
 
 // What the two calls on drafted trees share.

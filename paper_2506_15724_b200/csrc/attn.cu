@@ -52,6 +52,11 @@ int launch_prefill_attn(const madakv_config& c, int layer, const PromptCall& a, 
   p.lse_out = a.lse_out;
   p.q_win = a.q_win;
   p.lse_win = a.lse_win;
+  p.win_len = a.win_len;
+  // (calls that hold every key's query leave no earlier row in a window)
+  const bool whole = p.q_off ? p.q_off == p.k_off && p.q_rows >= p.k_rows : !p.q_len && (p.q_rows >= p.k_rows || p.q_rows >= p.n_max);
+  if (p.win_len && !whole)
+    if (const int rc = launch_window_move(p, c, st)) return rc;
   return launch(p, c, false, st);
 }
 

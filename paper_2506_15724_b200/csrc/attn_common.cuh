@@ -30,6 +30,7 @@ struct AttnParams {
   int n_max;
   void* q_win;
   float* lse_win;
+  int32_t* win_len;  // null, or: windows keep the rows of earlier queries, and these are the keys up to which they are complete
   // tree: the drafted rows stand in k and v, the ragged cache here
   const void *k_c, *v_c;
   const int64_t* seg_off;
@@ -150,12 +151,25 @@ __device__ __forceinline__ bool prompt_item(const AttnParams& p, unsigned i, Att
   return true;
 }
 
-// The proxy tokens' rows that are none of the call's queries: log-sum-exp -inf, query 0. `threads` threads of every block.
+// A window without all of its rows, in win_len. (~n: that of a prompt of n keys, which eviction has gone on from.)
+constexpr int32_t kNoWindow = INT32_MIN;
+
+// The proxy tokens' rows that are none of the call's queries: log-sum-exp -inf, query 0. `threads` threads of every block. Where windows keep earlier
+// rows (win_len) those of sequences with fewer new queries than proxy tokens have been moved by the launch before.
 template <int ROW_BYTES>
 __device__ __forceinline__ void fill_window(const AttnParams& p, int thread, int threads) {
   if (!p.lse_win && !p.q_win) return;
   for (int x = blockIdx.x; x < p.B * p.Hq; x += gridDim.x) {
-    const int b = x / p.Hq, none = max(0, p.w - prompt_queries(p, b, p.q_off || p.q_len ? 0 : prompt_keys(p, b)));
+    const int b = x / p.Hq, keys = !p.win_len && (p.q_off || p.q_len) ? 0 : prompt_keys(p, b), queries = prompt_queries(p, b, keys);
+    int none = max(0, p.w - queries);
+    if (p.win_len) {
+      const bool whole = queries >= min(p.w, keys);
+      if (thread == 0 && x % p.Hq == 0 && (whole || queries > 0)) {
+        int32_t* held = p.win_len + b * p.L + p.layer;
+        *held = whole || (p.causal && *held == keys - queries) ? keys : kNoWindow;
+      }
+      if (!whole) none = 0;
+    }
     const int64_t row = (((int64_t)b * p.L + p.layer) * p.Hq + x % p.Hq) * p.w;
     if (p.lse_win)
       for (int r = thread; r < none; r += threads) p.lse_win[row + r] = -INFINITY;
@@ -271,6 +285,7 @@ inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int til
   p.part_ml = reinterpret_cast<float2*>(p.part + (int64_t)kAttnPartRows * c.head_dim);
 }
 
+int launch_window_move(const AttnParams& p, const madakv_config& c, cudaStream_t st);  // ahead of a call whose windows keep earlier rows
 int launch_attn_plain(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);
 int launch_attn_join(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);  // behind a call with shares
 int launch_attn_split(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st);

@@ -341,6 +341,7 @@ struct PromptCall {
   float* lse_out;
   void* q_win;
   float* lse_win;
+  int32_t* win_len;  // null: windows are written in full
 };
 struct TreeCall {
   int nodes;

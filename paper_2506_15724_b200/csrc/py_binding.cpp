@@ -446,7 +446,7 @@ struct Rows {
 
 PyObject* prefill_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  Checked a(args, n, 14);
+  Checked a(args, n, 15);
   if (a.bad_config) return PyLong_FromLong(a.bad_config);
   const int32_t layer = a.integer();
   const bool q_packed = args[10] != Py_None, k_packed = args[11] != Py_None;
@@ -462,7 +462,11 @@ PyObject* prefill_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   float* lse_win = a.array<float>("lse_win", at::kFloat, a.heads * w, true, true);
   const int64_t *q_off = a.array<int64_t>("q_off", at::kLong, B + 1, true, true), *k_off = a.array<int64_t>("k_off", at::kLong, B + 1, true, true);
   const int32_t *seq_len = a.array<int32_t>("seq_len", at::kInt, B, true), *q_len = a.array<int32_t>("q_len", at::kInt, B, true);
+  int32_t* win_len = a.array<int32_t>("win_len", at::kInt, B * a.cfg->n_layers, true, true);
   return without_lock([&] {
+    if (win_len)
+      return madakv_prefill_attn_keep(a.cfg, layer, q.data, q.st, q.rows, q_off, q_len, k.data, k.st, v.data, v.st, k.rows, k_off, seq_len,
+                                      out.data, out.st, lse, q_win, lse_win, win_len, ws, bytes, st);
     return madakv_prefill_attn(a.cfg, layer, q.data, q.st, q.rows, q_off, q_len, k.data, k.st, v.data, v.st, k.rows, k_off, seq_len,
                                out.data, out.st, lse, q_win, lse_win, ws, bytes, st);
   });

@@ -1,11 +1,13 @@
 """The proxy tokens' queries and log-sum-exps on their way from the attention of a prompt to eviction: prompts in one call and in chunks, what
 eviction goes on from, what it refuses. Scores are compared with Eq. 7 in 64 bits; tolerances are sums of roundings."""
+import ctypes
 import math
 
 import pytest
 import torch
 
 from paper_2506_15724_b200 import binding as mk
+from test_prompt_and_trees import FAKE, lib  # noqa: F401
 
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
@@ -76,6 +78,19 @@ def test_rows_without_normaliser_have_no_weight(dtype, path, Hq, Hkv, d, w, monk
     assert not psi[0, 0].any() and mk.madakv_poll_status(ws) == 0
 
 
+def test_keeping_windows_refusals_before_any_launch(lib):  # noqa: F811
+    c = mk.make_config(torch.bfloat16, 1, 1, 4, 4, 128, 512, 8)
+    need, st = mk.madakv_workspace_bytes(c), mk.MadakvStrides(4 * 512 * 128, 4 * 512 * 128, 512 * 128, 128)
+
+    def call(q=FAKE, q_len=None, q_win=FAKE, lse_win=FAKE, win_len=FAKE, size=need - 1):
+        return lib.madakv_prefill_attn_keep(ctypes.byref(c), 0, q, st, 512, None, q_len, FAKE, st, FAKE, st, 512, None, FAKE, FAKE, st, None, q_win, lse_win,
+                                            win_len, FAKE, size, None)
+
+    assert call() == call(q_len=FAKE) == mk.EWORKSPACE
+    assert call(q=None) == call(q_win=None) == call(lse_win=None) == call(win_len=None) == mk.EINVAL
+    assert call(win_len=ctypes.c_void_p(0x10002)) == call(lse_win=ctypes.c_void_p(0x10002)) == call(q_win=ctypes.c_void_p(0x10004)) == mk.EALIGN
+
+
 class Prompt:
     """A prompt of several layers, buffers for it, and the calls of a user that goes through it."""
 
@@ -131,6 +146,44 @@ class Prompt:
 
     def refused(self):
         assert mk.madakv_poll_status(self.buf.ws) == mk.ESHAPE
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,w,ends", [(64, 16, [200, 400, 495, 500]), (128, 16, [497, 498, 500]), (64, 32, [3, 10, 40, 41, 60, 333, 334, 500]),
+                                      (64, 1, [499, 500]), (128, 40, [5, 333, 363, 393, 423, 453, 483, 500])])
+def test_eviction_after_a_prompt_in_chunks(dtype, d, w, ends, packed):
+    """Chunks shorter than the window, sequences that end in earlier chunks than others, one shorter than the window."""
+    p = Prompt(dtype, [500, 333, 9, 41], w=w, d=d)
+    for begin, end in zip([0] + ends, ends):
+        for layer in range(p.L):
+            p.chunk(layer, begin, end, packed)
+    p.evict()
+    p.check()
+
+
+@pytest.mark.gpu
+def test_eviction_after_a_prompt_token_by_token():
+    p = Prompt("bf16", [60, 23], w=24)
+    for layer in range(p.L):
+        for i in range(60):
+            p.chunk(layer, i, i + 1)
+    p.evict()
+    p.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_longer_prompt_goes_on_from_a_whole_one(dtype):
+    """A call of as many queries as keys, then a few tokens more."""
+    p = Prompt(dtype, [300, 200])
+    for layer in range(p.L):
+        p.buf.run_prefill(layer, p.q[:, :, :, :290], p.k[:, :, :, :290], p.v[:, :, :, :290], p.out[:, :, :, :290], seq_len=i32(290, 200))
+    for layer in range(p.L):
+        p.chunk(layer, 290, 300)
+    p.evict()
+    p.check()
 
 
 @pytest.mark.gpu
