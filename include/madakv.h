@@ -135,6 +135,13 @@ int madakv_score(const madakv_config* cfg, const void* q_win, madakv_strides sq,
 int madakv_score_lse(const madakv_config* cfg, const void* q_win, madakv_strides sq, const void* k, madakv_strides sk,
                      const int32_t* seq_len, const float* lse, float* psi, void* ws, size_t ws_bytes, void* stream);
 
+/* madakv_score_lse on the windows that madakv_prefill_attn_keep has left (q_win, lse, win_len), of all layers. Those of a sequence of n = seq_len[b] > 0
+ * keys have to be complete for n keys, and either all of them new or all of them those that this call has scored before (a repetition): else
+ * MADAKV_ESHAPE is recorded and the scores are not to be used. win_len [B, L] int32, in and out: scored windows are marked, so that a layer that
+ * the next prompt has not reached is told from one that it has.                                             */
+int madakv_score_kept(const madakv_config* cfg, const void* q_win, madakv_strides sq, const void* k, madakv_strides sk,
+                      const int32_t* seq_len, const float* lse, int32_t* win_len, float* psi, void* ws, size_t ws_bytes, void* stream);
+
 /* Stages 2-3 (Eq. 6, 8, 9, 10, 11). All sums of psi are taken exactly, in 2^-32 fixed point:
  *   Q(x) = floor(x * 2^32) for x > 0, else 0;   W_m = sum_{i in X_m} Q(psi[u][i])                 (Eq. 6)
  *   pref[u][m] = W_m / (W_v + W_t)  (0 if the denominator is 0)                                    (Eq. 8 ratio)
@@ -367,9 +374,10 @@ int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, 
  *   m >= min(w, n)  all rows are written, as above
  *   0 < m           the rows of earlier queries move up by m places and this call's follow them, if the window was complete for a prompt of n - m
  *                   keys and cfg->causal is set (else earlier queries have not seen all keys); otherwise the window is marked as incomplete and its
- *                   other rows become 0 and -inf
+ *                   other rows become 0 and -inf. (A window that madakv_score_kept has marked is not gone on from.)
  *   m = 0           nothing changes
- *   win_len [B, L] int32, in and out: the number of keys of the prompt for which a window is complete. -1 in all of it to begin with.
+ *   win_len [B, L] int32, in and out: the number of keys of the prompt for which a window is complete. -1 in all of it to begin with; what else
+ *           than such a number it may hold is the two calls' own.
  * A launch ahead of the attention moves the rows, unless the call has as many queries as keys by its arguments.                  */
 int madakv_prefill_attn_keep(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,
                              const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,

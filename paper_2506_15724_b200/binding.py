@@ -22,6 +22,7 @@ STATIC_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = [
     "madakv_abi_version", "madakv_status_string", "madakv_workspace_bytes", "madakv_score", "madakv_score_lse",
+    "madakv_score_kept",
     "madakv_allocate", "madakv_allocate_layer", "madakv_demand_layer",
     "madakv_select", "madakv_compact", "madakv_decode_attn", "madakv_decode_attn_static", "madakv_poll_status",
     "madakv_compact_quant", "madakv_expand_quant", "madakv_decode_attn_quant", "madakv_decode_attn_track", "madakv_evict",
@@ -70,6 +71,7 @@ def lib():
         L.madakv_workspace_bytes.argtypes = [cfgp, ctypes.POINTER(sz)]
         L.madakv_score.argtypes = [cfgp, vp, MadakvStrides, vp, MadakvStrides, vp, vp, vp, vp, sz, vp]
         L.madakv_score_lse.argtypes = [cfgp, vp, MadakvStrides, vp, MadakvStrides, vp, vp, vp, vp, sz, vp]
+        L.madakv_score_kept.argtypes = [cfgp, vp, MadakvStrides, vp, MadakvStrides, vp, vp, vp, vp, vp, sz, vp]
         L.madakv_allocate.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.madakv_allocate_layer.argtypes = [cfgp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.madakv_demand_layer.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -158,6 +160,13 @@ def madakv_score_lse(cfg, q_win, k, seq_len, lse, psi, ws):
     rc = _native.score_lse(cfg, q_win, k, seq_len, lse, psi, ws)
     if rc:
         raise MadakvError("madakv_score_lse", rc)
+
+
+def madakv_score_kept(cfg, q_win, k, seq_len, lse, win_len, psi, ws):
+    """The windows of madakv_prefill_attn with win_len; incomplete ones, or those of different prompts, record ESHAPE."""
+    rc = _native.score_kept(cfg, q_win, k, seq_len, lse, win_len, psi, ws)
+    if rc:
+        raise MadakvError("madakv_score_kept", rc)
 
 
 def madakv_allocate(cfg, psi, mask, seq_len, budget, mass, pref, demand, phi, budgets, ws):
@@ -307,7 +316,7 @@ class EvictionBuffers:
         self.q_win = z((B, L, Hq, cfg.window, d), dt) if want_lse else None
         self.lse_win = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
         self.win_len = torch.full((B, L), -1, dtype=torch.int32, device=device) if want_lse else None
-        self.prefilled = False
+        self.prefilled = set()  # layers that run_prefill has been called for
         self.mass = z((B, L, Hkv, 2), torch.float64)
         self.pref = z((B, L, Hkv, 2), torch.float64)
         self.demand = z((B, L, Hkv, 2), torch.int32)
@@ -336,16 +345,17 @@ class EvictionBuffers:
         if self.lse is None:
             raise ValueError("run_prefill: buffers without want_lse=True keep no log-sum-exps")
         madakv_prefill_attn(self.cfg, layer, q, k, v, out, self.ws, q_win=self.q_win, lse_win=self.lse_win, win_len=self.win_len, **lengths)
-        self.prefilled = True
+        self.prefilled.add(int(layer))
 
     def run_eviction(self, q_win, k, v, mask, seq_len, budget):
         """Stages 1-4, enqueued on the current stream. q_win None: the queries and log-sum-exps that run_prefill has kept of every layer, with
-        which K is read once."""
+        which K is read once. ValueError if there is a layer that run_prefill was never called for; what only the device knows (windows that are not
+        complete for seq_len keys, layers that a new prompt has not reached) records ESHAPE, and the eviction is not to be used."""
         c = self.cfg
         if q_win is None:
-            if not self.prefilled:
-                raise ValueError("run_eviction: no q_win, and no run_prefill that has kept it")
-            madakv_score_lse(c, self.q_win, k, seq_len, self.lse_win, self.psi, self.ws)
+            if len(self.prefilled) < c.n_layers:
+                raise ValueError("run_eviction: no q_win, and layers that run_prefill has kept none of")
+            madakv_score_kept(c, self.q_win, k, seq_len, self.lse_win, self.win_len, self.psi, self.ws)
         else:
             madakv_score(c, q_win, k, seq_len, self.lse, self.psi, self.ws)
         madakv_allocate(c, self.psi, mask, seq_len, budget, self.mass, self.pref, self.demand, self.phi, self.budgets,

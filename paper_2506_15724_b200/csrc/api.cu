@@ -46,15 +46,29 @@ int madakv_score(const madakv_config* cfg, const void* q_win, madakv_strides sq,
   return launch_score(*cfg, q_win, sq, k, sk, seq_len, lse, psi, ws, (cudaStream_t)stream);
 }
 
-int madakv_score_lse(const madakv_config* cfg, const void* q_win, madakv_strides sq, const void* k, madakv_strides sk,
-                     const int32_t* seq_len, const float* lse, float* psi, void* ws, size_t ws_bytes, void* stream) {
-  int rc = check_config(cfg);
-  if (rc) return rc;
+static int check_score_lse(const madakv_config* cfg, const void* q_win, madakv_strides sq, const void* k, madakv_strides sk,
+                           const int32_t* seq_len, const float* lse, const float* psi, const void* ws, size_t ws_bytes) {
+  if (const int rc = check_config(cfg)) return rc;
   if (!q_win || !k || !seq_len || !lse || !psi) return MADAKV_EINVAL;
   if (!aligned16(q_win) || !aligned16(k) || !aligned16(psi) || ((uintptr_t)seq_len & 3) || ((uintptr_t)lse & 3))
     return MADAKV_EALIGN;
   if (!strides_ok(*cfg, sq) || !strides_ok(*cfg, sk)) return MADAKV_EALIGN;
-  if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
+  return check_ws(*cfg, ws, ws_bytes);
+}
+
+int madakv_score_lse(const madakv_config* cfg, const void* q_win, madakv_strides sq, const void* k, madakv_strides sk,
+                     const int32_t* seq_len, const float* lse, float* psi, void* ws, size_t ws_bytes, void* stream) {
+  if (const int rc = check_score_lse(cfg, q_win, sq, k, sk, seq_len, lse, psi, ws, ws_bytes)) return rc;
+  return launch_score_lse(*cfg, q_win, sq, k, sk, seq_len, lse, psi, ws, (cudaStream_t)stream);
+}
+
+int madakv_score_kept(const madakv_config* cfg, const void* q_win, madakv_strides sq, const void* k, madakv_strides sk,
+                      const int32_t* seq_len, const float* lse, int32_t* win_len, float* psi, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_score_lse(cfg, q_win, sq, k, sk, seq_len, lse, psi, ws, ws_bytes);
+  if (rc) return rc;
+  if (!win_len) return MADAKV_EINVAL;
+  if ((uintptr_t)win_len & 3) return MADAKV_EALIGN;
+  if ((rc = launch_window_check(*cfg, seq_len, win_len, ws, (cudaStream_t)stream))) return rc;
   return launch_score_lse(*cfg, q_win, sq, k, sk, seq_len, lse, psi, ws, (cudaStream_t)stream);
 }
 

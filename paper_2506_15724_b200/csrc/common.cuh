@@ -357,6 +357,7 @@ struct TreeCall {
   int64_t capacity;
 };
 int launch_prefill_attn(const madakv_config& c, int layer, const PromptCall& a, void* ws, cudaStream_t st);
+int launch_window_check(const madakv_config& c, const int32_t* seq_len, int32_t* win_len, void* ws, cudaStream_t st);
 int launch_tree_attn(const madakv_config& c, int layer, const TreeCall& a, const void* k_c, const void* v_c, const int32_t* kept_len,
                      void* out, madakv_strides so, float* lse_out, void* ws, cudaStream_t st);
 int launch_tree_commit(const madakv_config& c, int layer, const TreeCall& a, const int32_t* node, void* k_c, void* v_c,

@@ -99,6 +99,23 @@ PyObject* score(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+PyObject* score_kept(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(args, n, 8);
+  const madakv_config* cfg = a.config();
+  const at::Tensor &q = a.tensor(), &k = a.tensor();
+  const madakv_strides sq = strides(q), sk = strides(k);
+  const int32_t* seq_len = a.ptr<int32_t>();
+  const float* lse = a.ptr<float>();
+  int32_t* win_len = a.ptr<int32_t>();
+  float* psi = a.ptr<float>();
+  const at::Tensor& ws = a.tensor();
+  void *qp = q.data_ptr(), *kp = k.data_ptr(), *wp = ws.data_ptr(), *st = stream();
+  const size_t bytes = (size_t)ws.numel();
+  return without_lock([&] { return madakv_score_kept(cfg, qp, sq, kp, sk, seq_len, lse, win_len, psi, wp, bytes, st); });
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* allocate(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Args a(args, n, 11);
@@ -537,6 +554,7 @@ PyCFunction as_method(F f) {
 PyMethodDef methods[] = {
     {"score", as_method(score<false>), METH_FASTCALL, nullptr},
     {"score_lse", as_method(score<true>), METH_FASTCALL, nullptr},
+    {"score_kept", as_method(score_kept), METH_FASTCALL, nullptr},
     {"allocate", as_method(allocate), METH_FASTCALL, nullptr},
     {"allocate_layer", as_method(allocate_layer), METH_FASTCALL, nullptr},
     {"demand_layer", as_method(demand_layer), METH_FASTCALL, nullptr},

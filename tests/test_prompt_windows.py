@@ -91,6 +91,18 @@ def test_keeping_windows_refusals_before_any_launch(lib):  # noqa: F811
     assert call(win_len=ctypes.c_void_p(0x10002)) == call(lse_win=ctypes.c_void_p(0x10002)) == call(q_win=ctypes.c_void_p(0x10004)) == mk.EALIGN
 
 
+def test_scores_of_kept_windows_refusals_before_any_launch(lib):  # noqa: F811
+    c = mk.make_config(torch.bfloat16, 1, 1, 4, 4, 128, 512, 8)
+    need, st = mk.madakv_workspace_bytes(c), mk.MadakvStrides(4 * 512 * 128, 4 * 512 * 128, 512 * 128, 128)
+
+    def call(q=FAKE, k=FAKE, seq=FAKE, lse=FAKE, win_len=FAKE, psi=FAKE, size=need):
+        return lib.madakv_score_kept(ctypes.byref(c), q, st, k, st, seq, lse, win_len, psi, FAKE, size, None)
+
+    assert call(q=None) == call(k=None) == call(seq=None) == call(lse=None) == call(win_len=None) == call(psi=None) == mk.EINVAL
+    assert call(win_len=ctypes.c_void_p(0x10002)) == call(lse=ctypes.c_void_p(0x10002)) == call(q=ctypes.c_void_p(0x10004)) == mk.EALIGN
+    assert call(size=need - 1) == mk.EWORKSPACE
+
+
 class Prompt:
     """A prompt of several layers, buffers for it, and the calls of a user that goes through it."""
 
@@ -196,3 +208,105 @@ def test_a_given_window_leaves_the_kept_one_alone():
     check_scores(p.buf.psi, *scores(other, p.k, p.lens, p.w))
     p.evict()
     p.check()
+
+
+@pytest.mark.gpu
+def test_eviction_refuses_a_layer_that_was_never_run():
+    p = Prompt("bf16", [300, 200], L=3)
+    with pytest.raises(ValueError):
+        p.evict()
+    p.whole([0, 2])
+    with pytest.raises(ValueError):
+        p.evict()
+    p.whole([1])
+    p.evict()
+    p.check()
+
+
+@pytest.mark.gpu
+def test_eviction_reports_windows_of_different_prompts():
+    """A second prompt whose prefill has not reached every layer: some windows are still the first prompt's."""
+    p = Prompt("bf16", [300, 200], L=3)
+    p.whole()
+    p.evict()
+    p.check()
+    first = p.buf.kept_idx.clone()
+    p.evict()  # the same again
+    p.check()
+    assert torch.equal(first, p.buf.kept_idx)
+    p.new()
+    p.whole([1])
+    p.evict()
+    p.refused()
+    p.evict()  # (it stays refused)
+    p.refused()
+    p.whole([0, 2])
+    p.evict()
+    p.check()
+
+
+@pytest.mark.gpu
+def test_eviction_reports_windows_of_other_lengths():
+    p = Prompt("bf16", [300, 200])
+    p.whole()
+    p.evict(lens=[300, 199])
+    p.refused()
+    p.evict()
+    p.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [0, 1])
+def test_eviction_reports_incomplete_windows(causal):
+    """Fewer new queries than proxy tokens, and nothing before them (or, where every query sees every key, keys that they did not see)."""
+    p = Prompt("bf16", [300, 200], causal=causal)
+    for layer in range(p.L):
+        p.chunk(layer, 290, 300)
+    p.evict()
+    p.refused()
+    for ends in ([300], [100, 290, 300], [150, 300]):
+        p.new()
+        for layer in range(p.L):
+            for begin, end in zip([0] + ends, ends):
+                p.chunk(layer, begin, end)
+        p.evict()
+        if causal == 0 and ends == [100, 290, 300]:
+            p.refused()
+        else:
+            p.check()
+    # a prompt whose eviction has been is not gone on from: what stands before may be another's
+    p.new()
+    for layer in range(p.L):
+        p.chunk(layer, 295, 300)
+    p.evict()
+    p.refused()
+
+
+@pytest.mark.gpu
+def test_captured_chunks_and_evictions():
+    """Chunks and eviction in a graph, replayed for other prompts; and chunks in graphs of their own."""
+    p = Prompt("bf16", [300, 200])
+    ends = [150, 296, 300]
+    spans = list(zip([0] + ends, ends))
+    counts = [(i32(*[min(x, e) for x in p.lens]), i32(*[max(0, min(x, e) - b) for x in p.lens])) for b, e in spans]
+    lens = i32(*p.lens)
+
+    def prefill(span):
+        (begin, end), (keys, count) = spans[span], counts[span]
+        for layer in range(p.L):
+            p.buf.run_prefill(layer, p.q[:, :, :, begin:end], p.k, p.v, p.out[:, :, :, begin:end], seq_len=keys, q_len=count)
+
+    def evict():
+        p.buf.run_eviction(None, p.k, p.v, p.mask, lens, p.budget)
+
+    graphs = [torch.cuda.CUDAGraph() for _ in range(5)]
+    for graph, calls in zip(graphs, ([lambda i=i: prefill(i) for i in range(3)] + [evict], *[[lambda i=i: prefill(i)] for i in range(3)], [evict])):
+        with torch.cuda.graph(graph):
+            for call in calls:
+                call()
+    for run in (graphs[:1], graphs[1:], graphs[:1]):
+        q, k = normal(p.gen, p.q.shape, "bf16"), normal(p.gen, p.k.shape, "bf16")
+        p.q.copy_(q), p.k.copy_(k)
+        for graph in run:
+            graph.replay()
+        p.check()
