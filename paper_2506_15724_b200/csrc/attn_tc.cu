@@ -190,10 +190,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int r_q = group_of(p, r), r_head = r - r_q * p.g;
     const uint64_t scale2x = pack2(p.scale2, p.scale2);
     uint32_t n_s = 0, n_o = 0, n_pair = 0, n_out = 0;  // tiles of keys done, meetings of the eight warps, copies of results
-    auto meet = [&] {
+    auto meet = [&] {  // (each half has waited for its own accumulator's products and goes on to read the other half's)
+      tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sb.pair);
       wait.all(&sb.pair, n_pair++ & 1, kSiteTile);
+      tc_fence_after();
     };
     for (uint32_t round = 0;; ++round) {
       const Work& w = sb.ring[round % kRing];
