@@ -357,6 +357,9 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  * rounded to bf16 before the product with v (their sum is not), out is rounded once. fp32: an element counts as three bf16 terms (24 bits),
  * a product as those of their products that are not below 2^-24 of it, sums are fp32; an infinite element counts as the largest finite
  * bf16 number, 3.39e38, and elements below 2^-110 keep fewer bits.
+ * Range: values of v up to 2^96 in magnitude. (The maximum that weights are taken against is one of some of a row's keys, whose weights may add up to 2^16 a
+ * tile: beyond, sums may overflow and give infinities or NaN for finite values.) Weights below 2^-126 of it are off by as much as 2^-127 or are 0; a
+ * key that a query does not see has weight 0 whatever its value, as long as that is finite.
  * Every query of a sequence reads whole tiles of up to 128 keys: a row of v that is not finite makes NaN of results of the same sequence
  * whose query stands up to 127 positions before it too. What stands behind a sequence's last key is never used.
  * out, lse_out, q_win and lse_win overlap neither one another nor an input; out has no dimension of stride 0.

@@ -87,14 +87,15 @@ __host__ __device__ constexpr uint32_t instr_desc_pv(int n) { return instr_desc_
 
 // 2^x of two numbers without the exponential unit, which is what bounds narrow heads: x = j + f, |f| <= 1/2; 2^f as the polynomial of
 // degree 5 with the least largest relative error (7.5e-8, by exchange; 2.1e-7 with its roundings, as good as the unit's), j added to its
-// exponent. At most 2^-126 from -126 down, and above 2^16 from there up and for NaN: the tile is then done again, by the unit.
+// exponent. From -127 down 2^-149, which bf16 rounds to 0 (a key that is not seen has no weight, whatever its value), off by at most 2^-127 from
+// there to -126; above 2^16 from there up and for NaN: the tile is then done again, by the unit.
 // (Of 8 pairs one: 32 / 8 heads of 64, 16384 tokens 1426 -> 1359 us, 809 TFLOP/s; of 16 pairs one or three and of 4 pairs one gain less,
 // of 8 pairs three nothing. Heads of 128, which the products bound, lose by any.)
 __device__ __forceinline__ void exp2_pair(float& lo, float& hi) {
   constexpr float kC0 = 1.00000012f, kC1 = 0.693146944f, kC2 = 0.240221202f, kC3 = 0.0555071309f, kC4 = 0.00967554096f, kC5 = 0.00132764725f;
   constexpr float kRound = 12582912.f;  // 1.5 * 2^23: a sum's last bit is 1
   auto clamp = [](float x) {
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-126.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-127.f));
     asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(127.f));
     return x;
   };
