@@ -160,12 +160,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
         }
       };
       const uint64_t scale2x = pack2(p.scale2, p.scale2);
-      bool look = true;  // rows without a reference
+      bool look = true;  // rows without a reference, or with one of huge logits
       for (int x = 0; x < tiles; ++x) {
         if (!wait.all(&sb.s_full[x & 1], x >> 1 & 1, kSiteFull)) break;
         tc_fence_after();
         float f = 1.f, part = 0.f;
         uint32_t z[N];
+        float ref = m;
         bool fresh = look;  // the reference is the maximum so far with this tile's (else it has been for a while)
         while (active) {
 #pragma unroll
@@ -191,12 +192,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
               top[0] = max3f(top[0], __uint_as_float(z[c]), __uint_as_float(z[c + 1]));
               top[1] = max3f(top[1], __uint_as_float(z[c + 2]), __uint_as_float(z[c + 3]));
             }
-            const float now = fmaxf(m, fmaxf(top[0], top[1]) * p.scale2);
-            f = ex2(m - (now == -INFINITY ? 0.f : now));
-            m = now;
-            look = __any_sync(0xffffffffu, valid && m == -INFINITY);
+            const float now = fmaxf(m, fmaxf(top[0], top[1]));
+            f = m == -INFINITY ? 0.f : ex2((m - now) * p.scale2);
+            m = ref = now;
+            const bool huge = valid && beyond_rounding(m, p.scale2);
+            look = __any_sync(0xffffffffu, huge || (valid && m == -INFINITY));
+            if (huge) {
+              ref = 0.f;
+#pragma unroll
+              for (int c = 0; c < N; ++c) z[c] = __float_as_uint(__uint_as_float(z[c]) - m);
+            }
           }
-          const float off = m == -INFINITY ? 0.f : -m;
+          const float off = ref == -INFINITY ? 0.f : -ref * p.scale2;
           const uint64_t off2 = pack2(off, off);
           uint64_t sum[2] = {0, 0};
 #pragma unroll
@@ -274,8 +281,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(const __grid_co
           for (int i = 0; i < 8; ++i) x[i] = none ? 0u : __float_as_uint(o[c + i] * norm);
           store32(dst + c, x, split || p.wide_out);
         }
-        if (split) p.part_ml[row] = make_float2(m, l);
-        else finish(t, r_head, row_lse(m, l));
+        if (split) p.part_ml[row] = make_float2(m * p.scale2, l);
+        else finish(t, r_head, row_lse(m * p.scale2, l));
       }
     }
   } else {

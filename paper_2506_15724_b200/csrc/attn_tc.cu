@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int stride = dual ? 2 : 1, tile_end = dual || s ? w.end : w.end0;
       int tile = w.begin + (dual ? s : 0);
       const bool some = tile < tile_end;
-      bool look = true;  // rows without a reference
+      bool look = true;  // rows without a reference, or with one of huge logits
       for (bool first = true; tile < tile_end; tile += stride, first = false) {
         if (!wait.all(&sb.s_full[s], n_s & 1, kSiteFull)) break;
         tc_fence_after();
@@ -242,8 +242,9 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (c >= left) z[c] = 0xff800000u;
           }
           // weights of the tile to where the product reads them; their sum is good where they were taken against a fit reference
+          float ref = m;
           auto weights = [&](auto exact) {
-            const float off = m == -INFINITY ? 0.f : -m * p.scale2;
+            const float off = ref == -INFINITY ? 0.f : -ref * p.scale2;
             const uint64_t off2 = pack2(off, off);
             uint64_t sum[2] = {0, 0};
 #pragma unroll
@@ -283,8 +284,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const float now = fmaxf(top[0], top[1]), f = m == -INFINITY ? 0.f : ex2((m - now) * p.scale2);
             l *= f;
-            m = now;
-            look = __any_sync(0xffffffffu, valid && m == -INFINITY);
+            m = ref = now;
+            const bool huge = valid && beyond_rounding(m, p.scale2);
+            look = __any_sync(0xffffffffu, huge || (valid && m == -INFINITY));
+            if (huge) {
+              ref = 0.f;
+#pragma unroll
+              for (int c = 0; c < kKeys; ++c) z[c] = __float_as_uint(__uint_as_float(z[c]) - m);
+            }
             // (P over S: S of this tile has arrived, so the product before it, which was issued before, is done)
             if (!first) {
               if (kApart && !wait.all(&sb.o_tile[s], (n_s - 1) & 1, kSiteDrain)) break;

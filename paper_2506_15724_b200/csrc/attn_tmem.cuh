@@ -104,6 +104,9 @@ __device__ __forceinline__ void load32(const void* from, uint32_t* r, bool wide)
     r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w, r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
   }
 }
+// Weights are 2^(z * scale - round(m * scale)): all of a row's share the factor that the rounding leaves, 2^-24 of the logit in the exponent. True: that
+// is so much that weights or their sum leave fp32's range; the row's logits are then taken less m before they are scaled.
+__device__ __forceinline__ bool beyond_rounding(float m, float scale2) { return fabsf(fmaf(m, scale2, -__fmul_rn(m, scale2))) > 8.f; }  // (of infinities: false)
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));

@@ -59,6 +59,93 @@ def test_huge_values_do_not_reach_nodes_that_do_not_see_them(dtype, d):
     assert torch.equal(outs[0][..., :17, :], outs[1][..., :17, :]) and outs[0].isfinite().all()
 
 
+# ------------------------------------------------------------------------------------------------- infinities in fp32
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [2, 147, 386, 640])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_infinite_keys_in_fp32(d, at, sign):
+    """An infinite element counts as the largest finite bf16 number: the key has all of the weight, or none. (Queries below 2^-7 in magnitude: the
+    products stay finite.)"""
+    gen = torch.Generator(device="cuda").manual_seed(at)
+    n = 700
+    cfg = config("f32", 1, 1, 1, 1, d, n)
+    q = (torch.rand((1, 1, 1, n, d), generator=gen, device="cuda") + 0.01) * torch.where(torch.rand((1, 1, 1, n, 1), generator=gen, device="cuda") < 0.5, -1, 1) / 256
+    k, v = normal(gen, (1, 1, 1, n, d), "f32"), normal(gen, (1, 1, 1, n, d), "f32")
+    k[0, 0, 0, at, 5] = sign * math.inf
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 1, n), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=i32(n))
+    qq, kk, vv, oo, yy = q[0, 0, 0], k[0, 0, 0], v[0, 0, 0], out[0, 0, 0], lse[0, 0, 0]
+    check("f32", qq[:at], kk[:at], vv[:at], causal(n)[:at, :at], d ** -0.5, oo[:at], yy[:at])
+    later = torch.arange(n, device="cuda") >= at
+    all_of_it, none = later & (qq[:, 5] * sign > 0), later & (qq[:, 5] * sign < 0)
+    want = (qq.double() @ kk.double().nan_to_num(posinf=BIG_BF16, neginf=-BIG_BF16)[at]) * d ** -0.5
+    assert all_of_it.sum() > 3 and none.sum() > 3
+    assert torch.all((oo[all_of_it] - vv[at]).abs() <= 2.0 ** -22 * vv[at].abs())
+    assert torch.all((yy.double() - want).abs()[all_of_it] <= 2.0 ** -20 * want.abs()[all_of_it])
+    rest = torch.arange(n, device="cuda") != at
+    some = none & (torch.arange(n, device="cuda") > 0)
+    check("f32", qq[some], kk[rest], vv[rest], causal(n)[some][:, rest], d ** -0.5, oo[some], yy[some])
+
+
+# ------------------------------------------------------------------------------------------------- logits beyond what exponentials tell apart
+def check_ties(dtype, q, k, v, see, scale, out, lse):
+    """Logits that are exact and equal or very far apart: what is left are roundings of weights, sums and results (as in check)."""
+    z = (q.double() @ k.double().T * scale).masked_fill(~see, -math.inf)
+    want_lse, w = torch.logsumexp(z, 1), torch.softmax(z, 1)  # (less the maximum first: a log-sum-exp of 2^58 has no room for the logarithm)
+    want = w @ v.double()
+    sums = (k.shape[0] / 16 + 64) * 2.0 ** -23
+    most = HALF[dtype] * want.abs() + ((HALF[dtype] if dtype == "bf16" else 0.0) + sums) * (w @ v.double().abs()) + 1e-30
+    err = (out.double() - want).abs()
+    assert torch.all(err <= most), float((err / most).nan_to_num(math.inf).max())
+    assert torch.all((lse.double() - want_lse).abs() <= sums + 2.0 ** -21 * want_lse.abs())
+
+
+def steps_of(gen, n, d, size, low, dtype):
+    k = torch.zeros((n, d), device="cuda")
+    k[:, 0] = torch.randint(low, low + 6, (n,), generator=gen, device="cuda").float() * size
+    return k.to(DT[dtype])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [10, 24, 35, 61, 100])
+@pytest.mark.parametrize("low", [-6, -2, 1])
+@pytest.mark.parametrize("n,m", [(700, 700), (9000, 40)])
+def test_prefill_of_huge_logits(dtype, d, power, low, n, m):
+    """The keys with the largest logit share the weight equally, also where a logit's rounding is larger than what separates weights."""
+    gen = torch.Generator(device="cuda").manual_seed(power)
+    cfg = config(dtype, 1, 1, 1, 1, d, n)
+    q, v = torch.zeros((1, 1, 1, m, d), device="cuda").to(DT[dtype]), normal(gen, (1, 1, 1, n, d), dtype)
+    q[..., 0] = 1.0
+    k = steps_of(gen, n, d, 2.0 ** power, low, dtype).view(1, 1, 1, n, d)
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 1, m), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=i32(n), q_len=i32(m))
+    see = torch.arange(n, device="cuda") <= torch.arange(m, device="cuda").view(-1, 1) + n - m
+    check_ties(dtype, q[0, 0, 0], k[0, 0, 0], v[0, 0, 0], see, d ** -0.5, out[0, 0, 0], lse[0, 0, 0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [10, 35, 100])
+@pytest.mark.parametrize("n", [0, 300, 9000])
+def test_trees_of_huge_logits(dtype, d, power, n):
+    gen = torch.Generator(device="cuda").manual_seed(power)
+    T, seg = 20, Segments(gen, dtype, [n], d)
+    cfg = config(dtype, 1, 1, 1, 1, d, max(n, 1))
+    q, v = torch.zeros((1, 1, 1, T, d), device="cuda").to(DT[dtype]), normal(gen, (1, 1, 1, T, d), dtype)
+    q[..., 0] = 1.0
+    seg.k[:n] = steps_of(gen, n, d, 2.0 ** power, -4, dtype)
+    k = steps_of(gen, T, d, 2.0 ** power, -3, dtype).view(1, 1, 1, T, d)
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 1, T), device="cuda")
+    mk.madakv_tree_attn(cfg, -1, q, k, v, as_int64([[(1 << (i + 1)) - 1 for i in range(T)]]), seg.k, seg.v, seg.seg_off, seg.kept_len, out, lse,
+                        mk.new_workspace(cfg))
+    see = torch.cat((torch.ones((T, n), dtype=torch.bool, device="cuda"), causal(T)), 1)
+    check_ties(dtype, q[0, 0, 0], torch.cat((seg.k[:n], k[0, 0, 0])), torch.cat((seg.v[:n], v[0, 0, 0])), see, d ** -0.5, out[0, 0, 0], lse[0, 0, 0])
+
+
 # ------------------------------------------------------------------------------------------------- strides
 def shifted(x):
     """The same numbers in rows that begin on 16-byte boundaries of which no two neighbours are 32-byte ones."""
