@@ -360,8 +360,9 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  * Range: values of v up to 2^96 in magnitude. (The maximum that weights are taken against is one of some of a row's keys, whose weights may add up to 2^16 a
  * tile: beyond, sums may overflow and give infinities or NaN for finite values.) Weights below 2^-126 of it are off by as much as 2^-127 or are 0; a
  * key that a query does not see has weight 0 whatever its value, as long as that is finite.
- * Every query of a sequence reads whole tiles of up to 128 keys: a row of v that is not finite makes NaN of results of the same sequence
- * whose query stands up to 127 positions before it too. What stands behind a sequence's last key is never used.
+ * Up to 128 / g queries of a sequence share a tile of rows (g = H_q / H_kv), which reads whole tiles of up to 128 keys as far as the last of them
+ * sees: a row of v that is not finite makes NaN of results of the same KV head's queries up to 126 + floor(128 / g) positions before it too.
+ * What stands behind a sequence's last key is never used.
  * out, lse_out, q_win and lse_win overlap neither one another nor an input; out has no dimension of stride 0.
  * Deterministic. Where few queries see many keys the keys are shared out over blocks; a second launch joins the partial results, which stand
  * in the workspace. (How many shares goes by q_rows, k_rows and n_max, which the host knows: few queries in a large buffer, with q_len
@@ -400,7 +401,8 @@ int madakv_prefill_attn_keep(const madakv_config* cfg, int32_t layer, const void
  * bit set) gets out = 0 and lse = -inf; a segment that selection refused counts as empty. The cache is only read.
  *   lse_out [B, L, H_q, T] fp32, contiguous, or null
  * Rows of out and lse_out of nodes that are not there are left as they were. Roundings as in madakv_prefill_attn; H_q / H_kv at most 64. A
- * row of the segment's or of a node's value that is not finite makes NaN of the results of all nodes of the sequence, seen or not. */
+ * row of the segment's or of a node's value that is not finite makes NaN of the results of all nodes on the same segment, seen or not. (A tree of one
+ * node rounds its weights to bf16 for any g; madakv_decode_attn does from g = 3 on.)                                                    */
 int madakv_tree_attn(const madakv_config* cfg, int32_t layer, int32_t nodes, const void* q, madakv_strides sq, const void* k_tree,
                      madakv_strides sk, const void* v_tree, madakv_strides sv, const uint64_t* mask, const int32_t* n_nodes,
                      const void* k_c, const void* v_c, const int64_t* seg_off, const int32_t* kept_len, int64_t capacity,

@@ -59,6 +59,26 @@ def test_huge_values_do_not_reach_nodes_that_do_not_see_them(dtype, d):
     assert torch.equal(outs[0][..., :17, :], outs[1][..., :17, :]) and outs[0].isfinite().all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,d,shift", [(1, 128, 0), (1, 128, 1), (1, 64, 1), (7, 128, 0), (7, 64, 3), (2, 64, 77)])
+@pytest.mark.parametrize("at", [255, 260, 639])
+def test_a_value_that_is_no_number_reaches_so_far(dtype, Hq, d, shift, at):
+    """NaN in a row of V: in the results of the queries that see it, and of none that stands more than 126 + floor(128 / g) positions before it."""
+    gen = torch.Generator(device="cuda").manual_seed(at)
+    n, g = 700 + shift, Hq
+    cfg = config(dtype, 1, 1, Hq, 1, d, n)
+    q, k, v = normal(gen, (1, 1, Hq, 700, d), dtype), normal(gen, (1, 1, 1, n, d), dtype), normal(gen, (1, 1, 1, n, d), dtype)
+    v[0, 0, 0, at, 3] = math.nan
+    out, lse = torch.empty_like(q), torch.empty((1, 1, Hq, 700), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=i32(n), q_len=i32(700))
+    assert lse.isfinite().all() and out[0, 0, :, at - shift:, 3].isnan().all()
+    clean = max(0, at - (126 + 128 // g) - shift)  # queries; query i stands at i + shift
+    see = torch.arange(n, device="cuda") <= torch.arange(clean, device="cuda").view(-1, 1) + shift
+    for h in range(Hq):
+        check(dtype, q[0, 0, h, :clean], k[0, 0, 0], v[0, 0, 0].nan_to_num(0.0), see, d ** -0.5, out[0, 0, h, :clean], lse[0, 0, h, :clean])
+
+
 # ------------------------------------------------------------------------------------------------- infinities in fp32
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
