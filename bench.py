@@ -477,7 +477,7 @@ class Bench:
         # a single layer may be given far more than the nominal budget by the compensation of Eq. 10-11
         per_layer = wl.B * wl.Hkv * (wl.n + wl.max_new_tokens)
         one = [mk.EvictionBuffers(cfg1, per_layer, device=self.dev) for _ in range(slots)]
-        ws_side = [mk.new_workspace(buf.cfg, self.dev) for _ in range(slots)]  # allocate_layer's and select's workspace
+        ws_side = [mk.new_workspace(buf.cfg, self.dev, attention=False) for _ in range(slots)]  # allocate_layer's and select's workspace
         lse = torch.empty((wl.B, wl.L, wl.Hq, wl.w), dtype=torch.float32, device=self.dev)
         mk.madakv_score(buf.cfg, inp["q_win"], inp["k"], inp["seq_len"], lse, buf.psi, buf.ws)
         lse_l = [lse[:, l:l + 1].contiguous() for l in range(wl.L)]

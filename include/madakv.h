@@ -103,6 +103,11 @@ typedef struct madakv_strides {
  * each other's results, and may leave counters behind that spoil later calls until the buffer is zeroed again.   */
 int madakv_workspace_bytes(const madakv_config* cfg, size_t* bytes_out);
 
+/* Bytes at which madakv_prefill_attn, madakv_prefill_attn_keep and madakv_tree_attn have all the room that they make use of: up to
+ * 20 MB more for heads of 64, 39 for 128. In less, down to madakv_workspace_bytes, they share keys out over fewer blocks (a number of which the last bits of a
+ * result depend on), or over none, and calls of few queries on many keys take longer. Other calls need no more than madakv_workspace_bytes. */
+int madakv_workspace_bytes_attn(const madakv_config* cfg, size_t* bytes_out);
+
 /* Stage 1 (Eq. 7 with the softmax of Eq. 5). For unit (b,l,h) and key i < seq_len[b]:
  *   psi[u][i] = sum over the g query heads of the KV group and over window rows r of
  *               softmax_i( scale * q_win[b,l,hq,r,:] . k[b,l,h,i,:] )

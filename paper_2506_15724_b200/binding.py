@@ -21,7 +21,7 @@ STATUS_NAMES = ["OK", "EINVAL", "ESHAPE", "EALIGN", "EWORKSPACE", "ECAPACITY", "
 STATIC_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = [
-    "madakv_abi_version", "madakv_status_string", "madakv_workspace_bytes", "madakv_score", "madakv_score_lse",
+    "madakv_abi_version", "madakv_status_string", "madakv_workspace_bytes", "madakv_workspace_bytes_attn", "madakv_score", "madakv_score_lse",
     "madakv_score_kept",
     "madakv_allocate", "madakv_allocate_layer", "madakv_demand_layer",
     "madakv_select", "madakv_compact", "madakv_decode_attn", "madakv_decode_attn_static", "madakv_poll_status",
@@ -68,7 +68,7 @@ def lib():
         L.madakv_abi_version.restype = ctypes.c_int
         L.madakv_status_string.restype = ctypes.c_char_p
         L.madakv_status_string.argtypes = [ctypes.c_int]
-        L.madakv_workspace_bytes.argtypes = [cfgp, ctypes.POINTER(sz)]
+        L.madakv_workspace_bytes.argtypes = L.madakv_workspace_bytes_attn.argtypes = [cfgp, ctypes.POINTER(sz)]
         L.madakv_score.argtypes = [cfgp, vp, MadakvStrides, vp, MadakvStrides, vp, vp, vp, vp, sz, vp]
         L.madakv_score_lse.argtypes = [cfgp, vp, MadakvStrides, vp, MadakvStrides, vp, vp, vp, vp, sz, vp]
         L.madakv_score_kept.argtypes = [cfgp, vp, MadakvStrides, vp, MadakvStrides, vp, vp, vp, vp, vp, sz, vp]
@@ -145,9 +145,15 @@ def madakv_workspace_bytes(cfg):
     return out.value
 
 
-def new_workspace(cfg, device="cuda"):
-    """A zeroed device workspace of the size the library asks for."""
-    return torch.zeros(madakv_workspace_bytes(cfg), dtype=torch.uint8, device=device)
+def madakv_workspace_bytes_attn(cfg):
+    out = ctypes.c_size_t(0)
+    _check("madakv_workspace_bytes_attn", lib().madakv_workspace_bytes_attn(cfg, ctypes.byref(out)))
+    return out.value
+
+
+def new_workspace(cfg, device="cuda", attention=True):
+    """A zeroed device workspace. attention: with room for the shares of prompt and tree attention, up to 39 MB that other calls do without."""
+    return torch.zeros((madakv_workspace_bytes_attn if attention else madakv_workspace_bytes)(cfg), dtype=torch.uint8, device=device)
 
 
 def madakv_score(cfg, q_win, k, seq_len, lse, psi, ws):
@@ -309,7 +315,7 @@ class EvictionBuffers:
         # kept_idx holds the position of every row of the segments. (To be set by who fills it in other ways than run_eviction, a replayed
         # graph of it included, after steps without positions.)
         self.placed = True
-        self.ws = new_workspace(cfg, device)
+        self.ws = new_workspace(cfg, device, attention=want_lse or not quant)  # (neither run_prefill nor run_tree else)
         self.psi = z((B, L, Hkv, n), torch.float32)
         self.lse = z((B, L, Hq, cfg.window), torch.float32) if want_lse else None
         # run_prefill's proxy tokens, and for how many keys they are complete (lse holds the log-sum-exps of queries that run_eviction is given)

@@ -34,6 +34,14 @@ int madakv_workspace_bytes(const madakv_config* cfg, size_t* bytes_out) {
   return MADAKV_OK;
 }
 
+int madakv_workspace_bytes_attn(const madakv_config* cfg, size_t* bytes_out) {
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  if (!bytes_out) return MADAKV_EINVAL;
+  *bytes_out = ws_bytes_attn(*cfg);
+  return MADAKV_OK;
+}
+
 int madakv_score(const madakv_config* cfg, const void* q_win, madakv_strides sq, const void* k, madakv_strides sk,
                  const int32_t* seq_len, float* lse, float* psi, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_config(cfg);
@@ -291,7 +299,7 @@ static bool all_strides_ok(const madakv_config& c, std::initializer_list<madakv_
   return true;
 }
 
-static int prefill(const madakv_config* cfg, int32_t layer, const PromptCall& a, void* ws, size_t ws_bytes, void* stream) {
+static int prefill(const madakv_config* cfg, int32_t layer, PromptCall a, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_config(cfg);
   if (rc) return rc;
   if (!a.q || !a.k || !a.v || !a.out) return MADAKV_EINVAL;
@@ -304,6 +312,7 @@ static int prefill(const madakv_config* cfg, int32_t layer, const PromptCall& a,
     return MADAKV_EALIGN;
   if (!all_strides_ok(*cfg, {a.sq, a.sk, a.sv, a.so})) return MADAKV_EALIGN;
   if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
+  a.part_rows = attn_part_rows(*cfg, ws_bytes);
   return launch_prefill_attn(*cfg, layer, a, ws, (cudaStream_t)stream);
 }
 
@@ -311,7 +320,7 @@ int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, 
                         const int64_t* q_off, const int32_t* q_len, const void* k, madakv_strides sk, const void* v,
                         madakv_strides sv, int64_t k_rows, const int64_t* k_off, const int32_t* seq_len, void* out,
                         madakv_strides so, float* lse_out, void* q_win, float* lse_win, void* ws, size_t ws_bytes, void* stream) {
-  return prefill(cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win, nullptr},
+  return prefill(cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win, nullptr, 0},
                  ws, ws_bytes, stream);
 }
 
@@ -321,7 +330,7 @@ int madakv_prefill_attn_keep(const madakv_config* cfg, int32_t layer, const void
                              madakv_strides so, float* lse_out, void* q_win, float* lse_win, int32_t* win_len, void* ws,
                              size_t ws_bytes, void* stream) {
   if (!q_win || !lse_win || !win_len) return MADAKV_EINVAL;
-  return prefill(cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win, win_len},
+  return prefill(cfg, layer, {q, sq, q_rows, q_off, q_len, k, sk, v, sv, k_rows, k_off, seq_len, out, so, lse_out, q_win, lse_win, win_len, 0},
                  ws, ws_bytes, stream);
 }
 
@@ -344,11 +353,12 @@ int madakv_tree_attn(const madakv_config* cfg, int32_t layer, int32_t nodes, con
                      void* out, madakv_strides so, float* lse_out, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_config(cfg);
   if (rc) return rc;
-  const TreeCall a{nodes, q, sq, k_tree, sk, v_tree, sv, mask, n_nodes, seg_off, capacity};
+  TreeCall a{nodes, q, sq, k_tree, sk, v_tree, sv, mask, n_nodes, seg_off, capacity, 0};
   if (!q || !out) return MADAKV_EINVAL;
   if ((rc = check_tree(cfg, layer, a, k_c, v_c, kept_len))) return rc;
   if (!aligned16(q) || !aligned16(out) || ((uintptr_t)lse_out & 3) || !all_strides_ok(*cfg, {sq, so})) return MADAKV_EALIGN;
   if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
+  a.part_rows = attn_part_rows(*cfg, ws_bytes);
   return launch_tree_attn(*cfg, layer, a, k_c, v_c, kept_len, out, so, lse_out, ws, (cudaStream_t)stream);
 }
 
@@ -358,7 +368,7 @@ int madakv_tree_commit(const madakv_config* cfg, int32_t layer, int32_t nodes, c
                        const int32_t* position, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_config(cfg);
   if (rc) return rc;
-  const TreeCall a{nodes, nullptr, sk, k_tree, sk, v_tree, sv, mask, n_nodes, seg_off, capacity};
+  const TreeCall a{nodes, nullptr, sk, k_tree, sk, v_tree, sv, mask, n_nodes, seg_off, capacity, 0};
   if (!node || (kept_idx == nullptr) != (position == nullptr)) return MADAKV_EINVAL;
   if ((rc = check_tree(cfg, layer, a, k_c, v_c, kept_len))) return rc;
   if (((uintptr_t)node & 3) || ((uintptr_t)acc & 3) || ((uintptr_t)kept_idx & 3) || ((uintptr_t)position & 3)) return MADAKV_EALIGN;

@@ -6,7 +6,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-AttnParams base_params(const madakv_config& c, int layer, void* ws) {
+AttnParams base_params(const madakv_config& c, int layer, void* ws, int part_rows) {
   AttnParams p = {};
   p.B = c.batch;
   p.L = c.n_layers;
@@ -20,6 +20,7 @@ AttnParams base_params(const madakv_config& c, int layer, void* ws) {
   p.n_max = c.max_seq_len;
   p.scale2 = scale_of(c) * kLog2e;
   p.ws = ws;
+  p.part_rows = part_rows;
   return p;
 }
 int launch(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t st) {
@@ -31,7 +32,7 @@ int launch(const AttnParams& p, const madakv_config& c, bool tree, cudaStream_t 
 }  // namespace
 
 int launch_prefill_attn(const madakv_config& c, int layer, const PromptCall& a, void* ws, cudaStream_t st) {
-  AttnParams p = base_params(c, layer, ws);
+  AttnParams p = base_params(c, layer, ws, a.part_rows);
   if (p.g > kMaxGroup) return MADAKV_EUNSUPPORTED;
   const int64_t e = elem_bytes(c);
   auto at = [&](const void* x, const madakv_strides& s) { return (void*)((char*)x + layer * s.layer * e); };
@@ -62,7 +63,7 @@ int launch_prefill_attn(const madakv_config& c, int layer, const PromptCall& a, 
 
 int launch_tree_attn(const madakv_config& c, int layer, const TreeCall& a, const void* k_c, const void* v_c, const int32_t* kept_len,
                      void* out, madakv_strides so, float* lse_out, void* ws, cudaStream_t st) {
-  AttnParams p = base_params(c, layer, ws);
+  AttnParams p = base_params(c, layer, ws, a.part_rows);
   if (p.g > kMaxGroup) return MADAKV_EUNSUPPORTED;
   p.q = a.q;
   p.sq = a.sq;

@@ -42,6 +42,7 @@ struct AttnParams {
   // shares of the keys: partial results [item, slot, row of the tile, D] and their (max, in the logarithm to base 2, sum) [item, slot, row]
   float* part;
   float2* part_ml;
+  int part_rows;       // rows that there is room for
   int slots, least_tiles;
   int tile_keys;       // keys of a tile
   int* order;          // tree, null or: the number of items that have rows, then those items, the longest first
@@ -270,7 +271,7 @@ inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int til
   p.tile_rows = (int)(p.tile_q < p.q_rows ? p.tile_q : p.q_rows) * p.g;
   const float most = (float)(keys / tile_keys + 1), mean = most - (!tree && p.causal ? (float)(queries < keys ? queries : keys) / (2 * tile_keys) : 0.f);
   const float tile = p.q_rows > p.tile_q / 2 ? cost.whole : cost.half;
-  const int64_t by_room = p.n_items ? kAttnPartRows / (p.n_items * p.tile_rows) : 1;
+  const int64_t by_room = p.n_items ? p.part_rows / (p.n_items * p.tile_rows) : 1;
   float best = 0.f;
   p.slots = 1;
   for (int s = 1; s <= kAttnSlots && (s == 1 || (s <= by_room && 2 * s <= most + 1.f && most >= (float)cost.least)); ++s) {
@@ -282,7 +283,7 @@ inline void attn_slots(AttnParams& p, const madakv_config& c, bool tree, int til
   p.least_tiles = cost.least;
   p.tile_keys = tile_keys;
   p.part = reinterpret_cast<float*>((char*)p.ws + ws_layout(c).decode_off);
-  p.part_ml = reinterpret_cast<float2*>(p.part + (int64_t)kAttnPartRows * c.head_dim);
+  p.part_ml = reinterpret_cast<float2*>(p.part + (int64_t)p.part_rows * c.head_dim);
 }
 
 int launch_window_move(const AttnParams& p, const madakv_config& c, cudaStream_t st);  // ahead of a call whose windows keep earlier rows

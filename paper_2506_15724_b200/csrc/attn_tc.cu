@@ -839,7 +839,7 @@ int run(AttnParams p, const madakv_config& c, cudaStream_t st) {
   };
   p.wide_out = wide(p.out, p.so);
   p.wide_q = wide(p.q, p.sq) && (uintptr_t)p.q_win % 32 == 0;
-  if (kTree && p.slots == 1 && p.n_items > 148 && p.n_items < (int64_t)kAttnPartRows * D) {
+  if (kTree && p.slots == 1 && p.n_items > 148 && p.n_items < (int64_t)p.part_rows * D) {
     p.order = reinterpret_cast<int*>(p.part);  // (no shares: the place of their results is free)
     const float most = 1.7f * (float)(((int64_t)c.max_seq_len + c.max_new_tokens) / kKeys + 2) + 4.f;
     launch_pdl(order_kernel, dim3(1), dim3(kClasses), 0, st, p, (kClasses - 1) / most);

@@ -23,7 +23,7 @@ namespace madakv {
 //                            log-sum-exp [units * rows] fp32 (rows = g * w padded to a multiple of 32), per-chunk
 //                            partial (max, sum) pairs, the bf16 terms of small fp32 calls (see ws_layout)
 //   [.., .. + decode)        stage 5 scratch: split partials [B * L * H_q * splits * (d + 2)] fp32; attention of prompts and of
-//                            drafted trees has its partials in the same place [kAttnPartRows * (d + 2)]
+//                            drafted trees has its partials in the same place, as many as the caller's workspace has room for
 // Stages 2-3 keep their scratch in shared memory.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr size_t kHeaderBytes = 256;
@@ -31,7 +31,9 @@ constexpr int kScoreChunk = 1024;   // keys per (max, sum) partial of the generi
 constexpr int kScoreTcChunk = 512;  // keys per work item (and per partial) of the tensor-core scoring path
 constexpr int kCounters = 16384;
 constexpr int kDecodeChunk = 256;   // cache rows per split of decode attention
-constexpr int kAttnPartRows = 2 * 148 * 256;  // rows of partial results of prompt and tree attention: two tiles of 256 for every SM
+// Rows of partial results that prompt and tree attention make use of: two tiles of 256 for every SM. (With less room they share out keys over fewer
+// blocks: 67 newest queries on 2 x 100003 keys, 32 heads, 313 us, in the workspace that other calls need 467; 16 nodes on 4 x 8192 rows 18.0 and 43.5.)
+constexpr int kAttnPartRows = 2 * 148 * 256;
 
 struct WsHeader {
   int32_t status;        // madakv_status set by device code
@@ -121,9 +123,7 @@ inline WsLayout ws_layout(const madakv_config& c) {
   w.score_split_off = off;
   off = align_up(off + split_area_bytes(c), 256);
   w.decode_off = off;
-  size_t rows_of_partials = (size_t)c.batch * c.n_layers * c.n_q_heads * (size_t)w.decode_splits;
-  if (rows_of_partials < kAttnPartRows) rows_of_partials = kAttnPartRows;
-  off = align_up(off + rows_of_partials * (c.head_dim + 2) * sizeof(float), 256);
+  off = align_up(off + (size_t)c.batch * c.n_layers * c.n_q_heads * (size_t)w.decode_splits * (c.head_dim + 2) * sizeof(float), 256);
   w.total = off;
   return w;
 }
@@ -164,6 +164,21 @@ inline int check_ws(const madakv_config& c, const void* ws, size_t ws_bytes) {
   if ((uintptr_t)ws & 255) return MADAKV_EALIGN;
   if (ws_bytes < ws_layout(c).total) return MADAKV_EWORKSPACE;
   return MADAKV_OK;
+}
+// Room for such rows in a workspace, and the bytes that give all that calls of this config make use of: as many shares of two tiles of 64 keys or
+// more as its longest segment has, of all rows that a call on one layer's prompts or on all layers' trees may have.
+inline int attn_part_rows(const madakv_config& c, size_t ws_bytes) {
+  const size_t rows = (ws_bytes - ws_layout(c).decode_off) / ((c.head_dim + 2) * sizeof(float));
+  return rows < kAttnPartRows ? (int)rows : kAttnPartRows;
+}
+inline size_t ws_bytes_attn(const madakv_config& c) {
+  const WsLayout w = ws_layout(c);
+  const size_t tiles = ((size_t)c.max_seq_len + c.max_new_tokens) / 64 + 1, shares = (tiles + 1) / 2 < 32 ? (tiles + 1) / 2 : 32;
+  const size_t prompt = (size_t)c.max_seq_len + 256, tree = 128 * (size_t)c.n_layers;  // queries of a head, filled up to whole items
+  size_t rows = shares > 1 ? shares * c.batch * c.n_q_heads * (prompt > tree ? prompt : tree) : 0;
+  if (rows > kAttnPartRows) rows = kAttnPartRows;
+  const size_t all = align_up(w.decode_off + rows * (c.head_dim + 2) * sizeof(float), 256);
+  return all > w.total ? all : w.total;
 }
 inline float scale_of(const madakv_config& c) {
   return c.softmax_scale > 0.0f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim);
@@ -342,6 +357,7 @@ struct PromptCall {
   void* q_win;
   float* lse_win;
   int32_t* win_len;  // null: windows are written in full
+  int part_rows;     // room for partial results
 };
 struct TreeCall {
   int nodes;
@@ -355,6 +371,7 @@ struct TreeCall {
   const int32_t* n_nodes;
   const int64_t* seg_off;
   int64_t capacity;
+  int part_rows;
 };
 int launch_prefill_attn(const madakv_config& c, int layer, const PromptCall& a, void* ws, cudaStream_t st);
 int launch_window_check(const madakv_config& c, const int32_t* seq_len, int32_t* win_len, void* ws, cudaStream_t st);

@@ -173,3 +173,57 @@ def shifted(x):
     y = torch.full((*x.shape[:-1], x.shape[-1] + e), SENTINEL, device="cuda").to(x.dtype)[..., e:]
     y.copy_(x)
     return y
+
+
+# ------------------------------------------------------------------------------------------------- workspaces
+def test_workspaces_of_callers_without_attention_are_small(lib):  # noqa: F811
+    """What a layer of 2048 tokens of 28 / 4 heads needs for eviction and decode is a few counters, log-sum-exps and partials."""
+    assert mk.madakv_workspace_bytes(config("bf16", 1, 1, 28, 4, 128, 2048, 32)) < 2 << 20
+    assert mk.madakv_workspace_bytes(config("f32", 1, 1, 4, 4, 64, 512, 8)) < 2 << 20
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_in_the_smallest_workspace(dtype, d):
+    """No room for shares of the keys, room for some, room for all."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    n, m, T = 9000, 30, 9
+    cfg = config(dtype, 1, 1, 4, 2, d, n)
+    least, most = mk.madakv_workspace_bytes(cfg), mk.new_workspace(cfg).numel()
+    q, k, v = normal(gen, (1, 1, 4, m, d), dtype), normal(gen, (1, 1, 2, n, d), dtype), normal(gen, (1, 1, 2, n, d), dtype)
+    seg = Segments(gen, dtype, [n, 700], d)
+    qt, kt, vt = normal(gen, (1, 1, 4, T, d), dtype), normal(gen, (1, 1, 2, T, d), dtype), normal(gen, (1, 1, 2, T, d), dtype)
+    mask = as_int64([[(1 << (i + 1)) - 1 for i in range(T)]])
+    for size in (least, least + 4 * m * 3 * (d + 2) * 4, most):
+        space = torch.zeros(size + 4096, dtype=torch.uint8, device="cuda")
+        space[size:] = 77
+        ws = space[:size]
+        out, lse, ot, yt = torch.empty_like(q), torch.empty((1, 1, 4, m), device="cuda"), torch.empty_like(qt), torch.empty((1, 1, 4, T), device="cuda")
+        mk.madakv_prefill_attn(cfg, 0, q, k, v, out, ws, lse_out=lse, seq_len=i32(n), q_len=i32(m))
+        mk.madakv_tree_attn(cfg, -1, qt, kt, vt, mask, seg.k, seg.v, seg.seg_off, seg.kept_len, ot, yt, ws)
+        assert mk.madakv_poll_status(ws) == 0 and torch.all(space[size:] == 77)
+        see = torch.arange(n, device="cuda") <= torch.arange(m, device="cuda").view(-1, 1) + n - m
+        for h in range(4):
+            a, rows = seg.off[h // 2], seg.lens[h // 2]
+            check(dtype, q[0, 0, h], k[0, 0, h // 2], v[0, 0, h // 2], see, d ** -0.5, out[0, 0, h], lse[0, 0, h])
+            check(dtype, qt[0, 0, h], torch.cat((seg.k[a:a + rows], kt[0, 0, h // 2])), torch.cat((seg.v[a:a + rows], vt[0, 0, h // 2])),
+                  torch.cat((torch.ones((T, rows), dtype=torch.bool, device="cuda"), causal(T)), 1), d ** -0.5, ot[0, 0, h], yt[0, 0, h])
+
+
+@pytest.mark.gpu
+def test_many_tree_items_in_the_smallest_workspace():
+    """More items than blocks: the list of them in the order of what they cost needs room too."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    B, H, T, d, lens = 2, 100, 3, 64, [70, 0, 150, 9]
+    seg = Segments(gen, "bf16", [lens[u % 4] for u in range(B * H)], d)
+    cfg = config("bf16", B, 1, H, H, d, 150)
+    q, k, v = (normal(gen, (B, 1, H, T, d), "bf16") for _ in range(3))
+    got = []
+    for size in (mk.madakv_workspace_bytes(cfg), mk.new_workspace(cfg).numel()):
+        space = torch.zeros(size + 4096, dtype=torch.uint8, device="cuda")
+        space[size:] = 77
+        got.append(torch.empty_like(q))
+        mk.madakv_tree_attn(cfg, -1, q, k, v, as_int64([[1, 3, 7]] * B), seg.k, seg.v, seg.seg_off, seg.kept_len, got[-1], None, space[:size])
+        assert mk.madakv_poll_status(space[:size]) == 0 and torch.all(space[size:] == 77)
+    assert torch.equal(*got)
