@@ -306,6 +306,8 @@ static int prefill(const madakv_config* cfg, int32_t layer, PromptCall a, void* 
   if ((a.k_off != nullptr) == (a.seq_len != nullptr) || (a.q_off && a.q_len)) return MADAKV_EINVAL;
   if (layer < 0 || layer >= cfg->n_layers || a.q_rows <= 0 || a.k_rows <= 0) return MADAKV_ESHAPE;
   if (a.q_rows > 0x7fffffffll || a.k_rows > 0x7fffffffll) return MADAKV_EUNSUPPORTED;
+  if (a.q_off) a.sq.batch = a.so.batch = 0;  // (packed: not used, whatever stands there)
+  if (a.k_off) a.sk.batch = a.sv.batch = 0;
   if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.out) || !aligned16(a.q_win) || ((uintptr_t)a.q_off & 7) ||
       ((uintptr_t)a.k_off & 7) || ((uintptr_t)a.q_len & 3) || ((uintptr_t)a.seq_len & 3) || ((uintptr_t)a.lse_out & 3) ||
       ((uintptr_t)a.lse_win & 3) || ((uintptr_t)a.win_len & 3))

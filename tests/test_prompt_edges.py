@@ -227,3 +227,18 @@ def test_many_tree_items_in_the_smallest_workspace():
         mk.madakv_tree_attn(cfg, -1, q, k, v, as_int64([[1, 3, 7]] * B), seg.k, seg.v, seg.seg_off, seg.kept_len, got[-1], None, space[:size])
         assert mk.madakv_poll_status(space[:size]) == 0 and torch.all(space[size:] == 77)
     assert torch.equal(*got)
+
+
+# ------------------------------------------------------------------------------------------------- refusals
+
+
+def test_batch_strides_of_packed_sequences_are_not_used(lib):  # noqa: F811
+    c = config(B=2)
+    odd, st = mk.MadakvStrides(1, 4 * 512 * 128, 512 * 128, 128), mk.MadakvStrides(4 * 512 * 128, 4 * 512 * 128, 512 * 128, 128)
+
+    def call(sq, skv, so, q_off, k_off):
+        return lib.madakv_prefill_attn(ctypes.byref(c), 0, FAKE, sq, 512, q_off, None, FAKE, skv, FAKE, skv, 512, k_off, None if k_off else FAKE, FAKE, so,
+                                       None, None, None, FAKE, mk.madakv_workspace_bytes(c) - 1, None)
+
+    assert call(odd, odd, odd, FAKE, FAKE) == call(st, odd, st, None, FAKE) == call(odd, st, odd, FAKE, None) == mk.EWORKSPACE
+    assert call(odd, st, st, None, None) == call(st, odd, st, None, None) == call(st, st, odd, None, FAKE) == call(st, odd, st, FAKE, None) == mk.EALIGN
