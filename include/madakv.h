@@ -368,7 +368,8 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  * Up to 128 / g queries of a sequence share a tile of rows (g = H_q / H_kv), which reads whole tiles of up to 128 keys as far as the last of them
  * sees: a row of v that is not finite makes NaN of results of the same KV head's queries up to 126 + floor(128 / g) positions before it too.
  * What stands behind a sequence's last key is never used.
- * out, lse_out, q_win and lse_win overlap neither one another nor an input; out has no dimension of stride 0.
+ * out, lse_out, q_win and lse_win overlap neither one another nor an input; out has no dimension of stride 0 among those that the call writes
+ * (MADAKV_EINVAL). Stretches of q_off do not overlap one another.
  * Deterministic. Where few queries see many keys the keys are shared out over blocks; a second launch joins the partial results, which stand
  * in the workspace. (How many shares goes by q_rows, k_rows and n_max, which the host knows: few queries in a large buffer, with q_len
  * saying so, are not shared out. Pass a view of the rows that are there.) A bounded wait that runs out is recorded as MADAKV_ETIMEOUT; the call's results are then not to be used, the next
@@ -404,7 +405,7 @@ int madakv_prefill_attn_keep(const madakv_config* cfg, int32_t layer, const void
  *   k_c, v_c, seg_off, kept_len, capacity: the ragged cache, as in madakv_decode_attn; layer -1 means all layers
  * madakv_tree_attn: node i attends to all rows of every segment and to the nodes that it sees. A node that sees nothing (an empty segment, no
  * bit set) gets out = 0 and lse = -inf; a segment that selection refused counts as empty. The cache is only read.
- *   lse_out [B, L, H_q, T] fp32, contiguous, or null
+ *   lse_out [B, L, H_q, T] fp32, contiguous, or null; out as in madakv_prefill_attn
  * Rows of out and lse_out of nodes that are not there are left as they were. Roundings as in madakv_prefill_attn; H_q / H_kv at most 64. A
  * row of the segment's or of a node's value that is not finite makes NaN of the results of all nodes on the same segment, seen or not. (A tree of one
  * node rounds its weights to bf16 for any g; madakv_decode_attn does from g = 3 on.)                                                    */
@@ -415,7 +416,7 @@ int madakv_tree_attn(const madakv_config* cfg, int32_t layer, int32_t nodes, con
 
 /* Appends to every segment of sequence b the rows of k_tree and v_tree of the nodes that mask[b][node[b]] names, in ascending order, and
  * makes kept_len longer by them. node [B] int32: the last accepted node, negative: none. A segment without room for all of them is left
- * as it is and MADAKV_ECAPACITY is recorded; a node that is not there (node[b] >= n_nodes[b]) appends nothing and records MADAKV_ESHAPE.
+ * as it is and MADAKV_ECAPACITY is recorded (k_tree and v_tree do not lie in the cache); a node that is not there (node[b] >= n_nodes[b]) appends nothing and records MADAKV_ESHAPE.
  *   acc      [capacity] fp32 or null: an appended row starts with weight 0
  *   kept_idx [capacity] int32 and position [B] int32, both or neither: row i of the path gets position[b] + i                    */
 int madakv_tree_commit(const madakv_config* cfg, int32_t layer, int32_t nodes, const uint64_t* mask, const int32_t* n_nodes,

@@ -298,6 +298,10 @@ static bool all_strides_ok(const madakv_config& c, std::initializer_list<madakv_
     if (!strides_ok(c, s)) return false;
   return true;
 }
+// No dimension of more than one element of what a call writes has stride 0.
+static bool rows_apart(int64_t batch, int64_t layers, int64_t heads, const madakv_strides& s) {
+  return (batch <= 1 || s.batch) && (layers <= 1 || s.layer) && (heads <= 1 || s.head);
+}
 
 static int prefill(const madakv_config* cfg, int32_t layer, PromptCall a, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_config(cfg);
@@ -313,6 +317,7 @@ static int prefill(const madakv_config* cfg, int32_t layer, PromptCall a, void* 
       ((uintptr_t)a.lse_win & 3) || ((uintptr_t)a.win_len & 3))
     return MADAKV_EALIGN;
   if (!all_strides_ok(*cfg, {a.sq, a.sk, a.sv, a.so})) return MADAKV_EALIGN;
+  if (!rows_apart(a.q_off ? 1 : cfg->batch, 1, cfg->n_q_heads, a.so)) return MADAKV_EINVAL;
   if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
   a.part_rows = attn_part_rows(*cfg, ws_bytes);
   return launch_prefill_attn(*cfg, layer, a, ws, (cudaStream_t)stream);
@@ -359,6 +364,7 @@ int madakv_tree_attn(const madakv_config* cfg, int32_t layer, int32_t nodes, con
   if (!q || !out) return MADAKV_EINVAL;
   if ((rc = check_tree(cfg, layer, a, k_c, v_c, kept_len))) return rc;
   if (!aligned16(q) || !aligned16(out) || ((uintptr_t)lse_out & 3) || !all_strides_ok(*cfg, {sq, so})) return MADAKV_EALIGN;
+  if (!rows_apart(cfg->batch, layer < 0 ? cfg->n_layers : 1, cfg->n_q_heads, so)) return MADAKV_EINVAL;
   if ((rc = check_ws(*cfg, ws, ws_bytes))) return rc;
   a.part_rows = attn_part_rows(*cfg, ws_bytes);
   return launch_tree_attn(*cfg, layer, a, k_c, v_c, kept_len, out, so, lse_out, ws, (cudaStream_t)stream);

@@ -2,6 +2,7 @@
 // status comes back as an int. What bounds a call on one layer is the host: with the arguments gathered in Python and handed
 // over by ctypes a decode call took 5.4 us, here 3.1, nearly all of it the launch.
 #define PY_SSIZE_T_CLEAN
+#include <ATen/MemoryOverlap.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -301,6 +302,23 @@ struct Checked : Args {
   }
 };
 
+// What a call writes shares no memory with its inputs nor with what else it writes (arguments by number, after all have been checked). Views of one
+// storage that leave gaps for one another are taken to do so on purpose, unless they begin at the same element.
+void check_apart(PyObject* const* args, std::initializer_list<int> written, std::initializer_list<int> read, std::initializer_list<const char*> names) {
+  const at::Tensor* all[16];
+  int n = 0;
+  for (const auto& list : {written, read})
+    for (const int i : list) all[n++] = args[i] == Py_None ? nullptr : &THPVariable_Unpack(args[i]);
+  auto held = [](const at::Tensor* t) { return t->unsafeGetTensorImpl()->unsafe_storage().unsafeGetStorageImpl(); };
+  for (int w = 0; w < (int)written.size(); ++w)
+    for (int i = w + 1; i < n; ++i) {
+      if (!all[w] || !all[i] || held(all[w]) != held(all[i]) || !all[w]->numel() || !all[i]->numel()) continue;
+      const at::MemOverlapStatus s = at::get_overlap_status(*all[w], *all[i]);
+      if (s == at::MemOverlapStatus::Full || s == at::MemOverlapStatus::Partial || all[w]->data_ptr() == all[i]->data_ptr())
+        Checked::wrong(names.begin()[w], "overlaps another tensor of the call");
+    }
+}
+
 struct QuantCache {
   uint8_t *k_code, *v_code;
   void *k_par, *v_par;
@@ -480,6 +498,7 @@ PyObject* prefill_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int64_t *q_off = a.array<int64_t>("q_off", at::kLong, B + 1, true, true), *k_off = a.array<int64_t>("k_off", at::kLong, B + 1, true, true);
   const int32_t *seq_len = a.array<int32_t>("seq_len", at::kInt, B, true), *q_len = a.array<int32_t>("q_len", at::kInt, B, true);
   int32_t* win_len = a.array<int32_t>("win_len", at::kInt, B * a.cfg->n_layers, true, true);
+  check_apart(args, {5, 7, 8, 9}, {2, 3, 4}, {"out", "lse_out", "q_win", "lse_win"});
   return without_lock([&] {
     if (win_len)
       return madakv_prefill_attn_keep(a.cfg, layer, q.data, q.st, q.rows, q_off, q_len, k.data, k.st, v.data, v.st, k.rows, k_off, seq_len,
@@ -510,6 +529,7 @@ PyObject* tree_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   size_t bytes;
   void *ws = a.workspace(bytes), *st = stream();
   const int32_t* n_nodes = a.array<int32_t>("n_nodes", at::kInt, a.cfg->batch, true);
+  check_apart(args, {10, 11}, {2, 3, 4, 6, 7}, {"out", "lse_out"});
   return without_lock([&] {
     return madakv_tree_attn(a.cfg, layer, (int32_t)q.rows, q.data, q.st, k.data, k.st, v.data, v.st, (const uint64_t*)mask, n_nodes, k_c,
                             v_c, seg_off, kept_len, capacity, out.data, out.st, lse, ws, bytes, st);
@@ -540,6 +560,7 @@ PyObject* tree_commit(PyObject*, PyObject* const* args, Py_ssize_t n) {
   float* acc = a.array<float>("acc", at::kFloat, capacity, true);
   int32_t* kept_idx = a.array<int32_t>("kept_idx", at::kInt, capacity, true);
   const int32_t* position = a.array<int32_t>("position", at::kInt, B, true);
+  check_apart(args, {6, 7}, {4, 5}, {"k_c", "v_c"});
   return without_lock([&] {
     return madakv_tree_commit(a.cfg, layer, (int32_t)k.rows, (const uint64_t*)mask, n_nodes, node, k.data, k.st, v.data, v.st, k_c, v_c,
                               seg_off, kept_len, capacity, acc, kept_idx, position, ws, bytes, st);

@@ -175,6 +175,20 @@ def shifted(x):
     return y
 
 
+@pytest.mark.gpu
+def test_results_between_the_rows_of_an_input():
+    """Queries and results as two halves of the heads of one tensor: they share its memory and no element."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    n, d = 300, 64
+    cfg = config("bf16", 2, 1, 3, 1, d, n)
+    x = normal(gen, (2, 1, n, 6, d), "bf16").transpose(2, 3)
+    q, out, k, v = x[:, :, :3], x[:, :, 3:], normal(gen, (2, 1, 1, n, d), "bf16"), normal(gen, (2, 1, 1, n, d), "bf16")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), seq_len=i32(n, n))
+    want = torch.empty_like(q)
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, want, mk.new_workspace(cfg), seq_len=i32(n, n))
+    assert torch.equal(out, want) and want.any()
+
+
 # ------------------------------------------------------------------------------------------------- workspaces
 def test_workspaces_of_callers_without_attention_are_small(lib):  # noqa: F811
     """What a layer of 2048 tokens of 28 / 4 heads needs for eviction and decode is a few counters, log-sum-exps and partials."""
@@ -230,6 +244,27 @@ def test_many_tree_items_in_the_smallest_workspace():
 
 
 # ------------------------------------------------------------------------------------------------- refusals
+def test_results_without_strides_are_refused(lib):  # noqa: F811
+    """A dimension of out that the call writes and that has stride 0: rows would be written over one another."""
+    c = config(B=2, L=2)
+    S, short = mk.MadakvStrides, lambda cfg: mk.madakv_workspace_bytes(cfg) - 1  # (so that nothing is launched)
+    st = S(2 * 4 * 512 * 128, 4 * 512 * 128, 512 * 128, 128)
+
+    def prefill(so, q_off=None, cfg=c):
+        return lib.madakv_prefill_attn(ctypes.byref(cfg), 0, FAKE, st, 512, q_off, None, FAKE, st, FAKE, st, 512, None, FAKE, FAKE, so, None, None, None,
+                                       FAKE, short(cfg), None)
+
+    def tree(so, layer=-1, cfg=c):
+        return lib.madakv_tree_attn(ctypes.byref(cfg), layer, 5, FAKE, st, FAKE, st, FAKE, st, FAKE, None, FAKE, FAKE, FAKE, FAKE, 100, FAKE, so, None,
+                                    FAKE, short(cfg), None)
+
+    for call in (prefill, tree):
+        assert call(st) == mk.EWORKSPACE
+        assert call(S(0, st.layer, st.head, st.token)) == call(S(st.batch, st.layer, 0, st.token)) == mk.EINVAL
+        assert call(S(0, st.layer, st.head, st.token), cfg=config(B=1, L=2)) == mk.EWORKSPACE  # (a dimension of one element)
+    assert prefill(S(0, st.layer, st.head, st.token), q_off=FAKE) == mk.EWORKSPACE
+    assert tree(S(st.batch, 0, st.head, st.token)) == mk.EINVAL and tree(S(st.batch, 0, st.head, st.token), layer=1) == mk.EWORKSPACE
+    assert prefill(S(st.batch, 0, st.head, st.token)) == mk.EWORKSPACE  # (one layer is written)
 
 
 def test_batch_strides_of_packed_sequences_are_not_used(lib):  # noqa: F811
@@ -242,3 +277,35 @@ def test_batch_strides_of_packed_sequences_are_not_used(lib):  # noqa: F811
 
     assert call(odd, odd, odd, FAKE, FAKE) == call(st, odd, st, None, FAKE) == call(odd, st, odd, FAKE, None) == mk.EWORKSPACE
     assert call(odd, st, st, None, None) == call(st, odd, st, None, None) == call(st, st, odd, None, FAKE) == call(st, odd, st, FAKE, None) == mk.EALIGN
+
+
+@pytest.mark.gpu
+def test_results_that_overlap_are_refused():
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    cfg = config("bf16", 2, 1, 4, 2, 64, 32)
+    q, k = normal(gen, (2, 1, 4, 32, 64), "bf16"), normal(gen, (2, 1, 2, 32, 64), "bf16")
+    space = torch.zeros(2 * q.numel(), dtype=torch.bfloat16, device="cuda")
+    part = lambda first, like: space[first:first + like.numel()].view(like.shape)  # noqa: E731
+    ok = dict(q=part(0, q), k=k, v=k, out=part(q.numel(), q), ws=mk.new_workspace(cfg), seq_len=i32(32, 32))
+    mk.madakv_prefill_attn(cfg, 0, **ok)
+    win, lse = part(q.numel() - 64, torch.empty((2, 1, 4, 8, 64))), part(q.numel() - 64, torch.empty(2, 1, 4, 64)).view(torch.float32)
+    alone = torch.empty((2, 1, 4, 32), device="cuda")
+    for change in (dict(out=ok["q"]), dict(out=part(q.numel() - 64, q)), dict(q=k[:, :, :1].expand_as(q), out=part(0, q), v=part(64, k)),
+                   dict(out=k.repeat(1, 1, 2, 1, 1), k=k, lse_out=alone, lse_win=alone.view(-1)[:64].view(2, 1, 4, 8)), dict(q_win=win), dict(lse_out=lse)):
+        with pytest.raises(ValueError):
+            mk.madakv_prefill_attn(cfg, 0, **{**ok, **change})
+    with pytest.raises((ValueError, mk.MadakvError)):
+        mk.madakv_prefill_attn(cfg, 0, **{**ok, "out": torch.empty_like(q)[:, :, :1].expand_as(q)})
+    seg = Segments(gen, "bf16", [10, 11, 12, 13], 64)
+    qt, kt = normal(gen, (2, 1, 4, 3, 64), "bf16"), normal(gen, (2, 1, 2, 3, 64), "bf16")
+    tree = dict(q=qt, k_tree=kt, v_tree=kt, mask=torch.ones((2, 3), dtype=torch.int64, device="cuda"), k_c=seg.k, v_c=seg.v, seg_off=seg.seg_off,
+                kept_len=seg.kept_len, out=torch.empty_like(qt), lse_out=None, ws=ok["ws"])
+    mk.madakv_tree_attn(cfg, -1, **tree)
+    for change in (dict(out=qt), dict(q=seg.k[:24].view(qt.shape), out=seg.k[:24].view(qt.shape)), dict(out=seg.v[2:26].view(qt.shape)),
+                   dict(lse_out=tree["out"].view(-1)[:48].view(torch.float32).view(2, 1, 4, 3))):
+        with pytest.raises(ValueError):
+            mk.madakv_tree_attn(cfg, -1, **{**tree, **change})
+    node = i32(0, 0)
+    for change in (dict(k_tree=seg.v[:12].view(kt.shape)), dict(v_tree=seg.v[:12].view(kt.shape))):
+        with pytest.raises(ValueError):
+            mk.madakv_tree_commit(cfg, -1, tree["mask"], node, **{**{x: tree[x] for x in ("k_tree", "v_tree", "k_c", "v_c", "seg_off", "kept_len", "ws")}, **change})
