@@ -410,6 +410,6 @@ class EvictionBuffers:
         if not self.track:
             raise ValueError("run_trim: buffers without track=True accumulate no weights")
         if recent and not self.placed:
-            raise ValueError("run_trim: recent rows cannot be told where run_decode was given no position")
+            raise ValueError("run_trim: recent rows cannot be told where run_decode or run_commit was given no position")
         call = madakv_evict_quant if self.quant else madakv_evict
         call(self.cfg, layer, limit, recent, self.acc, self.kept_idx, self.seg_off, self.kept_len, *self.cache, self.ws)

@@ -309,3 +309,13 @@ def test_results_that_overlap_are_refused():
     for change in (dict(k_tree=seg.v[:12].view(kt.shape)), dict(v_tree=seg.v[:12].view(kt.shape))):
         with pytest.raises(ValueError):
             mk.madakv_tree_commit(cfg, -1, tree["mask"], node, **{**{x: tree[x] for x in ("k_tree", "v_tree", "k_c", "v_c", "seg_off", "kept_len", "ws")}, **change})
+
+
+@pytest.mark.gpu
+def test_trims_name_every_call_that_leaves_positions_out():
+    cfg = config("bf16", n=64)
+    buf = mk.EvictionBuffers(cfg, 400, track=True)
+    k = torch.zeros((1, 1, 4, 1, 128), device="cuda").bfloat16()
+    buf.run_commit(torch.ones((1, 1), dtype=torch.int64, device="cuda"), i32(-1), k, k)
+    with pytest.raises(ValueError, match="run_commit"):
+        buf.run_trim(torch.zeros((1, 1, 4), dtype=torch.int32, device="cuda"), recent=2)
