@@ -108,6 +108,28 @@ def test_infinite_keys_in_fp32(d, at, sign):
     check("f32", qq[some], kk[rest], vv[rest], causal(n)[some][:, rest], d ** -0.5, oo[some], yy[some])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_infinite_values_and_queries_in_fp32(d):
+    """Values: queries before them are what they were; queries: theirs alone."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    n = 300
+    cfg = config("f32", 1, 1, 1, 1, d, n)
+    q, k, v = (normal(gen, (1, 1, 1, n, d), "f32") for _ in range(3))
+    v[0, 0, 0, 170] = math.inf
+    v[0, 0, 0, 171, ::2] = -math.inf
+    q[0, 0, 0, 40, 9] = -math.inf
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 1, n), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=i32(n))
+    rows = torch.arange(n, device="cuda") != 40
+    z = torch.logsumexp((q[0, 0, 0].double().nan_to_num(posinf=0, neginf=0) @ k[0, 0, 0].double().T * d ** -0.5).masked_fill(~causal(n), -math.inf), 1)
+    mag = (q[0, 0, 0].double().nan_to_num(posinf=0, neginf=0).abs() @ k[0, 0, 0].double().abs().T * d ** -0.5).amax(1)
+    most = (d + 8) * 2.0 ** -23 * mag + (n / 16 + 68) * 2.0 ** -23 + 2.0 ** -22 * z.abs()  # (as in check)
+    assert torch.all((lse[0, 0, 0].double() - z).abs()[rows] <= most[rows])
+    rows[170:] = False
+    check("f32", q[0, 0, 0, rows], k[0, 0, 0, :170], v[0, 0, 0, :170], causal(n)[rows, :170], d ** -0.5, out[0, 0, 0, rows], lse[0, 0, 0, rows])
+
+
 # ------------------------------------------------------------------------------------------------- logits beyond what exponentials tell apart
 def check_ties(dtype, q, k, v, see, scale, out, lse):
     """Logits that are exact and equal or very far apart: what is left are roundings of weights, sums and results (as in check)."""
@@ -176,6 +198,44 @@ def shifted(x):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,m", [(400, 400), (90, 90), (9000, 33)])
+def test_rows_on_16_byte_boundaries(dtype, d, n, m):
+    """Whole tiles and part of one, results that go out at once and shares; proxy tokens' queries behind an odd 16 bytes."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    w = 16
+    cfg = config(dtype, 1, 1, 4, 2, d, n, w)
+    q, k, v = normal(gen, (1, 1, 4, m, d), dtype), normal(gen, (1, 1, 2, n, d), dtype), normal(gen, (1, 1, 2, n, d), dtype)
+    ws, e, got = mk.new_workspace(cfg), 16 // q.element_size(), []
+    for f in (lambda x: x, shifted):
+        out = f(torch.full_like(q, SENTINEL))
+        space = torch.full((4 * w * d + e,), SENTINEL, device="cuda").to(DT[dtype])
+        q_win, lse_win = space[0 if f is not shifted else e:][:4 * w * d].view(1, 1, 4, w, d), torch.empty((1, 1, 4, w), device="cuda")
+        mk.madakv_prefill_attn(cfg, 0, f(q), f(k), f(v), out, ws, q_win=q_win, lse_win=lse_win, seq_len=i32(n), q_len=i32(m))
+        if f is shifted:
+            around = out.as_strided((4 * m, e), (d + e, 1), out.storage_offset() - e)
+            assert torch.all(around == SENTINEL) and torch.all(space[:e] == SENTINEL)
+        got.append((out, q_win, lse_win))
+    assert all(torch.equal(x, y) for x, y in zip(*got)) and torch.equal(got[0][1], q[:, :, :, m - w:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_trees_on_16_byte_boundaries(dtype, d):
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    T, seg = 21, Segments(gen, dtype, [5000, 31], d)
+    cfg = config(dtype, 1, 1, 14, 2, d, 5000)
+    q, k, v = normal(gen, (1, 1, 14, T, d), dtype), normal(gen, (1, 1, 2, T, d), dtype), normal(gen, (1, 1, 2, T, d), dtype)
+    mask, ws, got = as_int64([[(1 << (i + 1)) - 1 for i in range(T)]]), mk.new_workspace(cfg), []
+    for f in (lambda x: x, shifted):
+        got.append(f(torch.full_like(q, SENTINEL)))
+        mk.madakv_tree_attn(cfg, -1, f(q), f(k), f(v), mask, seg.k, seg.v, seg.seg_off, seg.kept_len, got[-1], None, ws)
+    assert torch.equal(*got)
+
+
+@pytest.mark.gpu
 def test_results_between_the_rows_of_an_input():
     """Queries and results as two halves of the heads of one tensor: they share its memory and no element."""
     gen = torch.Generator(device="cuda").manual_seed(8)
@@ -187,6 +247,56 @@ def test_results_between_the_rows_of_an_input():
     want = torch.empty_like(q)
     mk.madakv_prefill_attn(cfg, 0, q, k, v, want, mk.new_workspace(cfg), seq_len=i32(n, n))
     assert torch.equal(out, want) and want.any()
+
+
+# ------------------------------------------------------------------------------------------------- trees
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [260.0, 14.0, -300.0])
+@pytest.mark.parametrize("n", [900, 6000])
+def test_tree_logits_far_apart(dtype, d, size, n):
+    """Single rows of the segment and single nodes whose logits stand far above or below the others; the longer segment is shared out."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    T, seg = 30, Segments(gen, dtype, [n], d)
+    cfg = config(dtype, 1, 1, 2, 1, d, n)
+    q, k, v = torch.full((1, 1, 2, T, d), d ** -0.5, device="cuda").to(DT[dtype]), normal(gen, (1, 1, 1, T, d), dtype), normal(gen, (1, 1, 1, T, d), dtype)
+    q[:, :, 1] *= -0.5
+    at = torch.arange(5, n, 37, device="cuda")
+    seg.k[at] = (size * (1.0 + at / n * 0.5)).to(DT[dtype]).unsqueeze(1)
+    k[0, 0, 0, 7::9] = size * 1.75
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 2, T), device="cuda")
+    mk.madakv_tree_attn(cfg, -1, q, k, v, as_int64([[(1 << (i + 1)) - 1 for i in range(T)]]), seg.k, seg.v, seg.seg_off, seg.kept_len, out, lse,
+                        mk.new_workspace(cfg))
+    see = torch.cat((torch.ones((T, n), dtype=torch.bool, device="cuda"), causal(T)), 1)
+    for h in range(2):
+        check(dtype, q[0, 0, h], torch.cat((seg.k[:n], k[0, 0, 0])), torch.cat((seg.v[:n], v[0, 0, 0])), see, d ** -0.5, out[0, 0, h], lse[0, 0, h])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [300, 6000])
+def test_tree_keys_that_are_no_numbers(dtype, d, n):
+    """A NaN in a node's key: in the results of the nodes that see it; one in a row of a segment: in those of its heads and of no other's."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    T, seg = 20, Segments(gen, dtype, [n, n], d)
+    cfg = config(dtype, 1, 1, 4, 2, d, n)
+    q, k, v = normal(gen, (1, 1, 4, T, d), dtype), normal(gen, (1, 1, 2, T, d), dtype), normal(gen, (1, 1, 2, T, d), dtype)
+    k[0, 0, 0, 8, 3] = math.nan
+    seg.k[seg.off[1] + n - 7, d - 1] = math.nan
+    masks = [[(1 << (i + 1)) - 1 if i % 2 == 0 else 1 << i for i in range(T)]]
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 4, T), device="cuda")
+    mk.madakv_tree_attn(cfg, -1, q, k, v, as_int64(masks), seg.k, seg.v, seg.seg_off, seg.kept_len, out, lse, mk.new_workspace(cfg))
+    assert out[0, 0, 2:].isnan().all() and lse[0, 0, 2:].isnan().all()
+    bad = torch.tensor([bool(masks[0][i] >> 8 & 1) for i in range(T)], device="cuda")
+    assert bad.any() and not bad.all()
+    see = torch.tensor([[bool(masks[0][i] >> j & 1) for j in range(T)] for i in range(T)], device="cuda")
+    see = torch.cat((torch.ones((T, n), dtype=torch.bool, device="cuda"), see), 1)[~bad]
+    for h in range(2):
+        assert out[0, 0, h, bad].isnan().all() and lse[0, 0, h, bad].isnan().all()
+        check(dtype, q[0, 0, h, ~bad], torch.cat((seg.k[:n], k[0, 0, 0].nan_to_num(0.0))), torch.cat((seg.v[:n], v[0, 0, 0])), see, d ** -0.5,
+              out[0, 0, h, ~bad], lse[0, 0, h, ~bad])
 
 
 # ------------------------------------------------------------------------------------------------- workspaces

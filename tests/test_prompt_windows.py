@@ -164,7 +164,7 @@ class Prompt:
 @pytest.mark.parametrize("packed", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,w,ends", [(64, 16, [200, 400, 495, 500]), (128, 16, [497, 498, 500]), (64, 32, [3, 10, 40, 41, 60, 333, 334, 500]),
-                                      (64, 1, [499, 500]), (128, 40, [5, 333, 363, 393, 423, 453, 483, 500])])
+                                      (64, 1, [499, 500]), (128, 40, [5, 333, 363, 393, 423, 453, 483, 500]), (64, 300, [100, 350, 450, 500])])
 def test_eviction_after_a_prompt_in_chunks(dtype, d, w, ends, packed):
     """Chunks shorter than the window, sequences that end in earlier chunks than others, one shorter than the window."""
     p = Prompt(dtype, [500, 333, 9, 41], w=w, d=d)
@@ -194,6 +194,24 @@ def test_a_longer_prompt_goes_on_from_a_whole_one(dtype):
         p.buf.run_prefill(layer, p.q[:, :, :, :290], p.k[:, :, :, :290], p.v[:, :, :, :290], p.out[:, :, :, :290], seq_len=i32(290, 200))
     for layer in range(p.L):
         p.chunk(layer, 290, 300)
+    p.evict()
+    p.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("last", [0, 5, 40])
+def test_eviction_after_a_packed_prompt(dtype, last):
+    """Queries and keys behind one another, at once or with a last chunk; K and V in padded form for the eviction."""
+    p = Prompt(dtype, [300, 9, 120, 200], w=24)
+    flat = lambda x, a, e: torch.cat([x[b, :, :, a(m):e(m)] for b, m in enumerate(p.lens)], 2)  # noqa: E731
+    off = lambda a, e: torch.tensor([sum(e(m) - a(m) for m in p.lens[:b]) for b in range(p.B + 1)], device="cuda")  # noqa: E731
+    first, zero, full = lambda m: max(0, m - last), lambda m: 0, lambda m: m  # noqa: E731
+    for begin, end in [(zero, full)] if not last else [(zero, first), (first, full)]:
+        q, k, v, k_off = flat(p.q, begin, end), flat(p.k, zero, end), flat(p.v, zero, end), off(zero, end)
+        q_off = off(begin, end) if begin is first else k_off
+        for layer in range(p.L):
+            p.buf.run_prefill(layer, q, k, v, torch.empty_like(q), q_off=q_off, k_off=k_off)
     p.evict()
     p.check()
 
