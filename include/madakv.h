@@ -347,6 +347,7 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  *   k, v    [B, L, H_kv, k_rows, d] dtype, strides sk and sv
  *   With q_off (or k_off) non-null the sequences stand packed behind one another: q and out (k and v) are [L, H, rows, d], their
  *   strides' `batch` is not used, and
+ *     (the other stages take k and v as [B, L, H_kv, n_max, d] only: packed ones are copied into that form before eviction)
  *     q_off, k_off [B + 1] int64: sequence b has rows off[b] .. off[b + 1] - 1. A stretch that ends before it begins or beyond the last
  *           row counts as empty. The lengths follow from it, at most n_max.
  *   Otherwise
@@ -371,7 +372,7 @@ int madakv_evict_quant(const madakv_config* cfg, int32_t layer, const int32_t* l
  * out, lse_out, q_win and lse_win overlap neither one another nor an input; out has no dimension of stride 0 among those that the call writes
  * (MADAKV_EINVAL). Stretches of q_off do not overlap one another.
  * Deterministic. Where few queries see many keys the keys are shared out over blocks; a second launch joins the partial results, which stand
- * in the workspace. (How many shares goes by q_rows, k_rows and n_max, which the host knows: few queries in a large buffer, with q_len
+ * in the workspace. (How many shares goes by q_rows, k_rows, n_max and the workspace's size, which the host knows: few queries in a large buffer, with q_len
  * saying so, are not shared out. Pass a view of the rows that are there.) A bounded wait that runs out is recorded as MADAKV_ETIMEOUT; the call's results are then not to be used, the next
  * call's are whole.                                                                                             */
 int madakv_prefill_attn(const madakv_config* cfg, int32_t layer, const void* q, madakv_strides sq, int64_t q_rows,

@@ -11,8 +11,8 @@
 // The rows of the next tile are on their way from memory while those of one are split, and K of the next tile goes before V of this one,
 // which its products need later (half the chain of a tile).
 // Bound by the chain of a tile, warps 0-3 (three terms of every weight, O added up) and the six products (6 x 512 clocks for
-// 128 x 128 x 64 twice; the tensor pipe takes twice that for tiles as narrow): three prompts of 2503 tokens, 8 heads of 64, take 170 us, 145
-// TFLOP/s at long sequences of heads of 128; by fp32 multiply-adds 660 us, and the pipe for those could not take it below 300.
+// 128 x 128 x 64 twice; the tensor pipe takes twice that for tiles as narrow): three prompts of 2503 tokens, 8 heads of 64, take 173 us; 4096
+// tokens, 28 / 4 heads of 128, 708 us, 170 TFLOP/s; by fp32 multiply-adds 660 us, and the pipe for those could not take it below 300.
 #include "attn_tmem.cuh"
 
 namespace madakv {

