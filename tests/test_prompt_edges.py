@@ -79,6 +79,25 @@ def test_a_value_that_is_no_number_reaches_so_far(dtype, Hq, d, shift, at):
         check(dtype, q[0, 0, h, :clean], k[0, 0, 0], v[0, 0, 0].nan_to_num(0.0), see, d ** -0.5, out[0, 0, h, :clean], lse[0, 0, h, :clean])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rise", [0.0, 0.4, 3.0])
+@pytest.mark.parametrize("n,m", [(3000, 3000), (30000, 50)])
+def test_values_at_the_end_of_their_range(dtype, d, rise, n, m):
+    """Values of 2^96, in either sign, on logits that rise slowly: weights add up far beyond the reference that they are taken against."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    cfg = config(dtype, 1, 1, 1, 1, d, n)
+    q, k, v = normal(gen, (1, 1, 1, m, d), dtype) * 0.1, normal(gen, (1, 1, 1, n, d), dtype), normal(gen, (1, 1, 1, n, d), dtype)
+    q[..., 0] = d ** 0.5
+    k[..., 0] = (torch.arange(n, device="cuda") // 128 * rise).to(DT[dtype])  # (a tile's weights are e^rise of the last one's)
+    v = (torch.sign(v.float()) * 2.0 ** 96).to(DT[dtype])
+    out, lse = torch.empty_like(q), torch.empty((1, 1, 1, m), device="cuda")
+    mk.madakv_prefill_attn(cfg, 0, q, k, v, out, mk.new_workspace(cfg), lse_out=lse, seq_len=i32(n), q_len=i32(m))
+    see = torch.arange(n, device="cuda") <= torch.arange(m, device="cuda").view(-1, 1) + n - m
+    check(dtype, q[0, 0, 0], k[0, 0, 0], v[0, 0, 0], see, d ** -0.5, out[0, 0, 0], lse[0, 0, 0])
+
+
 # ------------------------------------------------------------------------------------------------- infinities in fp32
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
